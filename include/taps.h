@@ -17,6 +17,12 @@
  *   verify_layer      one attention layer of the target over the tree: projections,
  *                     per-head RMSNorm, rotary positions by tree depth, tree attention,
  *                     output projection (the verification forward's layer slice).
+ * Around the round, for serving over a paged cache (the Limitations leave cache management
+ * and sampled decoding to the serving system):
+ *   kv_reserve_paged  pages for the requests' next rows, block tables and slot maps
+ *   kv_append_paged   new K/V rows into the pools through a slot map
+ *   decode_attn_paged attention of one new token per request (a step without a draft)
+ *   taps_sample       tokens from the target's logits at a temperature (the walk's targets)
  *
  * Conventions shared by every call:
  *   - Pointers are DEVICE memory owned by the caller unless marked [host].
@@ -411,6 +417,137 @@ taps_status verify_layer_paged(const void *X, const taps_layer_weights *w, void 
                                int32_t budget, int32_t Hq, int32_t Hkv, int32_t head_dim,
                                int32_t max_ctx, float scale, void *Y, void *ws, size_t ws_bytes,
                                hipStream_t stream);
+
+/* Pages for the next rows of a batch's requests: block tables and slot maps from request
+ * lengths.  Request b is to own the logical rows 0 .. ctx + new - 1, i.e. want = ceil((ctx +
+ * new) / page_rows) pages (ctx = ctx_len[b], at least 0; new = n_new[b] clamped to [0,
+ * max_new]); it holds held_pages[b] (clamped to [0, max_pages]), the first entries of its table
+ * row.  A request with more gives the last ones back, one with fewer takes new ones:
+ *   - every page that a request gives back is pushed onto the stack of free pages, in the
+ *     order of requests, each request's in the order of its table row;
+ *   - then the requests that need pages take them off the top, in the order of requests, each
+ *     in the order of its table row, as long as the stack holds all that this and the earlier
+ *     requests need.  From the first request that is short on, no request takes pages, and the
+ *     ones that need some keep what they have.
+ * A request whose rows need more than max_pages pages keeps what it has and is short.
+ *   block_table  [batch][max_pages] int32 page ids; entries held .. want - 1 of the requests
+ *                that take pages are written, no other
+ *   held_pages, ctx_len, n_new  [batch] int32.  A request that has ended: ctx_len = n_new = 0
+ *   free_pages   [num_pages] int32, the stack: entries 0 .. n_free - 1 are free pages; pushed
+ *                ones are written from entry n_free on (none past num_pages)
+ *   n_free       [1] int32, clamped to [0, num_pages]
+ *   num_pages, page_rows  as for tree_verify_attn_paged; max_pages * page_rows at most 2^30
+ *   held_out     [batch] pages held afterwards; must not be the held_pages array
+ *   n_free_out   [1] free pages afterwards; must not be the n_free array
+ *   n_short      [1] number of requests that did not get what they need
+ *   slot_map     [batch][max_new] int64, or NULL: the pool row of logical row ctx + i, page id
+ *                * page_rows + (ctx + i) % page_rows, for i < new; -1 from new on, and for
+ *                every row of a request that is short
+ * batch at most 4096.  The call is one kernel and needs no workspace; a page id must not be in
+ * two places (the tables' held entries and the stack). */
+taps_status kv_reserve_paged(int32_t *block_table, int32_t max_pages, const int32_t *held_pages,
+                             const int32_t *ctx_len, const int32_t *n_new, int32_t batch,
+                             int32_t max_new, int32_t *free_pages, const int32_t *n_free,
+                             int32_t num_pages, int32_t page_rows, int32_t *held_out,
+                             int32_t *n_free_out, int32_t *n_short, int64_t *slot_map,
+                             hipStream_t stream);
+
+/* New K and V rows into a paged cache: row t of K_new and V_new goes to row slot_map[t] of the
+ * pools (page slot / page_rows, row slot % page_rows of it); slots outside [0, num_pages *
+ * page_rows), such as the -1 of kv_reserve_paged, are left out.  No other row is written.
+ *   K_new, V_new  [rows][Hkv][head_dim], consecutive rows k_stride and v_stride elements apart
+ *                 (at least Hkv * head_dim, a multiple of 16 bytes): slices of a fused
+ *                 projection's rows need no copy.  Not in the pools' memory
+ *   slot_map      [rows] int64; a slot must not be named twice (its row would be a mix)
+ *   K_pages, V_pages, num_pages, page_rows  as for tree_verify_attn_paged
+ *   head_dim 64 or 128; dtype TAPS_BF16 or TAPS_FP32 for all four; 16-byte aligned bases */
+taps_status kv_append_paged(const void *K_new, const void *V_new, int64_t k_stride,
+                            int64_t v_stride, const int64_t *slot_map, int32_t rows, int32_t Hkv,
+                            int32_t head_dim, int32_t dtype, void *K_pages, void *V_pages,
+                            int32_t num_pages, int32_t page_rows, hipStream_t stream);
+
+/* Host-only check of the sizes of decode_attn_paged, no device access. */
+taps_status decode_attn_paged_validate(int32_t batch, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                                       int32_t max_len, int32_t page_rows, int32_t dtype,
+                                       float scale);
+
+/* Bytes of scratch decode_attn_paged needs (the splits' parts; 0 for short caches and for
+ * sizes that it rejects).  Calls that may overlap on the GPU need scratch of their own. */
+size_t decode_attn_paged_workspace_bytes(int32_t batch, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                                         int32_t max_len, int32_t page_rows, int32_t dtype);
+
+/* Attention of one new token per request over a paged KV cache: the decoding step of requests
+ * that have no draft.  O[b,h] = softmax_j(scale * Q[b,h] . K[j,g]) V[j,g] over the logical rows
+ * j < kv_len[b] (the new token's own row, appended before the call, among them), g = h / (Hq /
+ * Hkv); zeros where kv_len[b] is 0.
+ *   Q            [batch][Hq][head_dim], consecutive requests q_stride elements apart (at least
+ *                Hq * head_dim, a multiple of 16 bytes)
+ *   K_pages, V_pages, num_pages, page_rows, block_table, max_pages  as for
+ *                tree_verify_attn_paged, in dtype; max_pages * page_rows at least max_len
+ *   kv_len       [batch] int32, clamped to [0, max_len].  Rows past it may hold anything; rows
+ *                below it that are not finite leave outputs that are not
+ *   head_dim     64 or 128; Hq a multiple of Hkv; batch * Hkv at most 65535
+ *   max_len      [host] upper bound of kv_len, sizes the grid
+ *   dtype        TAPS_BF16 (fp32 accumulation, output rounded to nearest even) or TAPS_FP32
+ *   scale        softmax scale, finite and > 0
+ *   O            [batch][Hq][head_dim] in dtype, 16-byte aligned
+ *   ws           decode_attn_paged_workspace_bytes(...) bytes, 16-byte aligned */
+taps_status decode_attn_paged(const void *Q, int64_t q_stride, const void *K_pages,
+                              const void *V_pages, int32_t num_pages, int32_t page_rows,
+                              const int32_t *block_table, int32_t max_pages,
+                              const int32_t *kv_len, int32_t batch, int32_t Hq, int32_t Hkv,
+                              int32_t head_dim, int32_t max_len, int32_t dtype, float scale,
+                              void *O, void *ws, size_t ws_bytes, hipStream_t stream);
+
+#define TAPS_MAX_SAMPLE_VOCAB (1 << 20)
+
+/* [host] Settings of taps_sample: DEVICE arrays of one value per request; a NULL array turns
+ * its setting off.
+ *   temperature  T > 0; 0, negative or NaN: the largest logit (greedy).  NULL: 1
+ *   top_k        keep the top_k first tokens of the rank order; <= 0 or >= vocab: all
+ *   top_p        of those, keep the shortest prefix whose probability reaches top_p; >= 1 or
+ *                NaN: all; <= 0: the first
+ *   min_p        of those, keep the tokens whose probability is at least min_p times the
+ *                largest one's; <= 0 or NaN: all; >= 1: those equal to the largest */
+typedef struct {
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+} taps_sampling;
+
+/* Host-only check of the sizes of taps_sample, no device access. */
+taps_status taps_sample_validate(int32_t batch, int32_t budget, int32_t vocab, int64_t row_stride,
+                                 int32_t dtype);
+
+/* Bytes of scratch taps_sample needs.  Calls that may overlap on the GPU need scratch of their
+ * own. */
+size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab, int32_t dtype);
+
+/* One token per logits row, from a given random number: the target's token after each node of
+ * a draft tree (accept_walk on them accepts a drafted token with the target's own probability
+ * of it, so the emitted tokens are samples of the target), or, with budget 1, each request's
+ * next token.
+ *   logits     [batch][budget][vocab] bf16 or fp32, consecutive rows row_stride elements apart
+ *              (at least vocab), 16-byte aligned base
+ *   n_nodes    [batch] int32 rows to sample per request, or NULL (all): rows i >= n_nodes[b]
+ *              get token -1 and probability 0, their logits are not read
+ *   s          the settings
+ *   u          [batch][budget] float random numbers in [0, 1) (NaN counts 0; others are clamped)
+ *   tokens     [batch][budget] int32
+ *   probs      [batch][budget] float, or NULL: the token's probability among the kept ones
+ * A row's rank order is value descending, then index ascending; -0 equals +0; NaN is last.
+ * Token r of it has the integer weight W_r = 2^43 * exp((x_r - x_0) / T), rounded to nearest
+ * (evaluated in fp64 to within 2^-50 of exp), 2^43 where x_r equals x_0 (infinite values too)
+ * and 0 for NaN.  All sums are exact: S_k the sum of the weights after top_k; top_p keeps up to
+ * the first token whose running sum reaches ceil(top_p * S_k); S is the sum of all that are
+ * kept.  The token is the first whose running sum exceeds floor(u * S), its probability W / S.
+ * (Weights that round to 0, below 2^-44 of the largest, are never drawn.)  A row of NaN alone
+ * gives token 0 with probability 0.  budget at most TAPS_MAX_BUDGET, vocab at most
+ * TAPS_MAX_SAMPLE_VOCAB, batch * budget at most 2^20. */
+taps_status taps_sample(const void *logits, int64_t row_stride, int32_t batch, int32_t budget,
+                        int32_t vocab, int32_t dtype, const int32_t *n_nodes,
+                        const taps_sampling *s, const float *u, int32_t *tokens, float *probs,
+                        void *ws, size_t ws_bytes, hipStream_t stream);
 
 /* Human-readable name of a status code (static string). */
 const char *taps_status_string(int32_t status);

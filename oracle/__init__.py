@@ -15,6 +15,9 @@ Layout
   scorer.py     the learned-scorer hook: MLP on edge features, sibling softmax (Sec. 4.2)
   layer.py      one Qwen3-style attention layer over the tree: projections, per-head
                 RMSNorm, rotary positions by tree depth, tree attention, output projection
+  pages.py      pages from a free-page stack, slot maps, rows by slot
+  decode.py     attention of one new token per request over a paged cache
+  sample.py     token sampling with temperature, top-k, top-p and min-p
 
 Pins (what fixes each part without trusting this code) live in
 tests/test_oracle_*.py.  Parity of the oracle against the paper's own numbers
@@ -28,3 +31,6 @@ from .select import (  # noqa: F401
 from .attention import ancestor_sets, tree_attention, tree_attention_paged  # noqa: F401
 from .walk import accept_walk  # noqa: F401
 from .commit import committed_path, kv_commit, kv_commit_paged  # noqa: F401
+from .decode import decode_attention_paged  # noqa: F401
+from .pages import kv_append_paged, kv_reserve_paged  # noqa: F401
+from .sample import sample, sample_row  # noqa: F401

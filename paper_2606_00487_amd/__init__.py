@@ -14,6 +14,16 @@ memory and the current stream.
     new_ctx, tokens, n = com(K, V, kv_offset, ctx_len, tree, path, path_len, bonus)  # kv_commit
     lay = VerifyLayer(batch, budget, Hq, Hkv, head_dim, hidden, max_ctx)
     Y = lay(X, LayerWeights(Wq, Wk, Wv, Wo, q_norm, k_norm), K, V, kv_offset, ctx_len, tree)
+
+Around the round, over a paged cache:
+
+    res = PagedKVReserve(batch, max_pages, num_pages, page_rows, max_new)
+    held, n_free, short, slots = res(block_table, held, ctx_len, n_new, free_pages, n_free)
+    PagedKVAppend(Hkv, head_dim, page_rows)(K_new, V_new, slots, K_pages, V_pages)
+    dec = PagedDecodeAttention(batch, Hq, Hkv, head_dim, max_len, page_rows)
+    O = dec(Q, K_pages, V_pages, block_table, kv_len)                 # decode_attn_paged
+    smp = TokenSampler(batch, budget, vocab)
+    target_tokens, probs = smp(logits, u, tree.n_nodes, temperature=T, top_p=p)   # taps_sample
 """
 from __future__ import annotations
 
@@ -439,3 +449,175 @@ class PagedVerifyLayer:
             ctypes.byref(st), batch, budget, Hq, Hkv, hd, max_ctx, self.scale, _ptr(self.Y),
             _ptr(self.ws), self.ws.numel(), _stream()))
         return self.Y
+
+
+def _here(name: str, *tensors):
+    """The calls below run on the current device: their tensors have to live there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"{name}: tensors on {t.device}, the current device is cuda:{dev}")
+
+
+def _need_rows(t: torch.Tensor, name: str, dtype, inner):
+    """[rows, *inner] whose rows may be apart; returns the distance of rows in elements."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise TypeError(f"{name}: expected a GPU tensor")
+    if t.shape[1:] != inner:
+        raise ValueError(f"{name}: expected [rows, {', '.join(map(str, inner))}], "
+                         f"got {tuple(t.shape)}")
+    n = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size > 1 and stride != n:
+            raise ValueError(f"{name}: each row must be contiguous")
+        n *= size
+    return t.stride(0) if t.shape[0] > 1 else n
+
+
+def _need_pools(K_pages, V_pages, dtype, page_rows, Hkv, hd):
+    _need(K_pages, "K_pages", dtype)
+    if K_pages.dim() != 4 or K_pages.shape[1:] != (page_rows, Hkv, hd):
+        raise ValueError(f"K_pages: expected [pages, {page_rows}, {Hkv}, {hd}], "
+                         f"got {tuple(K_pages.shape)}")
+    _need(V_pages, "V_pages", dtype, K_pages.shape)
+
+
+class PagedKVReserve:
+    """kv_reserve_paged: pages for the requests' next rows, from the free-page stack into
+    their block tables, and the slot map of the new rows."""
+
+    def __init__(self, batch, max_pages, num_pages, page_rows, max_new, slot_map=True):
+        """max_new: upper bound of n_new and, with slot_map, the slot map's columns."""
+        self.lib = load()
+        self.shape = (batch, max_pages, num_pages, int(page_rows), max_new)
+        self.slot_map = slot_map
+
+    def __call__(self, block_table, held_pages, ctx_len, n_new, free_pages, n_free):
+        """block_table [batch, max_pages] and free_pages [num_pages] are updated in place.
+        Returns new tensors: pages held [batch], free pages [1], requests that are short [1]
+        (all int32) and the slot map [batch, max_new] int64 (None without slot_map)."""
+        batch, max_pages, num_pages, page_rows, max_new = self.shape
+        _need(block_table, "block_table", torch.int32, (batch, max_pages))
+        _need(held_pages, "held_pages", torch.int32, (batch,))
+        _need(ctx_len, "ctx_len", torch.int32, (batch,))
+        _need(n_new, "n_new", torch.int32, (batch,))
+        _need(free_pages, "free_pages", torch.int32, (num_pages,))
+        _need(n_free, "n_free", torch.int32, (1,))
+        _here("kv_reserve_paged", block_table, held_pages, ctx_len, n_new, free_pages, n_free)
+        held, free, short = (torch.empty_like(held_pages), torch.empty_like(n_free),
+                             torch.empty_like(n_free))
+        slots = torch.empty(batch, max_new, dtype=torch.int64,
+                            device=block_table.device) if self.slot_map else None
+        _lib.check(self.lib, "kv_reserve_paged", self.lib.kv_reserve_paged(
+            _ptr(block_table), max_pages, _ptr(held_pages), _ptr(ctx_len), _ptr(n_new), batch,
+            max_new, _ptr(free_pages), _ptr(n_free), num_pages, page_rows, _ptr(held), _ptr(free),
+            _ptr(short), _ptr(slots), _stream()))
+        return held, free, short, slots
+
+
+class PagedKVAppend:
+    """kv_append_paged: new K/V rows into the page pools through a slot map."""
+
+    def __init__(self, Hkv, head_dim, page_rows, dtype=BF16):
+        self.lib = load()
+        self.shape = (Hkv, head_dim, int(page_rows), dtype)
+
+    def __call__(self, K_new, V_new, slot_map, K_pages, V_pages):
+        """K_new, V_new: [rows, Hkv, head_dim], rows contiguous in themselves (slices of a fused
+        projection's rows are fine).  slot_map: int64 of `rows` entries in any shape."""
+        Hkv, hd, page_rows, dtype = self.shape
+        tdt = _TORCH_DT[dtype]
+        ks = _need_rows(K_new, "K_new", tdt, (Hkv, hd))
+        vs = _need_rows(V_new, "V_new", tdt, (Hkv, hd))
+        rows = K_new.shape[0]
+        _need(slot_map, "slot_map", torch.int64)
+        if V_new.shape[0] != rows or slot_map.numel() != rows:
+            raise ValueError(f"K_new has {rows} rows, V_new {V_new.shape[0]}, slot_map "
+                             f"{slot_map.numel()} entries")
+        _need_pools(K_pages, V_pages, tdt, page_rows, Hkv, hd)
+        _here("kv_append_paged", K_new, V_new, slot_map, K_pages, V_pages)
+        _lib.check(self.lib, "kv_append_paged", self.lib.kv_append_paged(
+            _ptr(K_new), _ptr(V_new), ks, vs, _ptr(slot_map), rows, Hkv, hd, dtype,
+            _ptr(K_pages), _ptr(V_pages), K_pages.shape[0], page_rows, _stream()))
+        return K_pages, V_pages
+
+
+class PagedDecodeAttention:
+    """decode_attn_paged: attention of one new token per request over a paged KV cache."""
+
+    def __init__(self, batch, Hq, Hkv, head_dim, max_len, page_rows, dtype=BF16, scale=None):
+        self.lib = load()
+        self.scale = float(scale if scale is not None else head_dim ** -0.5)
+        self.shape = (batch, Hq, Hkv, head_dim, max_len, int(page_rows), dtype)
+        _lib.check(self.lib, "decode_attn_paged_validate",
+                   self.lib.decode_attn_paged_validate(*self.shape, self.scale))
+        self.ws_bytes = self.lib.decode_attn_paged_workspace_bytes(*self.shape)
+
+    def __call__(self, Q, K_pages, V_pages, block_table, kv_len, out=None):
+        """Q: [batch, Hq, head_dim], requests may be apart.  Each call has scratch of its own
+        (from torch's allocator, on the current stream), so calls may overlap."""
+        batch, Hq, Hkv, hd, max_len, page_rows, dtype = self.shape
+        tdt = _TORCH_DT[dtype]
+        qs = _need_rows(Q, "Q", tdt, (Hq, hd))
+        if Q.shape[0] != batch:
+            raise ValueError(f"Q: expected {batch} requests, got {Q.shape[0]}")
+        _need_pools(K_pages, V_pages, tdt, page_rows, Hkv, hd)
+        _need(block_table, "block_table", torch.int32)
+        if block_table.dim() != 2 or block_table.shape[0] != batch:
+            raise ValueError(f"block_table: expected [{batch}, max_pages], "
+                             f"got {tuple(block_table.shape)}")
+        _need(kv_len, "kv_len", torch.int32, (batch,))
+        O = out if out is not None else torch.empty(batch, Hq, hd, dtype=tdt, device=Q.device)
+        _need(O, "O", tdt, (batch, Hq, hd))
+        _here("decode_attn_paged", Q, K_pages, V_pages, block_table, kv_len, O)
+        ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=Q.device) if self.ws_bytes else None
+        _lib.check(self.lib, "decode_attn_paged", self.lib.decode_attn_paged(
+            _ptr(Q), qs, _ptr(K_pages), _ptr(V_pages), K_pages.shape[0], page_rows,
+            _ptr(block_table), block_table.shape[1], _ptr(kv_len), batch, Hq, Hkv, hd, max_len,
+            dtype, self.scale, _ptr(O), _ptr(ws), self.ws_bytes, _stream()))
+        return O
+
+
+class TokenSampler:
+    """taps_sample: tokens from logits with temperature, top-k, top-p and min-p and given
+    random numbers."""
+
+    def __init__(self, batch, budget, vocab, dtype=BF16):
+        """budget: rows per request (the nodes of its tree; 1 without a draft)."""
+        self.lib = load()
+        self.shape = (batch, budget, vocab, dtype)
+        _lib.check(self.lib, "taps_sample_validate",
+                   self.lib.taps_sample_validate(batch, budget, vocab, vocab, dtype))
+        self.ws_bytes = self.lib.taps_sample_workspace_bytes(*self.shape)
+
+    def __call__(self, logits, u, n_nodes=None, temperature=None, top_k=None, top_p=None,
+                 min_p=None):
+        """logits: [batch, budget, vocab], rows may be apart (a padded vocabulary's slice); u:
+        [batch, budget] float32; n_nodes: [batch] int32 or None; the settings: [batch] tensors
+        (top_k int32, the others float32) or None.  Returns the tokens [batch, budget] int32 and
+        their probabilities, float32.  Each call has scratch of its own."""
+        batch, budget, vocab, dtype = self.shape
+        if logits.shape != (batch, budget, vocab):
+            raise ValueError(f"logits: expected [{batch}, {budget}, {vocab}], "
+                             f"got {tuple(logits.shape)}")
+        if batch > 1 and budget > 1 and logits.stride(0) != budget * logits.stride(1):
+            raise ValueError("logits: all rows must be the same distance apart")
+        rows = logits[0] if batch == 1 else logits[:, 0] if budget == 1 else logits.flatten(0, 1)
+        stride = _need_rows(rows, "logits", _TORCH_DT[dtype], (vocab,))
+        _need(u, "u", torch.float32, (batch, budget))
+        for t, name, dt in ((n_nodes, "n_nodes", torch.int32), (top_k, "top_k", torch.int32),
+                            (temperature, "temperature", torch.float32),
+                            (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+            if t is not None:
+                _need(t, name, dt, (batch,))
+        _here("taps_sample", logits, u, n_nodes, temperature, top_k, top_p, min_p)
+        tokens = torch.empty(batch, budget, dtype=torch.int32, device=u.device)
+        probs = torch.empty(batch, budget, dtype=torch.float32, device=u.device)
+        ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=u.device) if self.ws_bytes else None
+        st = _lib.Sampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
+        _lib.check(self.lib, "taps_sample", self.lib.taps_sample(
+            _ptr(logits), stride, batch, budget, vocab, dtype, _ptr(n_nodes), ctypes.byref(st),
+            _ptr(u), _ptr(tokens), _ptr(probs), _ptr(ws), self.ws_bytes, _stream()))
+        return tokens, probs

@@ -34,7 +34,9 @@ EXPORTED = [
     "taps_spec_exp_host", "verify_layer_workspace_bytes", "verify_layer", "taps_select_noalloc",
     "tree_verify_attn_paged_workspace_bytes", "tree_verify_attn_paged",
     "tree_verify_attn_paged_timed", "kv_commit_paged", "verify_layer_paged_workspace_bytes",
-    "verify_layer_paged",
+    "verify_layer_paged", "kv_reserve_paged", "kv_append_paged", "decode_attn_paged_validate",
+    "decode_attn_paged_workspace_bytes", "decode_attn_paged", "taps_sample_validate",
+    "taps_sample_workspace_bytes", "taps_sample",
 ]
 SELECT_SCRATCH_BYTES = 8 << 20   # TAPS_SELECT_SCRATCH_BYTES
 
@@ -65,6 +67,11 @@ class Tree(ctypes.Structure):
                 ("depth", ctypes.c_void_p), ("rank", ctypes.c_void_p),
                 ("q_reach", ctypes.c_void_p), ("n_nodes", ctypes.c_void_p),
                 ("topk_idx", ctypes.c_void_p), ("topk_val", ctypes.c_void_p)]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
 
 
 class TapsError(RuntimeError):
@@ -134,6 +141,25 @@ def load(path: str = LIB_PATH):
                                        P(Tree), i32, i32, i32, i32, i32, i32, f32, vp, vp, sz,
                                        vp]
     lib.verify_layer_paged.restype = i32
+    lib.kv_reserve_paged.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, vp,
+                                     vp, vp]
+    lib.kv_reserve_paged.restype = i32
+    lib.kv_append_paged.argtypes = [vp, vp, i64, i64, vp, i32, i32, i32, i32, vp, vp, i32, i32, vp]
+    lib.kv_append_paged.restype = i32
+    lib.decode_attn_paged_validate.argtypes = [i32] * 7 + [f32]
+    lib.decode_attn_paged_validate.restype = i32
+    lib.decode_attn_paged_workspace_bytes.argtypes = [i32] * 7
+    lib.decode_attn_paged_workspace_bytes.restype = sz
+    lib.decode_attn_paged.argtypes = [vp, i64, vp, vp, i32, i32, vp, i32, vp, i32, i32, i32, i32,
+                                      i32, i32, f32, vp, vp, sz, vp]
+    lib.decode_attn_paged.restype = i32
+    lib.taps_sample_validate.argtypes = [i32, i32, i32, i64, i32]
+    lib.taps_sample_validate.restype = i32
+    lib.taps_sample_workspace_bytes.argtypes = [i32] * 4
+    lib.taps_sample_workspace_bytes.restype = sz
+    lib.taps_sample.argtypes = [vp, i64, i32, i32, i32, i32, vp, P(Sampling), vp, vp, vp, vp, sz,
+                                vp]
+    lib.taps_sample.restype = i32
     lib.taps_status_string.argtypes = [i32]
     lib.taps_status_string.restype = ctypes.c_char_p
     lib.taps_spec_exp_host.argtypes = [f64]

@@ -30,9 +30,10 @@ PER_FILE = {
     # the AGPR form would copy its accumulators back and forth around every softmax
     "attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "attn_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 SOURCES = ["topk.hip", "select.hip", "attn.hip", "attn_f32.hip", "walk.hip", "commit.hip", "layer.hip",
-           "noalloc.hip", "api.cpp"]
+           "pages.hip", "decode.hip", "sample.hip", "noalloc.hip", "api.cpp"]
 
 
 def hipcc() -> str:

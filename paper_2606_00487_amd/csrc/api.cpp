@@ -497,4 +497,153 @@ taps_status verify_layer_paged(const void* X, const taps_layer_weights* w, void*
                    head_dim, max_ctx, scale, Y, ws, ws_bytes, stream, &pk, page_rows);
 }
 
+taps_status kv_reserve_paged(int32_t* block_table, int32_t max_pages, const int32_t* held_pages,
+                             const int32_t* ctx_len, const int32_t* n_new, int32_t batch,
+                             int32_t max_new, int32_t* free_pages, const int32_t* n_free,
+                             int32_t num_pages, int32_t page_rows, int32_t* held_out,
+                             int32_t* n_free_out, int32_t* n_short, int64_t* slot_map,
+                             hipStream_t stream) {
+  const int shift = page_shift_of(page_rows);
+  if (batch < 0 || max_pages < 1 || max_new < 0 || num_pages < 1 || shift < 0)
+    return TAPS_ERR_INVALID_ARG;
+  if (batch > kMaxReserveBatch) return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)max_pages * page_rows > (int64_t)1 << 30) return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)num_pages * page_rows > (int64_t)UINT32_MAX) return TAPS_ERR_UNSUPPORTED;
+  if (max_new > (1 << 27)) return TAPS_ERR_UNSUPPORTED;   // 65535 slices of 4096 slots hold it
+  if (batch == 0) return TAPS_OK;
+  if (!block_table || !held_pages || !ctx_len || !n_new || !free_pages || !n_free || !held_out ||
+      !n_free_out || !n_short)
+    return TAPS_ERR_INVALID_ARG;
+  // every workgroup reads the whole batch's counts while others write the new ones
+  if (held_out == held_pages || n_free_out == n_free) return TAPS_ERR_INVALID_ARG;
+  const uintptr_t a4 = (uintptr_t)block_table | (uintptr_t)held_pages | (uintptr_t)ctx_len |
+                       (uintptr_t)n_new | (uintptr_t)free_pages | (uintptr_t)n_free |
+                       (uintptr_t)held_out | (uintptr_t)n_free_out | (uintptr_t)n_short;
+  if ((a4 & 3) != 0 || ((uintptr_t)slot_map & 7) != 0) return TAPS_ERR_INVALID_ARG;
+  return launch_reserve(block_table, max_pages, held_pages, ctx_len, n_new, batch, free_pages,
+                        n_free, num_pages, shift, max_new, slot_map, held_out, n_free_out, n_short,
+                        stream) == hipSuccess
+             ? TAPS_OK
+             : TAPS_ERR_HIP;
+}
+
+taps_status kv_append_paged(const void* K_new, const void* V_new, int64_t k_stride,
+                            int64_t v_stride, const int64_t* slot_map, int32_t rows, int32_t Hkv,
+                            int32_t head_dim, int32_t dtype, void* K_pages, void* V_pages,
+                            int32_t num_pages, int32_t page_rows, hipStream_t stream) {
+  if (rows < 0 || Hkv < 1 || num_pages < 1 || page_shift_of(page_rows) < 0)
+    return TAPS_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return TAPS_ERR_UNSUPPORTED;
+  if (dtype != TAPS_BF16 && dtype != TAPS_FP32) return TAPS_ERR_INVALID_ARG;
+  if ((int64_t)Hkv * head_dim * 4 > ((int64_t)1 << 24)) return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)num_pages * page_rows > (int64_t)UINT32_MAX) return TAPS_ERR_UNSUPPORTED;
+  const int es = dtype == TAPS_BF16 ? 2 : 4, row = Hkv * head_dim;
+  if (k_stride < row || v_stride < row) return TAPS_ERR_INVALID_ARG;
+  if (k_stride > (int64_t)1 << 31 || v_stride > (int64_t)1 << 31) return TAPS_ERR_UNSUPPORTED;
+  if (((k_stride | v_stride) * es & 15) != 0) return TAPS_ERR_INVALID_ARG;
+  if (rows == 0) return TAPS_OK;
+  if (!K_new || !V_new || !slot_map || !K_pages || !V_pages) return TAPS_ERR_INVALID_ARG;
+  const uintptr_t a16 =
+      (uintptr_t)K_new | (uintptr_t)V_new | (uintptr_t)K_pages | (uintptr_t)V_pages;
+  if ((a16 & 15) != 0 || ((uintptr_t)slot_map & 7) != 0) return TAPS_ERR_INVALID_ARG;
+  return launch_append(K_new, V_new, k_stride * es, v_stride * es, slot_map, rows, row * es,
+                       K_pages, V_pages, (int64_t)num_pages * page_rows, stream) == hipSuccess
+             ? TAPS_OK
+             : TAPS_ERR_HIP;
+}
+
+taps_status decode_attn_paged_validate(int32_t batch, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                                       int32_t max_len, int32_t page_rows, int32_t dtype,
+                                       float scale) {
+  if (batch < 0 || Hq < 1 || Hkv < 1 || max_len < 0) return TAPS_ERR_INVALID_ARG;
+  if (Hq % Hkv != 0) return TAPS_ERR_INVALID_ARG;
+  if (dtype != TAPS_BF16 && dtype != TAPS_FP32) return TAPS_ERR_INVALID_ARG;
+  if (page_shift_of(page_rows) < 0) return TAPS_ERR_INVALID_ARG;
+  if (!std::isfinite(scale) || !(scale > 0.f)) return TAPS_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return TAPS_ERR_UNSUPPORTED;
+  if (max_len > 1 << 30) return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)batch * Hkv > 65535 || Hq > 65535) return TAPS_ERR_UNSUPPORTED;
+  // a tile's 32 rows are addressed with 32-bit offsets
+  if ((int64_t)Hkv * head_dim * 4 > ((int64_t)1 << 24)) return TAPS_ERR_UNSUPPORTED;
+  const DecodePlan p = plan_decode(batch, Hq, Hkv, max_len);
+  if ((int64_t)batch * Hkv * p.splits * p.htiles > (int64_t)1 << 30) return TAPS_ERR_UNSUPPORTED;
+  return TAPS_OK;
+}
+
+size_t decode_attn_paged_workspace_bytes(int32_t batch, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                                         int32_t max_len, int32_t page_rows, int32_t dtype) {
+  if (decode_attn_paged_validate(batch, Hq, Hkv, head_dim, max_len, page_rows, dtype, 1.0f) !=
+          TAPS_OK ||
+      batch == 0)
+    return 0;
+  return decode_ws_bytes(plan_decode(batch, Hq, Hkv, max_len), batch, Hq, head_dim);
+}
+
+taps_status decode_attn_paged(const void* Q, int64_t q_stride, const void* K_pages,
+                              const void* V_pages, int32_t num_pages, int32_t page_rows,
+                              const int32_t* block_table, int32_t max_pages,
+                              const int32_t* kv_len, int32_t batch, int32_t Hq, int32_t Hkv,
+                              int32_t head_dim, int32_t max_len, int32_t dtype, float scale,
+                              void* O, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const taps_status st = decode_attn_paged_validate(batch, Hq, Hkv, head_dim, max_len, page_rows,
+                                                    dtype, scale);
+  if (st != TAPS_OK) return st;
+  if (num_pages < 1 || max_pages < 1) return TAPS_ERR_INVALID_ARG;
+  if ((int64_t)num_pages * page_rows > (int64_t)UINT32_MAX) return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)max_pages * page_rows < max_len) return TAPS_ERR_INVALID_ARG;
+  const int es = dtype == TAPS_BF16 ? 2 : 4;
+  if (q_stride < (int64_t)Hq * head_dim || (q_stride * es & 15) != 0) return TAPS_ERR_INVALID_ARG;
+  if (q_stride > (int64_t)1 << 31) return TAPS_ERR_UNSUPPORTED;
+  if (batch == 0) return TAPS_OK;
+  if (!Q || !K_pages || !V_pages || !block_table || !kv_len || !O) return TAPS_ERR_INVALID_ARG;
+  const uintptr_t a16 =
+      (uintptr_t)Q | (uintptr_t)K_pages | (uintptr_t)V_pages | (uintptr_t)O;
+  if ((a16 & 15) != 0 || (((uintptr_t)block_table | (uintptr_t)kv_len) & 3) != 0)
+    return TAPS_ERR_INVALID_ARG;
+  const DecodePlan p = plan_decode(batch, Hq, Hkv, max_len);
+  const size_t need = decode_ws_bytes(p, batch, Hq, head_dim);
+  if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return TAPS_ERR_WORKSPACE;
+  const PagedKV pk{block_table, max_pages, num_pages, page_shift_of(page_rows)};
+  return launch_decode(Q, q_stride, K_pages, V_pages, pk, kv_len, batch, Hq, Hkv, head_dim,
+                       max_len, dtype, scale, p, O, ws, stream) == hipSuccess
+             ? TAPS_OK
+             : TAPS_ERR_HIP;
+}
+
+taps_status taps_sample_validate(int32_t batch, int32_t budget, int32_t vocab, int64_t row_stride,
+                                 int32_t dtype) {
+  if (batch < 0 || budget < 1 || vocab < 1 || row_stride < vocab) return TAPS_ERR_INVALID_ARG;
+  if (dtype != TAPS_BF16 && dtype != TAPS_FP32) return TAPS_ERR_INVALID_ARG;
+  if (budget > TAPS_MAX_BUDGET || vocab > TAPS_MAX_SAMPLE_VOCAB) return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)batch * budget > (int64_t)1 << 20 || row_stride > (int64_t)1 << 31)
+    return TAPS_ERR_UNSUPPORTED;
+  return TAPS_OK;
+}
+
+size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab, int32_t dtype) {
+  if (taps_sample_validate(batch, budget, vocab, vocab, dtype) != TAPS_OK || batch == 0) return 0;
+  return 0;
+}
+
+taps_status taps_sample(const void* logits, int64_t row_stride, int32_t batch, int32_t budget,
+                        int32_t vocab, int32_t dtype, const int32_t* n_nodes,
+                        const taps_sampling* s, const float* u, int32_t* tokens, float* probs,
+                        void* ws, size_t ws_bytes, hipStream_t stream) {
+  const taps_status st = taps_sample_validate(batch, budget, vocab, row_stride, dtype);
+  if (st != TAPS_OK) return st;
+  if (batch == 0) return TAPS_OK;
+  if (!logits || !s || !u || !tokens) return TAPS_ERR_INVALID_ARG;
+  if (((uintptr_t)logits & 15) != 0) return TAPS_ERR_INVALID_ARG;
+  const uintptr_t a4 = (uintptr_t)n_nodes | (uintptr_t)s->temperature | (uintptr_t)s->top_k |
+                       (uintptr_t)s->top_p | (uintptr_t)s->min_p | (uintptr_t)u |
+                       (uintptr_t)tokens | (uintptr_t)probs;
+  if ((a4 & 3) != 0) return TAPS_ERR_INVALID_ARG;
+  const size_t need = taps_sample_workspace_bytes(batch, budget, vocab, dtype);
+  if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return TAPS_ERR_WORKSPACE;
+  return launch_sample(logits, row_stride * (dtype == TAPS_BF16 ? 2 : 4), batch, budget, vocab,
+                       dtype, n_nodes, *s, u, tokens, probs, stream) == hipSuccess
+             ? TAPS_OK
+             : TAPS_ERR_HIP;
+}
+
 }  // extern "C"

@@ -149,6 +149,35 @@ hipError_t launch_qkv(const void* X, int K, const taps_layer_weights& w, const G
 hipError_t launch_oproj(const void* O, int M, int K, const void* Wo, int N, const GemmPlan& p,
                         void* scratch, void* Y, hipStream_t s);
 
+// Pages for a batch's requests and their slot maps (slots null: none); new rows by slot
+constexpr int kMaxReserveBatch = 4096;
+hipError_t launch_reserve(int32_t* table, int max_pages, const int32_t* held, const int32_t* ctx,
+                          const int32_t* n_new, int batch, int32_t* stack, const int32_t* n_free,
+                          int num_pages, int page_shift, int max_new, int64_t* slots,
+                          int32_t* held_out, int32_t* n_free_out, int32_t* n_short,
+                          hipStream_t s);
+hipError_t launch_append(const void* K_new, const void* V_new, int64_t k_stride_bytes,
+                         int64_t v_stride_bytes, const int64_t* slots, int rows, int row_bytes,
+                         void* K_pages, void* V_pages, int64_t pool_rows, hipStream_t s);
+
+// One new token per request over a paged cache: requests are cut into splits of split_len keys
+struct DecodePlan {
+  int split_len;   // a multiple of 128 (four waves' tiles)
+  int splits;      // splits that max_len keys need
+  int htiles;      // groups of 16 query heads of one KV head
+};
+DecodePlan plan_decode(int batch, int Hq, int Hkv, int max_len);
+size_t decode_ws_bytes(const DecodePlan& p, int batch, int Hq, int head_dim);
+// q_stride in elements; pools [num_pages][2^page_shift][Hkv][head_dim]
+hipError_t launch_decode(const void* Q, int64_t q_stride, const void* K, const void* V,
+                         const PagedKV& pk, const int32_t* len, int batch, int Hq, int Hkv,
+                         int head_dim, int max_len, int dtype, float scale, const DecodePlan& p,
+                         void* O, void* ws, hipStream_t s);
+
+hipError_t launch_sample(const void* logits, int64_t row_bytes, int batch, int budget, int vocab,
+                         int dtype, const int32_t* n_nodes, const taps_sampling& s,
+                         const float* u, int32_t* tokens, float* probs, hipStream_t stream);
+
 double spec_exp_host(double t);
 
 }  // namespace taps
