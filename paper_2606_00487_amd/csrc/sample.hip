@@ -16,8 +16,6 @@ namespace taps {
 
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / kWave;
 constexpr double kOne = 8796093022208.0;   // 2^43, the weight of the largest value
 
 // 2^y for -45 < y <= 0: y = k + r, |r| <= 1/2, e^(r ln 2) by its Taylor series to the 12th power
@@ -60,61 +58,129 @@ struct Weights {
   }
 };
 
+// Inclusive prefix sums over the lanes of a wave (DPP row shifts, then row broadcasts).  64 bits
+// in pieces of 22, 22 and 20 bits, whose sums fit 32: a lane crossing costs one instruction each,
+// where a shuffle through LDS would cost its latency six times over.
+__device__ inline uint32_t wave_scan_u32(uint32_t x) {
+  int v = (int)x;
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);  // row_shr:2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);  // row_shr:4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);  // row_shr:8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return (uint32_t)v;
+}
+__device__ inline uint64_t wave_scan_u64(uint64_t v) {
+  const uint32_t a = wave_scan_u32((uint32_t)v & 0x3FFFFFu);
+  const uint32_t b = wave_scan_u32((uint32_t)(v >> 22) & 0x3FFFFFu);
+  const uint32_t c = wave_scan_u32((uint32_t)(v >> 44));
+  return (uint64_t)a + ((uint64_t)b << 22) + ((uint64_t)c << 44);
+}
+__device__ inline uint64_t lane_u64(uint64_t v, int lane) {   // lane uniform
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), lane);
+  return ((uint64_t)hi << 32) | lo;
+}
 __device__ inline uint64_t wave_sum_u64(uint64_t v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
-    const uint32_t lo = __shfl_xor((uint32_t)v, m), hi = __shfl_xor((uint32_t)(v >> 32), m);
-    v += ((uint64_t)hi << 32) | lo;
-  }
-  return v;
+  return lane_u64(wave_scan_u64(v), kWave - 1);
 }
 
 constexpr int kBins = 2048;         // radix digits of the general path
 constexpr int kWindow = 36864;      // bf16 values counted one by one, from the largest down
-constexpr int kWindowRows = kWindow / kWave;
+constexpr int kRun = 256;           // values whose sums are kept together: four per lane
+constexpr int kRuns = kWindow / kRun;
 constexpr int kPerOctave = 32;      // fp32: bins of the weight per factor of two
 constexpr int kWeightBins = 1424;   // 44.5 octaves: smaller weights round to 0
 constexpr int kList = 1024;         // elements that are ranked one by one
-constexpr int kGroups = kThreads / 4;
-constexpr int kFewTopK = 192;       // top_k up to which the groups' maxima bound the window
+constexpr int kGroups = 256;        // thread groups whose maxima bound a small top_k
+constexpr int kFewTopK = 192;       // ... up to this one
 
-// Scratch of the three paths, which a row takes one after the other at most
+// Scratch of the paths, which a row takes one after the other at most
 struct GeneralScratch {
   uint64_t mass[kBins];
   uint32_t count[kBins];
 };
+struct ListScratch {
+  uint64_t list[kList], sorted[kList], cum[kList];
+};
 struct CountScratch {
-  uint32_t count[kWindow];          // elements per value, the largest value first
-  uint64_t mass[kWindowRows];       // sums of 64 values each; then those before them
-  uint32_t num[kWindowRows];
+  uint32_t count[kWindow / 2];      // elements per value, 16 bits each, the largest value first
+  uint64_t mass[kRuns];             // sums of the runs; then those before them
+  uint32_t num[kRuns];
 };
 struct BinScratch {
+  ListScratch l;
   uint64_t mass[kWeightBins];
   uint64_t before[kWeightBins];
-  uint64_t list[kList], sorted[kList], cum[kList];
 };
 template <int DT>
 union PathScratch {
   GeneralScratch g;
+  ListScratch l;
   CountScratch c;
 };
 template <>
 union PathScratch<TAPS_FP32> {
   GeneralScratch g;
+  ListScratch l;
   BinScratch b;
 };
 
-template <int DT>
+template <int DT, int NT>
 struct Shared {
   PathScratch<DT> u;
   uint32_t group[kGroups];
-  uint64_t red[kWaves];
-  uint32_t red32[kWaves];
+  uint64_t red[NT / kWave];
+  uint32_t red32[NT / kWave];
   uint64_t out64[2];
   uint32_t out32[4];
-  uint32_t n;
-  uint32_t ties[kList];
+  uint32_t n, n_hot;
+  uint16_t hot[NT];
 };
+
+template <class S, int NT>
+__device__ inline uint64_t block_sum_u64(uint64_t v, S& sh) {
+  v = wave_sum_u64(v);
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  __syncthreads();
+  if (lane == 0) sh.red[wave] = v;
+  __syncthreads();
+  uint64_t s = 0;
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) s += sh.red[w];
+  return s;
+}
+
+template <class S, int NT>
+__device__ inline uint64_t block_scan_u64(uint64_t v, S& sh, uint64_t* total) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  v = wave_scan_u64(v);
+  __syncthreads();
+  if (lane == kWave - 1) sh.red[wave] = v;
+  __syncthreads();
+  uint64_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) {
+    if (w < wave) before += sh.red[w];
+    all += sh.red[w];
+  }
+  *total = all;
+  return v + before;
+}
+
+template <class S, int NT>
+__device__ inline float block_max_f32(float v, S& sh) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  __syncthreads();
+  if (lane == 0) sh.red32[wave] = __float_as_uint(v);
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) v = fmaxf(v, __uint_as_float(sh.red32[w]));
+  return v;
+}
 
 // One row of logits, read 16 bytes at a time; f(key, index) for the elements of this thread.
 template <int DT>
@@ -151,38 +217,11 @@ struct Row {
       for (int e = max(e0, 0); e < min(e0 + U, vocab); ++e) f(key_at(e), e);
     }
   }
-  template <class F>
+  template <int NT, class F>
   __device__ inline void each(F&& f) const {
-    for (int u = threadIdx.x; u < units; u += kThreads) unit(u, f);
+    for (int u = threadIdx.x; u < units; u += NT) unit(u, f);
   }
 };
-
-template <int DT>
-__device__ inline uint64_t block_sum_u64(uint64_t v, Shared<DT>& sh) {
-  v = wave_sum_u64(v);
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  __syncthreads();
-  if (lane == 0) sh.red[wave] = v;
-  __syncthreads();
-  uint64_t s = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) s += sh.red[w];
-  return s;
-}
-
-template <int DT>
-__device__ inline uint32_t block_max_u32(uint32_t v, Shared<DT>& sh) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = max(v, (uint32_t)__shfl_xor(v, m));
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  __syncthreads();
-  if (lane == 0) sh.red32[wave] = v;
-  __syncthreads();
-  uint32_t s = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) s = max(s, sh.red32[w]);
-  return s;
-}
 
 // Where the running sum of the weights (or, with `by_count`, the count) in rank order first
 // exceeds `target`: the value's key, the sum and the count above it, and its ties.  `target` is
@@ -194,9 +233,9 @@ struct Crossing {
   uint32_t ties;     // elements with this key
 };
 
-template <int DT>
+template <int DT, int NT>
 __device__ Crossing find_crossing(const Row<DT>& row, const Weights& w, uint64_t target,
-                                  bool by_count, Shared<DT>& sh) {
+                                  bool by_count, Shared<DT, NT>& sh) {
   const int tid = threadIdx.x;
   uint32_t prefix = 0;
   uint64_t above = 0;
@@ -206,9 +245,9 @@ __device__ Crossing find_crossing(const Row<DT>& row, const Weights& w, uint64_t
     const int bits = low == 10 ? 10 : (DT == TAPS_BF16 && low == 21 ? 5 : 11);
     const int high = low;
     low -= bits;
-    for (int i = tid; i < kBins; i += kThreads) sh.u.g.mass[i] = 0ull, sh.u.g.count[i] = 0u;
+    for (int i = tid; i < kBins; i += NT) sh.u.g.mass[i] = 0ull, sh.u.g.count[i] = 0u;
     __syncthreads();
-    row.each([&](uint32_t k, int) {
+    row.template each<NT>([&](uint32_t k, int) {
       if (k == 0u || (high < 32 && (k >> high) != prefix)) return;   // NaN has no weight
       const uint32_t bin = (k >> low) & ((1u << bits) - 1u);
       const uint64_t m = by_count ? 1ull : w(k);
@@ -224,12 +263,7 @@ __device__ Crossing find_crossing(const Row<DT>& row, const Weights& w, uint64_t
       for (int c = (1 << bits) - kWave; !found && c > -kWave; c -= kWave) {
         const int bin = c + (kWave - 1 - tid);        // lane 0 holds the highest
         const uint64_t m = bin >= 0 ? sh.u.g.mass[bin] : 0ull;
-        uint64_t incl = m;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-          const uint32_t lo = __shfl_up((uint32_t)incl, d), hi = __shfl_up((uint32_t)(incl >> 32), d);
-          if (tid >= d) incl += ((uint64_t)hi << 32) | lo;
-        }
+        const uint64_t incl = wave_scan_u64(m);
         const uint64_t hit = __ballot(acc + incl > target);
         if (hit) {
           const int l = __ffsll((long long)hit) - 1;
@@ -240,8 +274,7 @@ __device__ Crossing find_crossing(const Row<DT>& row, const Weights& w, uint64_t
           }
           found = true;
         }
-        const uint32_t lo = __shfl((uint32_t)incl, kWave - 1), hi = __shfl((uint32_t)(incl >> 32), kWave - 1);
-        acc += ((uint64_t)hi << 32) | lo;
+        acc += lane_u64(incl, kWave - 1);
       }
     }
     __syncthreads();
@@ -256,25 +289,20 @@ __device__ Crossing find_crossing(const Row<DT>& row, const Weights& w, uint64_t
 }
 
 // index of the nth (from 0) element whose key is `key`, in index order
-template <int DT>
-__device__ __attribute__((noinline)) int nth_index(const Row<DT>& row, uint32_t key, uint32_t nth, Shared<DT>& sh) {
+template <int DT, int NT>
+__device__ __attribute__((noinline)) int nth_index(const Row<DT>& row, uint32_t key, uint32_t nth, Shared<DT, NT>& sh) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   uint32_t seen = 0;
-  for (int u0 = 0; u0 < row.units; u0 += kThreads) {
+  for (int u0 = 0; u0 < row.units; u0 += NT) {
     uint32_t n = 0;
     if (u0 + tid < row.units) row.unit(u0 + tid, [&](uint32_t k, int) { n += k == key ? 1u : 0u; });
-    uint32_t incl = n;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const uint32_t o = __shfl_up(incl, d);
-      if (lane >= d) incl += o;
-    }
+    const uint32_t incl = wave_scan_u32(n);
     __syncthreads();
     if (lane == kWave - 1) sh.red32[wave] = incl;
     __syncthreads();
     uint32_t before = seen, all = 0;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
+    for (int v = 0; v < (NT / kWave); ++v) {
       if (v < wave) before += sh.red32[v];
       all += sh.red32[v];
     }
@@ -326,56 +354,62 @@ __device__ inline uint64_t top_p_sum(float p, uint64_t S) {
 }
 
 // Any row: every question by a radix descent over the row in memory
-template <int DT>
+template <int DT, int NT>
 __device__ __attribute__((noinline)) Drawn sample_general(const Row<DT> row, const RowSettings st,
-                                                          Shared<DT>& sh) {
+                                                          Shared<DT, NT>& sh) {
   uint32_t best = 0;
-  row.each([&](uint32_t k, int) { best = max(best, k); });
-  best = block_max_u32(best, sh);
+  row.template each<NT>([&](uint32_t k, int) { best = max(best, k); });
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) best = max(best, (uint32_t)__shfl_xor(best, m));
+  __syncthreads();
+  if ((threadIdx.x & (kWave - 1)) == 0) sh.red32[threadIdx.x / kWave] = best;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) best = max(best, sh.red32[w]);
   if (!(st.T > 0.f) || best == 0u)   // greedy, or a row of NaN
-    return {nth_index<DT>(row, best, 0, sh), best ? 1.f : 0.f};
+    return {nth_index<DT, NT>(row, best, 0, sh), best ? 1.f : 0.f};
   const Weights w{key_value(best), best, 1.4426950408889634074 / (double)st.T};
   const double least = st.least();
   uint64_t S = 0, Sm = 0, have = 0;
-  row.each([&](uint32_t key, int) {
+  row.template each<NT>([&](uint32_t key, int) {
     const uint64_t m = key ? w(key) : 0ull;
     S += m;
     have += m ? 1 : 0;
     if (m && w.log2w(key) >= least) Sm += m;
   });
-  S = block_sum_u64(S, sh);
-  Sm = block_sum_u64(Sm, sh);
-  have = block_sum_u64(have, sh);
+  S = block_sum_u64<Shared<DT, NT>, NT>(S, sh);
+  Sm = block_sum_u64<Shared<DT, NT>, NT>(Sm, sh);
+  have = block_sum_u64<Shared<DT, NT>, NT>(have, sh);
   if (st.k > 0 && (uint64_t)st.k < have) {
     // the k-th token's value; its larger ones and the first of its ties are kept
-    const Crossing c = find_crossing<DT>(row, w, (uint64_t)(st.k - 1), true, sh);
+    const Crossing c = find_crossing<DT, NT>(row, w, (uint64_t)(st.k - 1), true, sh);
     uint64_t sum = 0;
-    row.each([&](uint32_t key, int) { sum += key > c.key ? w(key) : 0ull; });
-    S = block_sum_u64(sum, sh) + ((uint64_t)st.k - c.above) * w(c.key);
+    row.template each<NT>([&](uint32_t key, int) { sum += key > c.key ? w(key) : 0ull; });
+    S = block_sum_u64<Shared<DT, NT>, NT>(sum, sh) + ((uint64_t)st.k - c.above) * w(c.key);
   }
   if (st.p < 1.f) {
     const uint64_t P = top_p_sum(st.p, S);
-    const Crossing c = find_crossing<DT>(row, w, P - 1, false, sh);
+    const Crossing c = find_crossing<DT, NT>(row, w, P - 1, false, sh);
     const uint64_t W = w(c.key);
     S = c.above + ((P - 1 - c.above) / W + 1) * W;
   }
   S = min(S, Sm);
   const uint64_t target = draw_target(st.u, S);
-  const Crossing c = find_crossing<DT>(row, w, target, false, sh);
+  const Crossing c = find_crossing<DT, NT>(row, w, target, false, sh);
   const uint64_t W = w(c.key);
-  return {nth_index<DT>(row, c.key, (uint32_t)((target - c.above) / W), sh),
+  return {nth_index<DT, NT>(row, c.key, (uint32_t)((target - c.above) / W), sh),
           (float)((double)W / (double)S)};
 }
 
-// ----------------------------------------------------------------------------------
 // Passes over a row: its whole aligned 16-byte units, kAhead of them in flight per thread, and
 // the elements of its unaligned ends, one per thread.  Places without an element are NaN, which
 // no pass counts.  A row is read from HBM once; the passes after the first find it in the
-// caches.  (A workgroup's registers would hold a row of 150000 bf16 values, but the passes need
-// the rest of them: at every share kept there, the compiler spilled as much.)
-constexpr int kAhead = 4;
+// caches, and most of them read only the units of the threads that hold values above a bound.
+// (Registers for a row of 150000 bf16 values leave too few for the passes: at every share kept
+// there, the compiler spilled as much.)
+constexpr int kAhead = 10;
 
-template <int DT>
+template <int DT, int NT>
 struct Passes {
   static constexpr int U = Row<DT>::U;
   static constexpr uint32_t kNone = DT == TAPS_BF16 ? 0x7FC07FC0u : 0x7FC00000u;
@@ -386,37 +420,40 @@ struct Passes {
     head = x.lead ? min(U - x.lead, x.vocab) : 0;
     full = (x.vocab - head) / U;
   }
+  __device__ inline const char* first() const { return row.base + (int64_t)head * (16 / U); }
   // f(unit's 16 bytes, index of its first element); the trip count is the workgroup's
   template <class F>
   __device__ __attribute__((always_inline)) inline void units(F&& f) const {
     const int tid = threadIdx.x;
-    const char* const first = row.base + (int64_t)head * (16 / U);
-    for (int u0 = 0; u0 < full; u0 += kAhead * kThreads) {
+    for (int u0 = 0; u0 < full; u0 += kAhead * NT) {
       uint4 x[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j)
-        x[j] = *(const uint4*)(first + (int64_t)min(u0 + j * kThreads + tid, full - 1) * 16);
+        x[j] = *(const uint4*)(first() + (int64_t)min(u0 + j * NT + tid, full - 1) * 16);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const int u = u0 + j * kThreads + tid;
-        if (u0 + j * kThreads >= full) break;   // uniform
+        const int u = u0 + j * NT + tid;
+        if (u0 + j * NT >= full) break;   // uniform
         if (u >= full) x[j] = make_uint4(kNone, kNone, kNone, kNone);
         f(x[j], u * U + head);
       }
     }
-    if (row.vocab != full * U) {
-      const int rest = head + full * U;
-      int e = -1;
-      if (tid < U && tid < head) e = tid;
-      if (tid >= U && rest + tid - U < row.vocab) e = rest + tid - U;   // fewer than U of them
-      uint32_t b = kNone;
-      if (e >= 0)
-        b = DT == TAPS_BF16 ? 0x7FC00000u | ((const uint16_t*)row.base)[e]
-                            : ((const uint32_t*)row.base)[e];
-      f(make_uint4(b, kNone, kNone, kNone), max(e, 0));
-    }
+    ends(f);
   }
-  // the largest value (NaN left out; -inf where there is none)
+  template <class F>
+  __device__ __attribute__((always_inline)) inline void ends(F&& f) const {
+    if (row.vocab == full * U) return;
+    const int tid = threadIdx.x, rest = head + full * U;
+    int e = -1;
+    if (tid < U && tid < head) e = tid;
+    if (tid >= U && rest + tid - U < row.vocab) e = rest + tid - U;   // fewer than U of them
+    uint32_t b = kNone;
+    if (e >= 0)
+      b = DT == TAPS_BF16 ? 0x7FC00000u | ((const uint16_t*)row.base)[e]
+                          : ((const uint32_t*)row.base)[e];
+    f(make_uint4(b, kNone, kNone, kNone), max(e, 0));
+  }
+  // the largest value of this thread's units (NaN left out; -inf where there is none)
   __device__ __attribute__((always_inline)) inline float max_value() const {
     float mx = -INFINITY;
     units([&](const uint4& w, int) {
@@ -431,241 +468,284 @@ struct Passes {
     });
     return mx;
   }
-  // f(value, index) for the elements whose value is at least `thr`; units without any are
-  // passed over with two instructions per element
+  // f(value, index) for the elements with lo <= value <= hi: only the units of threads whose
+  // largest value `mx` reaches lo can hold one.  They are shared out to all threads; where they
+  // are most of the threads, every unit is read.  Callers synchronize before the next call.
   template <class F>
-  __device__ __attribute__((always_inline)) inline void at_least(float thr, F&& f) const {
-    units([&](const uint4& w, int e0) {
+  __device__ __attribute__((always_inline)) inline void between(float mx, float lo, float hi,
+                                                                Shared<DT, NT>& sh,
+                                                                F&& f) const {
+    const int tid = threadIdx.x;
+    if (tid == 0) sh.n_hot = 0u;
+    __syncthreads();
+    const uint64_t hot = __ballot(mx >= lo);
+    if (hot) {
+      uint32_t at = 0;
+      if ((tid & (kWave - 1)) == 0) at = atomicAdd(&sh.n_hot, (uint32_t)__popcll(hot));
+      at = __builtin_amdgcn_readfirstlane(at);
+      at += __builtin_amdgcn_mbcnt_hi((uint32_t)(hot >> 32),
+                                      __builtin_amdgcn_mbcnt_lo((uint32_t)hot, 0u));
+      if (mx >= lo) sh.hot[at] = (uint16_t)tid;
+    }
+    __syncthreads();
+    auto one = [&](const uint4& w, int e0) {
       const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-      bool any = false;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (DT == TAPS_BF16)
-          any |= __uint_as_float(ww[q] << 16) >= thr || __uint_as_float(ww[q] & 0xFFFF0000u) >= thr;
-        else
-          any |= __uint_as_float(ww[q]) >= thr;
-      }
-      if (!any) return;
 #pragma unroll
       for (int q = 0; q < U; ++q) {
         const uint32_t b = DT == TAPS_BF16
                                ? ((q & 1) ? ww[q >> 1] & 0xFFFF0000u : ww[q >> 1] << 16)
                                : ww[q & 3];
         const float x = __uint_as_float(b);
-        if (x >= thr) f(x, e0 + q);
+        if (x >= lo && x <= hi) f(x, e0 + q);
       }
-    });
+    };
+    const int n = (int)sh.n_hot, per = (full + NT - 1) / NT;
+    if (2 * n > NT) {
+      units(one);
+      return;
+    }
+    for (int i = tid; i < n * per; i += NT) {
+      const int j = i / n, u = j * NT + (int)sh.hot[i - j * n];
+      if (u < full) one(*(const uint4*)(first() + (int64_t)u * 16), u * U + head);
+    }
+    ends(one);
   }
 };
 
-__device__ inline uint64_t wave_scan_u64(uint64_t v) {
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const uint32_t lo = __shfl_up((uint32_t)v, d), hi = __shfl_up((uint32_t)(v >> 32), d);
-    if (lane >= d) v += ((uint64_t)hi << 32) | lo;
-  }
-  return v;
-}
-__device__ inline uint32_t wave_scan_u32(uint32_t v) {
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const uint32_t o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
-}
-__device__ inline uint64_t shfl_u64(uint64_t v, int lane) {
-  const uint32_t lo = __shfl((uint32_t)v, lane), hi = __shfl((uint32_t)(v >> 32), lane);
-  return ((uint64_t)hi << 32) | lo;
-}
-
-template <int DT>
-__device__ inline uint64_t block_scan_u64(uint64_t v, Shared<DT>& sh, uint64_t* total) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  v = wave_scan_u64(v);
-  __syncthreads();
-  if (lane == kWave - 1) sh.red[wave] = v;
-  __syncthreads();
-  uint64_t before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += sh.red[w];
-    all += sh.red[w];
-  }
-  *total = all;
-  return v + before;
-}
-
-template <int DT>
-__device__ inline float block_max_f32(float v, Shared<DT>& sh) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  __syncthreads();
-  if (lane == 0) sh.red32[wave] = __float_as_uint(v);
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) v = fmaxf(v, __uint_as_float(sh.red32[w]));
-  return v;
-}
-
-// A key that at least k elements reach: the k-th largest of the maxima of groups of four
+// A key that at least k elements reach: the k-th largest of the maxima of kGroups groups of
 // threads (0 where fewer groups hold a value).  k <= kFewTopK.
-template <int DT>
-__device__ inline uint32_t top_k_bound(float mx, int k, Shared<DT>& sh) {
+template <int DT, int NT>
+__device__ inline uint32_t top_k_bound(float mx, int k, Shared<DT, NT>& sh) {
+  constexpr int kPer = NT / kGroups;
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   uint32_t key = mx > -INFINITY ? value_key(__float_as_uint(mx)) : 0u;
-  key = max(key, (uint32_t)__shfl_xor(key, 1));
-  key = max(key, (uint32_t)__shfl_xor(key, 2));
-  if ((tid & 3) == 0) sh.group[tid >> 2] = key;
+#pragma unroll
+  for (int d = 1; d < kPer; d <<= 1) key = max(key, (uint32_t)__shfl_xor(key, d));
+  if (tid % kPer == 0) sh.group[tid / kPer] = key;
   __syncthreads();
   uint32_t g[kGroups / kWave];
 #pragma unroll
   for (int i = 0; i < kGroups / kWave; ++i) g[i] = sh.group[i * kWave + lane];
   uint32_t T = 0;
-  for (int bit = 31; bit >= (DT == TAPS_BF16 ? 16 : 0); --bit) {
-    const uint32_t c = T | (1u << bit);
-    int n = 0;
+  for (int bit = 30; bit >= (DT == TAPS_BF16 ? 16 : 0); bit -= 2) {   // two bits a step
+    const uint32_t c1 = T | (1u << bit), c2 = T | (2u << bit), c3 = T | (3u << bit);
+    int n1 = 0, n2 = 0, n3 = 0;
 #pragma unroll
-    for (int i = 0; i < kGroups / kWave; ++i) n += __popcll(__ballot(g[i] >= c));
-    if (n >= k) T = c;
+    for (int i = 0; i < kGroups / kWave; ++i) {
+      n1 += __popcll(__ballot(g[i] >= c1));
+      n2 += __popcll(__ballot(g[i] >= c2));
+      n3 += __popcll(__ballot(g[i] >= c3));
+    }
+    T = n3 >= k ? c3 : (n2 >= k ? c2 : (n1 >= k ? c1 : T));
   }
   return T;
 }
 
-// The nth (from 0) in index order of the `ties` elements equal to `value`
-template <int DT>
-__device__ __attribute__((always_inline)) inline int nth_equal(const Passes<DT>& passes, float value, uint32_t nth, uint32_t ties,
-                                Shared<DT>& sh) {
-  if (ties > (uint32_t)kList)
-    return nth_index<DT>(passes.row, value_key(__float_as_uint(value)), nth, sh);
+// ----------------------------------------------------------------------------------
+// Elements ranked one by one: list[0 .. n) into sorted[]
+template <int DT, int NT>
+__device__ inline void sort_list(uint32_t n, Shared<DT, NT>& sh) {
+  ListScratch& ls = sh.u.l;
+  for (uint32_t i = threadIdx.x; i < n; i += NT) {
+    const uint64_t mine = ls.list[i];
+    uint32_t rank = 0;
+    for (uint32_t j = 0; j < n; ++j) rank += ls.list[j] > mine ? 1u : 0u;
+    ls.sorted[rank] = mine;
+  }
+  __syncthreads();
+}
+
+// cum[i] = f(sum of w(key of sorted[0]) .. w(key of sorted[i])); returns the whole sum
+template <int DT, int NT, class W, class F>
+__device__ inline uint64_t sum_list(uint32_t n, Shared<DT, NT>& sh, W&& w, F&& f) {
+  constexpr int E = kList / NT;
+  ListScratch& ls = sh.u.l;
+  const uint32_t i0 = threadIdx.x * E;
+  uint64_t m[E], sum = 0, all;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    m[e] = i0 + e < n ? w((uint32_t)(ls.sorted[i0 + e] >> 32)) : 0ull;
+    sum += m[e];
+  }
+  uint64_t run = block_scan_u64<Shared<DT, NT>, NT>(sum, sh, &all) - sum;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    run += m[e];
+    if (i0 + e < n) ls.cum[i0 + e] = f(run);
+  }
+  __syncthreads();
+  return all;
+}
+
+// the first position of cum[0 .. n) that exceeds target (one does)
+template <int DT, int NT>
+__device__ inline uint32_t first_above(uint64_t target, uint32_t n, Shared<DT, NT>& sh) {
+  const ListScratch& ls = sh.u.l;
+  for (uint32_t i = threadIdx.x; i < n; i += NT)
+    if (ls.cum[i] > target && (i == 0 || ls.cum[i - 1] <= target)) sh.out32[1] = i;
+  __syncthreads();
+  const uint32_t r = sh.out32[1];
+  __syncthreads();
+  return r;
+}
+
+// how many of the list's first elements satisfy `in` (those that do come first)
+template <int DT, int NT, class F>
+__device__ inline uint32_t count_list(uint32_t n, Shared<DT, NT>& sh, F&& in) {
+  uint64_t c = 0;
+  for (uint32_t i = threadIdx.x; i < n; i += NT)
+    c += in((uint32_t)(sh.u.l.sorted[i] >> 32)) ? 1 : 0;
+  return (uint32_t)block_sum_u64<Shared<DT, NT>, NT>(c, sh);
+}
+
+// A float bound rounded down by more than the arithmetic can be off; M where it is not a number
+// (an infinite maximum)
+__device__ inline float bound_below(double x, float M) {
+  const float b = (float)(x - 1e-6 * (fabs(x) + fabs((double)M)));
+  return b == b ? b : M;
+}
+
+// A small top_k, or min_p: the elements above a bound, ranked.  False: more than kList of them.
+template <int DT, int NT>
+__device__ __attribute__((always_inline)) inline bool sample_listed(
+    const Passes<DT, NT>& passes, float mx, const Weights& w, const RowSettings& st,
+    Shared<DT, NT>& sh, Drawn* out) {
+  const double least = st.least();
+  float thr = -INFINITY;
+  if (st.cut_by_min_p()) thr = bound_below((double)w.top + least / w.scale, w.top);
+  if (st.few()) {
+    const uint32_t key = top_k_bound<DT, NT>(mx, st.k, sh);
+    if (key) thr = fmaxf(thr, key_value(key));
+  }
+  ListScratch& ls = sh.u.l;
   if (threadIdx.x == 0) sh.n = 0u;
   __syncthreads();
-  passes.units([&](const uint4& w, int e0) {
-    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-    bool any = false;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (DT == TAPS_BF16)
-        any |= __uint_as_float(ww[q] << 16) == value || __uint_as_float(ww[q] & 0xFFFF0000u) == value;
-      else
-        any |= __uint_as_float(ww[q]) == value;
-    }
-    if (!any) return;
-#pragma unroll
-    for (int q = 0; q < Passes<DT>::U; ++q) {
-      const uint32_t b = DT == TAPS_BF16 ? ((q & 1) ? ww[q >> 1] & 0xFFFF0000u : ww[q >> 1] << 16)
-                                         : ww[q & 3];
-      if (__uint_as_float(b) == value) sh.ties[atomicAdd(&sh.n, 1u)] = (uint32_t)(e0 + q);
-    }
+  passes.between(mx, thr, INFINITY, sh, [&](float x, int e) {
+    const uint32_t i = atomicAdd(&sh.n, 1u);
+    if (i < (uint32_t)kList) ls.list[i] = cand_key(value_key(__float_as_uint(x)), (uint32_t)e);
   });
   __syncthreads();
   const uint32_t n = sh.n;
-  for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-    const uint32_t mine = sh.ties[i];
-    uint32_t before = 0;
-    for (uint32_t j = 0; j < n; ++j) before += sh.ties[j] < mine ? 1u : 0u;
-    if (before == nth) sh.out32[3] = mine;
+  if (n > (uint32_t)kList) return false;
+  sort_list<DT, NT>(n, sh);
+  uint64_t S = sum_list<DT, NT>(n, sh, w, [](uint64_t c) { return c; });
+  if (st.k > 0 && (uint32_t)st.k < n) S = ls.cum[st.k - 1];
+  if (st.p < 1.f) S = ls.cum[first_above<DT, NT>(top_p_sum(st.p, S) - 1, n, sh)];
+  if (st.mp > 0.f) {
+    const uint32_t in =
+        count_list<DT, NT>(n, sh, [&](uint32_t key) { return w.log2w(key) >= least; });
+    S = min(S, ls.cum[in - 1]);
   }
-  __syncthreads();
-  return (int)sh.out32[3];
+  const uint32_t r = first_above<DT, NT>(draw_target(st.u, S), n, sh);
+  out->token = (int)cand_index(ls.sorted[r]);
+  out->prob = (float)((double)(ls.cum[r] - (r ? ls.cum[r - 1] : 0ull)) / (double)S);
+  return true;
 }
 
 // ----------------------------------------------------------------------------------
 // bf16: a row holds few distinct values, so the elements are counted by value (16-bit keys from
 // the largest down, as far as weights reach) and every sum is over values: one exponential per
-// value that occurs, none per element, and a crossing is exact at once.
-// Returns false where the window is too wide (or nothing exceeds -inf): the general path's.
+// value that occurs, none per element, and a crossing is exact at once.  Returns false where
+// the window is too wide or a value occurs 65536 times.
+// 16 bits per count let two workgroups share a CU's LDS.
 constexpr uint32_t kLowest16 = 0x007Fu;   // the key of -inf; smaller ones are NaN
 __device__ inline uint32_t key16(float x) { return value_key(__float_as_uint(x)) >> 16; }
+// the whole key of a 16-bit one: it ends in zeros, or ones where the value is negative
+__device__ inline uint32_t key32(uint32_t k) { return (k << 16) | ((k & 0x8000u) ? 0u : 0xFFFFu); }
 
-template <int DT>
-__device__ __attribute__((always_inline)) inline bool sample_counted(const Passes<DT>& passes, float mx_thread, float M,
-                                      const RowSettings& st, Shared<DT>& sh, Drawn* out) {
+template <int DT, int NT>
+__device__ __attribute__((always_inline)) inline bool sample_counted(
+    const Passes<DT, NT>& passes, float mx, const Weights& w, const RowSettings& st,
+    Shared<DT, NT>& sh, Drawn* out) {
+  constexpr int kWaves = NT / kWave;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  const uint32_t kM = key16(M);
+  const uint32_t kM = w.key >> 16;
   CountScratch& cs = sh.u.c;
-  const Weights w{M, value_key(__float_as_uint(M)), 1.4426950408889634074 / (double)st.T};
-  // values that can have a weight, and that the filters can keep (a little more never hurts:
-  // the bounds are rounded to bf16, so two more keys)
-  const double least = st.least();
-  const double reach = st.cut_by_min_p() ? fmax(least, -44.5) : -44.5;
-  const float low = (float)((double)M + reach / w.scale);
+  // down to the values whose weight rounds to 0 (two more: the bound is rounded to bf16)
+  const float low = (float)((double)w.top - 44.5 / w.scale);
   uint32_t klow = low > -INFINITY ? key16(low) : 0u;
   klow = klow > kLowest16 + 2u ? klow - 2u : kLowest16;
-  if (st.few()) klow = max(klow, top_k_bound<DT>(mx_thread, st.k, sh) >> 16);
   if (klow == 0x8000u) klow = 0x7FFFu;   // +0 and -0 are equal
   klow = min(klow, kM);
   const uint32_t Wn = kM - klow + 1u;
   if (Wn > (uint32_t)kWindow) return false;
-  for (uint32_t i = tid; i < (Wn + kWave - 1) / kWave * kWave; i += kThreads) cs.count[i] = 0u;
+  const int runs = (int)((Wn + kRun - 1) / kRun);
+  for (int i = tid; i < runs * (kRun / 8); i += NT)
+    ((uint4*)cs.count)[i] = make_uint4(0u, 0u, 0u, 0u);
   __syncthreads();
-  if (st.few() || st.cut_by_min_p()) {
-    // few elements: compare first.  The value of the lowest key
-    const float thr = __uint_as_float((klow & 0x8000u) ? (klow & 0x7FFFu) << 16 : (~klow & 0xFFFFu) << 16);
-    passes.at_least(thr, [&](float x, int) {
-      const uint32_t i = kM - key16(x);
-      if (i < Wn) atomicAdd(&cs.count[i], 1u);
-    });
-  } else {
-    passes.units([&](const uint4& v, int) {
-      const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
-      typedef short s16x2 __attribute__((ext_vector_type(2)));
-      typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-      const u16x2 top = {(unsigned short)kM, (unsigned short)kM};
+  uint32_t in_window = 0;   // of the wave
+  passes.units([&](const uint4& v, int) {
+    const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const u16x2 top = {(unsigned short)kM, (unsigned short)kM};
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        // both halves: key = sign ? ~bits : bits | 0x8000; NaN keys fall outside the window
-        const s16x2 b = __builtin_bit_cast(s16x2, ww[q]);
-        const uint32_t sign = __builtin_bit_cast(uint32_t, (s16x2)(b >> 15));
-        const u16x2 key = __builtin_bit_cast(u16x2, ww[q] ^ (sign | 0x80008000u));
-        const uint32_t idx = __builtin_bit_cast(uint32_t, (u16x2)(top - key));
-        const uint32_t i0 = idx & 0xFFFFu, i1 = idx >> 16;
-        if (i0 < Wn) atomicAdd(&cs.count[i0], 1u);
-        if (i1 < Wn) atomicAdd(&cs.count[i1], 1u);
-      }
-    });
-  }
-  __syncthreads();
-  if (tid == 0 && kM >= 0x8000u) {   // -0 counts as +0
-    const uint32_t z = kM - 0x8000u;
-    if (z + 1u < Wn) {
-      cs.count[z] += cs.count[z + 1u];
-      cs.count[z + 1u] = 0u;
+    for (int q = 0; q < 4; ++q) {
+      // both halves: key = sign ? ~bits : bits | 0x8000; NaN keys fall outside the window
+      const s16x2 b = __builtin_bit_cast(s16x2, ww[q]);
+      const uint32_t sign = __builtin_bit_cast(uint32_t, (s16x2)(b >> 15));
+      const u16x2 key = __builtin_bit_cast(u16x2, ww[q] ^ (sign | 0x80008000u));
+      const uint32_t idx = __builtin_bit_cast(uint32_t, (u16x2)(top - key));
+      const uint32_t i0 = idx & 0xFFFFu, i1 = idx >> 16;
+      in_window += __popcll(__ballot(i0 < Wn)) + __popcll(__ballot(i1 < Wn));
+      if (i0 < Wn) atomicAdd(&cs.count[i0 >> 1], 1u + (i0 & 1u) * 0xFFFFu);
+      if (i1 < Wn) atomicAdd(&cs.count[i1 >> 1], 1u + (i1 & 1u) * 0xFFFFu);
     }
+  });
+  __syncthreads();
+  auto count_at = [&](uint32_t i) -> uint32_t {
+    return (cs.count[i >> 1] >> (16 * (i & 1u))) & 0xFFFFu;
+  };
+  if (tid == 0 && kM >= 0x8000u && kM - 0x8000u + 1u < Wn) {   // -0 counts as +0
+    const uint32_t z = kM - 0x8000u;
+    const uint32_t a = count_at(z), b = count_at(z + 1u);
+    cs.count[z >> 1] += ((a + b) & 0xFFFFu) << (16 * (z & 1u));
+    cs.count[z >> 1] -= a << (16 * (z & 1u));
+    cs.count[(z + 1u) >> 1] -= b << (16 * ((z + 1u) & 1u));
   }
   __syncthreads();
 
-  // weight of the value at window position i
-  auto weight = [&](uint32_t i) -> uint64_t {
-    const uint32_t k = kM - i;   // 16 bits; the value's full key
-    return w((k << 16) | ((k & 0x8000u) ? 0u : 0xFFFFu));
+  // four values per lane of run r: their counts and weights
+  struct Four {
+    uint32_t c[4];
+    uint64_t W[4], m[4];
   };
-  const int rows = (int)((Wn + kWave - 1) / kWave);
-  for (int r = wave; r < rows; r += kWaves) {
-    const uint32_t c = cs.count[r * kWave + lane];
+  auto four = [&](int r, bool by_count) -> Four {
+    const uint2 p = ((const uint2*)cs.count)[r * kWave + lane];
+    Four f;
+    f.c[0] = p.x & 0xFFFFu;
+    f.c[1] = p.x >> 16;
+    f.c[2] = p.y & 0xFFFFu;
+    f.c[3] = p.y >> 16;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f.W[j] = f.c[j] ? w(key32(kM - (uint32_t)(r * kRun + 4 * lane + j))) : 0ull;
+      f.m[j] = by_count ? (uint64_t)f.c[j] : f.W[j] * f.c[j];
+    }
+    return f;
+  };
+  for (int r = wave; r < runs; r += kWaves) {
+    const uint2 p = ((const uint2*)cs.count)[r * kWave + lane];
     uint64_t m = 0;
     uint32_t n = 0;
-    if (__ballot(c != 0u)) {
-      m = c ? (uint64_t)c * weight(r * kWave + lane) : 0ull;
-      m = wave_sum_u64(m);
-      n = c;
-#pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) n += __shfl_xor(n, d);
+    if (__ballot((p.x | p.y) != 0u)) {
+      const Four f = four(r, false);
+      m = wave_sum_u64(f.m[0] + f.m[1] + f.m[2] + f.m[3]);
+      n = __builtin_amdgcn_readlane(wave_scan_u32(f.c[0] + f.c[1] + f.c[2] + f.c[3]), kWave - 1);
     }
     if (lane == 0) cs.mass[r] = m, cs.num[r] = n;
   }
   __syncthreads();
-  uint64_t S, have;
+  uint64_t S, have, counted;
   {
-    const uint64_t m = tid < rows ? cs.mass[tid] : 0ull;
-    const uint64_t n = tid < rows ? cs.num[tid] : 0ull;
-    const uint64_t pm = block_scan_u64(m, sh, &S) - m, pn = block_scan_u64(n, sh, &have) - n;
-    if (tid < rows) cs.mass[tid] = pm, cs.num[tid] = (uint32_t)pn;
+    const uint64_t m = tid < runs ? cs.mass[tid] : 0ull, n = tid < runs ? cs.num[tid] : 0ull;
+    const uint64_t pm = block_scan_u64<Shared<DT, NT>, NT>(m, sh, &S) - m;
+    const uint64_t pn = block_scan_u64<Shared<DT, NT>, NT>(n, sh, &have) - n;
+    if (tid < runs) cs.mass[tid] = pm, cs.num[tid] = (uint32_t)pn;
+    counted = block_sum_u64<Shared<DT, NT>, NT>(lane == 0 ? in_window : 0u, sh);
   }
-  __syncthreads();
+  // a count past 16 bits loses 65536, or turns them into one of its neighbour's
+  if (counted != have) return false;
 
   struct Cross {
     uint32_t pos, ties, nth;     // window position, elements there, the crossing one among them
@@ -673,33 +753,44 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(const Passe
   };
   // where the running sum (count) first exceeds target
   auto crossing = [&](uint64_t target, bool by_count) -> Cross {
-    if (tid < rows) {
+    if (tid < runs) {
       const uint64_t a = by_count ? cs.num[tid] : cs.mass[tid];
-      const uint64_t b = tid + 1 < rows ? (by_count ? cs.num[tid + 1] : cs.mass[tid + 1])
+      const uint64_t b = tid + 1 < runs ? (by_count ? cs.num[tid + 1] : cs.mass[tid + 1])
                                         : (by_count ? have : S);
       if (a <= target && target < b) sh.out32[0] = (uint32_t)tid;
     }
     __syncthreads();
-    const int r = (int)sh.out32[0];
+    const int r = __builtin_amdgcn_readfirstlane(sh.out32[0]);
     __syncthreads();
-    const uint32_t i = (uint32_t)(r * kWave + lane), c = cs.count[i];
-    const uint64_t W = c ? weight(i) : 0ull;
-    const uint64_t m = by_count ? (uint64_t)c : (uint64_t)c * W;
-    const uint64_t incl = (by_count ? (uint64_t)cs.num[r] : cs.mass[r]) + wave_scan_u64(m);
+    const Four f = four(r, by_count);
+    const uint64_t mine = f.m[0] + f.m[1] + f.m[2] + f.m[3];
+    const uint64_t incl = (by_count ? (uint64_t)cs.num[r] : cs.mass[r]) + wave_scan_u64(mine);
     const int l = __ffsll((long long)__ballot(incl > target)) - 1;
+    uint64_t above = incl - mine, W = f.W[0];
+    uint32_t j = 0, ties = f.c[0];
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+      if (j == (uint32_t)t && above + f.m[t] <= target) {
+        above += f.m[t];
+        j = t + 1;
+        W = f.W[t + 1];
+        ties = f.c[t + 1];
+      }
     Cross x;
-    x.pos = (uint32_t)(r * kWave + l);
-    x.ties = __shfl(c, l);
-    x.W = shfl_u64(W, l);
-    x.above = shfl_u64(incl - m, l);
+    x.pos = __builtin_amdgcn_readlane((uint32_t)(r * kRun + 4 * lane) + j, l);
+    x.ties = __builtin_amdgcn_readlane(ties, l);
+    x.W = lane_u64(W, l);
+    x.above = lane_u64(above, l);
     x.nth = by_count ? (uint32_t)(target - x.above) : (uint32_t)((target - x.above) / x.W);
     return x;
   };
   // sum of the weights before window position i
   auto sum_before = [&](uint32_t i) -> uint64_t {
-    const int r = (int)(i / kWave);
-    const uint32_t at = (uint32_t)(r * kWave + lane), c = cs.count[at];
-    const uint64_t m = c && at < i ? (uint64_t)c * weight(at) : 0ull;
+    const int r = (int)(i / kRun);
+    const Four f = four(r, false);
+    uint64_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m += (uint32_t)(r * kRun + 4 * lane + j) < i ? f.m[j] : 0ull;
     return cs.mass[r] + wave_sum_u64(m);
   };
 
@@ -713,178 +804,134 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(const Passe
     kept = c.above + (uint64_t)(c.nth + 1u) * c.W;
   }
   if (st.mp > 0.f) {
-    uint32_t lo = 0, hi = Wn;   // positions below lo are kept, those from hi on are not
+    const double least = st.least();
+    uint32_t lo = 0, hi = Wn;   // positions to lo are kept, those from hi on are not
     while (hi - lo > 1u) {
-      const uint32_t mid = (lo + hi) / 2u, k = kM - mid;
-      if (w.log2w((k << 16) | ((k & 0x8000u) ? 0u : 0xFFFFu)) >= least) lo = mid;
+      const uint32_t mid = (lo + hi) / 2u;
+      if (w.log2w(key32(kM - mid)) >= least) lo = mid;
       else hi = mid;
     }
     if (hi < Wn) kept = min(kept, sum_before(hi));
   }
   const Cross c = crossing(draw_target(st.u, kept), false);
-  const uint32_t k = kM - c.pos;
-  out->token = nth_equal<DT>(
-      passes, __uint_as_float((k & 0x8000u) ? (k & 0x7FFFu) << 16 : (~k & 0xFFFFu) << 16), c.nth,
-      c.ties, sh);
+  const uint32_t key = key32(kM - c.pos);
   out->prob = (float)((double)c.W / (double)kept);
+  if (c.ties > (uint32_t)kList) {
+    out->token = nth_index<DT, NT>(passes.row, key, c.nth, sh);
+    return true;
+  }
+  // the nth of the value's elements in index order
+  if (tid == 0) sh.n = 0u;
+  __syncthreads();   // the counts are read: the list may take their place
+  const float value = key_value(key);
+  passes.between(mx, value, value, sh, [&](float, int e) {
+    sh.u.l.list[atomicAdd(&sh.n, 1u)] = (uint64_t)(0xFFFFFFFFu - (uint32_t)e);
+  });
+  __syncthreads();
+  sort_list<DT, NT>(c.ties, sh);
+  out->token = (int)(0xFFFFFFFFu - (uint32_t)sh.u.l.sorted[c.nth]);
   return true;
 }
 
 // ----------------------------------------------------------------------------------
-// fp32, few candidates (a small top_k, or min_p): the elements above a bound, ranked one by
-// one.  False: more than kList of them.
-template <int DT>
-__device__ inline void sort_list(uint32_t n, Shared<DT>& sh) {
-  BinScratch& bs = sh.u.b;
-  const uint32_t i = threadIdx.x;
-  if (i < n) {
-    const uint64_t mine = bs.list[i];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) rank += bs.list[j] > mine ? 1u : 0u;
-    bs.sorted[rank] = mine;
-  }
-  __syncthreads();
-}
-
-// the first position of cum[0 .. n) that exceeds target (one does)
-template <int DT>
-__device__ inline uint32_t first_above(uint64_t target, uint32_t n, Shared<DT>& sh) {
-  const BinScratch& bs = sh.u.b;
-  const uint32_t i = threadIdx.x;
-  if (i < n && bs.cum[i] > target && (i == 0 || bs.cum[i - 1] <= target)) sh.out32[1] = i;
-  __syncthreads();
-  const uint32_t r = sh.out32[1];
-  __syncthreads();
-  return r;
-}
-
-template <int DT>
-__device__ __attribute__((always_inline)) inline bool sample_listed(const Passes<DT>& passes, float mx_thread, float M,
-                                     const RowSettings& st, Shared<DT>& sh, Drawn* out) {
-  const int tid = threadIdx.x;
-  BinScratch& bs = sh.u.b;
-  const Weights w{M, value_key(__float_as_uint(M)), 1.4426950408889634074 / (double)st.T};
-  const double least = st.least();
-  float thr = -INFINITY;
-  if (st.cut_by_min_p()) {   // rounded down by more than the arithmetic can be off
-    const double low = (double)M + least / w.scale;
-    thr = (float)(low - 1e-6 * (fabs(low) + fabs((double)M)));
-    if (thr != thr) thr = M;   // an infinite maximum
-  }
-  if (st.few()) {
-    const uint32_t key = top_k_bound<DT>(mx_thread, st.k, sh);
-    if (key) thr = fmaxf(thr, key_value(key));
-  }
-  if (tid == 0) sh.n = 0u;
-  __syncthreads();
-  passes.at_least(thr, [&](float x, int e) {
-    const uint32_t i = atomicAdd(&sh.n, 1u);
-    if (i < (uint32_t)kList) bs.list[i] = cand_key(value_key(__float_as_uint(x)), (uint32_t)e);
-  });
-  __syncthreads();
-  const uint32_t n = sh.n;
-  if (n > (uint32_t)kList) return false;
-  sort_list<DT>(n, sh);
-  const uint32_t key = (uint32_t)tid < n ? (uint32_t)(bs.sorted[tid] >> 32) : 0u;
-  const uint64_t W = key ? w(key) : 0ull;
-  uint64_t all;
-  const uint64_t cum = block_scan_u64(W, sh, &all);
-  if ((uint32_t)tid < n) bs.cum[tid] = cum;
-  uint64_t Sm = block_sum_u64(key && w.log2w(key) >= least ? W : 0ull, sh);   // also a barrier
-  uint64_t S = st.k > 0 && (uint32_t)st.k < n ? bs.cum[st.k - 1] : all;
-  if (st.p < 1.f) S = bs.cum[first_above<DT>(top_p_sum(st.p, S) - 1, n, sh)];
-  S = min(S, Sm);
-  const uint32_t r = first_above<DT>(draw_target(st.u, S), n, sh);
-  out->token = (int)cand_index(bs.sorted[r]);
-  out->prob = (float)((double)(bs.cum[r] - (r ? bs.cum[r - 1] : 0ull)) / (double)S);
-  return true;
-}
-
 // fp32, the whole vocabulary's sum (top_p or no filter): weights are added up by bins of 1/32
-// octave.  Weight 2^-(z / 32), z = 32 log2(e) (M - x) / T, is the bin's 2^-(b / 32), b = floor z,
-// times a factor 2^-((z - b) / 32) from a short series; a bin adds up its factors (integers of
-// 2^-43), and its sum is that times 2^-(b / 32), rounded down.  The bin where a running sum passes its
-// target is then ranked one by one.  False: more than kList elements in it.
-template <int DT>
-__device__ __attribute__((always_inline)) inline bool sample_binned(const Passes<DT>& passes, float M, const RowSettings& st,
-                                     Shared<DT>& sh, Drawn* out) {
+// octave.  Weight 2^-(z / 32), z = 32 log2(e) (M - x) / T, is the bin's 2^-(b / 32), b = floor
+// z, times a factor 2^-((z - b) / 32) from a short series; a bin adds up its factors (integers
+// of 2^-43), and its sum is that times 2^-(b / 32), rounded down.  The bin where a running sum
+// passes its target is then ranked one by one.  False: more than kList elements in it.
+template <int DT, int NT>
+__device__ __attribute__((always_inline)) inline bool sample_binned(
+    const Passes<DT, NT>& passes, float mx, const Weights& w, const RowSettings& st,
+    Shared<DT, NT>& sh, Drawn* out) {
   const int tid = threadIdx.x;
   BinScratch& bs = sh.u.b;
-  const double scale = kPerOctave * 1.4426950408889634074 / (double)st.T;
-  for (int i = tid; i < kWeightBins; i += kThreads) bs.mass[i] = 0ull;
+  const float M = w.top;
+  const double scale = kPerOctave * w.scale;
+  for (int i = tid; i < kWeightBins; i += NT) bs.mass[i] = 0ull;
   __syncthreads();
-  auto depth = [&](float x) -> double { return x == M ? 0.0 : ((double)M - (double)x) * scale; };
-  // the factor in units of 2^-43
-  auto factor = [&](double z, int b) -> uint64_t {
-    const double t = (z - (double)b) * (-0.69314718055994530942 / kPerOctave);
-    double p = 1.0 / 720.0;
-    p = fma(p, t, 1.0 / 120.0);
-    p = fma(p, t, 1.0 / 24.0);
-    p = fma(p, t, 1.0 / 6.0);
-    p = fma(p, t, 0.5);
-    p = fma(p, t, 1.0);
-    p = fma(p, t, 1.0);
-    // the sum with 512 has steps of 2^-43: its low bits are the rounded integer
-    return (uint64_t)(__double_as_longlong(p + 512.0) - __double_as_longlong(512.0));
+  // an infinite maximum: its equals have depth 0, not NaN
+  const bool inf = M == INFINITY;
+  auto depth = [&](float x) -> double {
+    const double d = (double)M - (double)x;
+    return (inf && x == M ? 0.0 : d) * scale;
+  };
+  // 512 + the factor: the double's low bits are the factor in units of 2^-43, rounded
+  auto factor = [&](double z) -> uint64_t {
+    constexpr double c = -0.69314718055994530942 / kPerOctave;
+    const double t = __builtin_amdgcn_fract(z);
+    double p = c * c * c * c * c * c / 720.0;
+    p = fma(p, t, c * c * c * c * c / 120.0);
+    p = fma(p, t, c * c * c * c / 24.0);
+    p = fma(p, t, c * c * c / 6.0);
+    p = fma(p, t, c * c * 0.5);
+    p = fma(p, t, c);
+    p = fma(p, t, 513.0);
+    return (uint64_t)(__double_as_longlong(p) - __double_as_longlong(512.0));
   };
   passes.units([&](const uint4& v, int) {
     const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const double z = depth(__uint_as_float(ww[q]));
-      if (z < (double)kWeightBins) {
-        const int b = (int)z;
-        atomicAdd((unsigned long long*)&bs.mass[b], (unsigned long long)factor(z, b));
-      }
+      if (z < (double)kWeightBins)
+        atomicAdd((unsigned long long*)&bs.mass[(int)z], (unsigned long long)factor(z));
     }
   });
   __syncthreads();
   auto bin_scale = [&](int b) -> double { return exp2_neg(-(double)b / kPerOctave); };
   uint64_t S;
   {
-    const int b0 = 2 * tid;
-    uint64_t m0 = 0, m1 = 0;
-    if (b0 < kWeightBins) {
-      m0 = (uint64_t)(bin_scale(b0) * (double)bs.mass[b0]);
-      m1 = (uint64_t)(bin_scale(b0 + 1) * (double)bs.mass[b0 + 1]);
+    constexpr int E = (kWeightBins + NT - 1) / NT;
+    uint64_t m[E], sum = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int b = tid * E + e;
+      m[e] = b < kWeightBins ? (uint64_t)(bin_scale(b) * (double)bs.mass[b]) : 0ull;
+      sum += m[e];
     }
-    const uint64_t incl = block_scan_u64(m0 + m1, sh, &S);
-    if (b0 < kWeightBins) bs.before[b0] = incl - m0 - m1, bs.before[b0 + 1] = incl - m1;
+    uint64_t run = block_scan_u64<Shared<DT, NT>, NT>(sum, sh, &S) - sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int b = tid * E + e;
+      if (b < kWeightBins) bs.before[b] = run;
+      run += m[e];
+    }
   }
   __syncthreads();
-  static_assert(kWeightBins % 2 == 0 && kWeightBins <= 2 * kThreads, "two bins per thread");
 
   // Ranks the elements of a bin: sorted[], and the running sums with each of them in cum[].
   // Returns their number; above kList nothing is ranked.
+  int ranked = -1;
   auto rank_bin = [&](int bin) -> uint32_t {
+    if (bin == ranked) return sh.n;
+    ranked = bin;
+    __syncthreads();
     if (tid == 0) sh.n = 0u;
     __syncthreads();
-    passes.units([&](const uint4& v, int e0) {
-      const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const double z = depth(__uint_as_float(ww[q]));
-        if (z >= (double)bin && z < (double)(bin + 1)) {
-          const uint32_t i = atomicAdd(&sh.n, 1u);
-          if (i < (uint32_t)kList) bs.list[i] = cand_key(value_key(ww[q]), (uint32_t)(e0 + q));
-        }
+    const float lo = bound_below((double)M - (double)(bin + 1) / scale, M);
+    const float hi = -bound_below((double)bin / scale - (double)M, -M);
+    passes.between(mx, lo, hi, sh, [&](float x, int e) {
+      const double z = depth(x);
+      if (z >= (double)bin && z < (double)(bin + 1)) {
+        const uint32_t i = atomicAdd(&sh.n, 1u);
+        if (i < (uint32_t)kList)
+          bs.l.list[i] = cand_key(value_key(__float_as_uint(x)), (uint32_t)e);
       }
     });
     __syncthreads();
     const uint32_t n = sh.n;
     if (n > (uint32_t)kList) return n;
-    sort_list<DT>(n, sh);
-    uint64_t f = 0;
-    if ((uint32_t)tid < n) f = factor(depth(key_value((uint32_t)(bs.sorted[tid] >> 32))), bin);
-    uint64_t all;
-    const uint64_t cum = block_scan_u64(f, sh, &all);
-    if ((uint32_t)tid < n) bs.cum[tid] = bs.before[bin] + (uint64_t)(bin_scale(bin) * (double)cum);
-    __syncthreads();
+    sort_list<DT, NT>(n, sh);
+    const double bsc = bin_scale(bin);
+    const uint64_t before = bs.before[bin];
+    sum_list<DT, NT>(
+        n, sh, [&](uint32_t key) { return factor(depth(key_value(key))); },
+        [&](uint64_t c) { return before + (uint64_t)(bsc * (double)c); });
     return n;
   };
   // the bin where the running sum first exceeds target
   auto bin_of = [&](uint64_t target) -> int {
-    for (int b = tid; b < kWeightBins; b += kThreads) {
+    for (int b = tid; b < kWeightBins; b += NT) {
       const uint64_t hi = b + 1 < kWeightBins ? bs.before[b + 1] : S;
       if (bs.before[b] <= target && target < hi) sh.out32[0] = (uint32_t)b;
     }
@@ -896,7 +943,7 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(const Passes
     const uint64_t target = top_p_sum(st.p, S) - 1;
     const uint32_t n = rank_bin(bin_of(target));
     if (n > (uint32_t)kList) return false;
-    kept = bs.cum[first_above<DT>(target, n, sh)];
+    kept = bs.l.cum[first_above<DT, NT>(target, n, sh)];
   }
   if (st.mp > 0.f) {
     const double last = -kPerOctave * st.least();   // the depth down to which tokens are kept
@@ -904,10 +951,9 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(const Passes
       const uint32_t n = rank_bin((int)last);
       if (n > (uint32_t)kList) return false;
       // kept ones of the bin come first; without any, all before it
-      bool in = false;
-      if ((uint32_t)tid < n) in = depth(key_value((uint32_t)(bs.sorted[tid] >> 32))) <= last;
-      const uint32_t num = (uint32_t)block_sum_u64(in ? 1ull : 0ull, sh);
-      kept = min(kept, num ? bs.cum[num - 1] : bs.before[(int)last]);
+      const uint32_t in =
+          count_list<DT, NT>(n, sh, [&](uint32_t key) { return depth(key_value(key)) <= last; });
+      kept = min(kept, in ? bs.l.cum[in - 1] : bs.before[(int)last]);
       __syncthreads();
     }
   }
@@ -915,19 +961,19 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(const Passes
   const int bin = bin_of(target);
   const uint32_t n = rank_bin(bin);
   if (n > (uint32_t)kList) return false;
-  const uint64_t key = bs.sorted[first_above<DT>(target, n, sh)];
+  const uint64_t key = bs.l.sorted[first_above<DT, NT>(target, n, sh)];
   out->token = (int)cand_index(key);
-  out->prob = (float)(bin_scale(bin) *
-                      (double)factor(depth(key_value((uint32_t)(key >> 32))), bin) / (double)kept);
+  out->prob = (float)(bin_scale(bin) * (double)factor(depth(key_value((uint32_t)(key >> 32)))) /
+                      (double)kept);
   return true;
 }
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void sample_kernel(
+template <int DT, int NT>
+__global__ __launch_bounds__(NT, 4) void sample_kernel(
     const void* __restrict__ logits, int64_t row_bytes, int budget, int vocab,
     const int32_t* __restrict__ n_nodes, const Settings s, const float* __restrict__ u,
     int32_t* __restrict__ tokens, float* __restrict__ probs) {
-  __shared__ Shared<DT> sh;
+  __shared__ Shared<DT, NT> sh;
   const int r = blockIdx.x, b = r / budget, tid = threadIdx.x;
   if (n_nodes && r - b * budget >= n_nodes[b]) {
     if (tid == 0) {
@@ -937,7 +983,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(
     return;
   }
   const Row<DT> row((const char*)logits + (size_t)r * row_bytes, vocab);
-  const Passes<DT> passes(row);
+  const Passes<DT, NT> passes(row);
   RowSettings st;
   st.T = s.temperature ? s.temperature[b] : 1.f;
   st.k = s.top_k ? s.top_k[b] : 0;
@@ -945,7 +991,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(
   st.mp = s.min_p ? s.min_p[b] : 0.f;
   st.u = u[r];
   const float mx = passes.max_value();
-  float M = block_max_f32(mx, sh);
+  float M = block_max_f32<Shared<DT, NT>, NT>(mx, sh);
   if (M == 0.f) M = 0.f;   // not -0
   Drawn d;
   bool done = false;
@@ -953,26 +999,48 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(
     if (!(st.T > 0.f)) {
       if (tid == 0) sh.n = 0xFFFFFFFFu;
       __syncthreads();
-      passes.at_least(M, [&](float, int e) { atomicMin(&sh.n, (uint32_t)e); });
+      passes.between(mx, M, INFINITY, sh, [&](float, int e) { atomicMin(&sh.n, (uint32_t)e); });
       __syncthreads();
       d = {(int)sh.n, 1.f};
       done = true;
-    } else if constexpr (DT == TAPS_BF16) {
-      done = sample_counted<DT>(passes, mx, M, st, sh, &d);
-    } else if (st.few() || st.cut_by_min_p()) {
-      done = sample_listed<DT>(passes, mx, M, st, sh, &d);
-    } else if (st.k <= 0 || st.k >= vocab) {
-      done = sample_binned<DT>(passes, M, st, sh, &d);
+    } else {
+      const Weights w{M, value_key(__float_as_uint(M)), 1.4426950408889634074 / (double)st.T};
+      if (st.few() || st.cut_by_min_p())
+        done = sample_listed<DT, NT>(passes, mx, w, st, sh, &d);
+      if constexpr (DT == TAPS_BF16) {
+        if (!done) {
+          __syncthreads();
+          done = sample_counted<DT, NT>(passes, mx, w, st, sh, &d);
+        }
+      } else if (!done && (st.k <= 0 || st.k >= vocab)) {
+        __syncthreads();
+        done = sample_binned<DT, NT>(passes, mx, w, st, sh, &d);
+      }
     }
   }
   if (!done) {   // uniform
     __syncthreads();
-    d = sample_general<DT>(row, st, sh);
+    d = sample_general<DT, NT>(row, st, sh);
   }
   if (tid == 0) {
     tokens[r] = d.token;
     if (probs) probs[r] = d.prob;
   }
+}
+
+template <int DT>
+hipError_t launch_dt(const void* logits, int64_t row_bytes, int budget, int vocab, int rows,
+                     const int32_t* n_nodes, const Settings& st, const float* u, int32_t* tokens,
+                     float* probs, hipStream_t stream) {
+  // one row per CU: all its waves; more rows: two workgroups share a CU, one's passes over
+  // memory beside the other's work in LDS
+  if (rows <= 256)
+    sample_kernel<DT, 1024><<<(unsigned)rows, 1024, 0, stream>>>(logits, row_bytes, budget, vocab,
+                                                                 n_nodes, st, u, tokens, probs);
+  else
+    sample_kernel<DT, 512><<<(unsigned)rows, 512, 0, stream>>>(logits, row_bytes, budget, vocab,
+                                                               n_nodes, st, u, tokens, probs);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -982,14 +1050,11 @@ hipError_t launch_sample(const void* logits, int64_t row_bytes, int batch, int b
                          const float* u, int32_t* tokens, float* probs, hipStream_t stream) {
   if (batch <= 0) return hipSuccess;
   const Settings st{s.temperature, s.top_p, s.min_p, s.top_k};
-  const unsigned rows = (unsigned)(batch * budget);
-  if (dtype == TAPS_BF16)
-    sample_kernel<TAPS_BF16><<<rows, kThreads, 0, stream>>>(logits, row_bytes, budget, vocab,
-                                                            n_nodes, st, u, tokens, probs);
-  else
-    sample_kernel<TAPS_FP32><<<rows, kThreads, 0, stream>>>(logits, row_bytes, budget, vocab,
-                                                            n_nodes, st, u, tokens, probs);
-  return hipGetLastError();
+  const int rows = batch * budget;
+  return dtype == TAPS_BF16 ? launch_dt<TAPS_BF16>(logits, row_bytes, budget, vocab, rows, n_nodes,
+                                                   st, u, tokens, probs, stream)
+                            : launch_dt<TAPS_FP32>(logits, row_bytes, budget, vocab, rows, n_nodes,
+                                                   st, u, tokens, probs, stream);
 }
 
 }  // namespace taps
