@@ -16,27 +16,35 @@ namespace taps {
 
 namespace {
 
-constexpr double kOne = 8796093022208.0;   // 2^43, the weight of the largest value
-
-// 2^y for -45 < y <= 0: y = k + r, |r| <= 1/2, e^(r ln 2) by its Taylor series to the 12th power
+// 2^y for -45 <= y <= 0: y = k + r, |r| <= 1/2, e^(r ln 2) by its Taylor series to the 12th power
 // (remainder below 2^-52), exact at y = 0.
+// (The coefficients are pinned to scalar registers: from vector ones every product copied its own.)
+__device__ inline double scalar(double c) {
+  asm("" : "+s"(c));
+  return c;
+}
 __device__ inline double exp2_neg(double y) {
   const double k = rint(y);
   const double t = (y - k) * 0.69314718055994530942;
   double p = 1.0 / 479001600.0;
-  p = fma(p, t, 1.0 / 39916800.0);
-  p = fma(p, t, 1.0 / 3628800.0);
-  p = fma(p, t, 1.0 / 362880.0);
-  p = fma(p, t, 1.0 / 40320.0);
-  p = fma(p, t, 1.0 / 5040.0);
-  p = fma(p, t, 1.0 / 720.0);
-  p = fma(p, t, 1.0 / 120.0);
-  p = fma(p, t, 1.0 / 24.0);
-  p = fma(p, t, 1.0 / 6.0);
+  p = fma(p, t, scalar(1.0 / 39916800.0));
+  p = fma(p, t, scalar(1.0 / 3628800.0));
+  p = fma(p, t, scalar(1.0 / 362880.0));
+  p = fma(p, t, scalar(1.0 / 40320.0));
+  p = fma(p, t, scalar(1.0 / 5040.0));
+  p = fma(p, t, scalar(1.0 / 720.0));
+  p = fma(p, t, scalar(1.0 / 120.0));
+  p = fma(p, t, scalar(1.0 / 24.0));
+  p = fma(p, t, scalar(1.0 / 6.0));
   p = fma(p, t, 0.5);
   p = fma(p, t, 1.0);
   p = fma(p, t, 1.0);
   return ldexp(p, (int)k);
+}
+// x in [0, 1] in units of 2^-43, rounded: doubles between 512 and 1024 have steps of 2^-43, so
+// the low bits of 512 + x are that integer
+__device__ inline uint64_t fixed43(double x512) {
+  return (uint64_t)(__double_as_longlong(x512) - __double_as_longlong(512.0));
 }
 
 // the float whose value_key is `key`
@@ -52,9 +60,9 @@ struct Weights {
   __device__ inline double log2w(uint32_t k) const {
     return k == key ? 0.0 : ((double)key_value(k) - (double)top) * scale;
   }
-  __device__ inline uint64_t operator()(uint32_t k) const {   // k != 0 (not NaN)
-    const double y = log2w(k);
-    return y > -44.5 ? (uint64_t)rint(exp2_neg(y) * kOne) : 0ull;
+  // (no branch: several weights of a thread are evaluated side by side; NaN counts as -45)
+  __device__ inline uint64_t operator()(uint32_t k) const {
+    return fixed43(512.0 + exp2_neg(fmax(log2w(k), -45.0)));
   }
 };
 
@@ -101,7 +109,7 @@ struct GeneralScratch {
   uint64_t mass[kBins];
   uint32_t count[kBins];
 };
-struct ListScratch {
+struct alignas(16) ListScratch {
   uint64_t list[kList], sorted[kList], cum[kList];
 };
 struct CountScratch {
@@ -338,6 +346,14 @@ struct RowSettings {
   }
 };
 
+// a / b where the quotient is below 2^31
+__device__ inline uint32_t quotient(uint64_t a, uint64_t b) {
+  uint32_t q = (uint32_t)((double)a / (double)b);
+  if (q * b > a) --q;
+  else if ((q + 1ull) * b <= a) ++q;
+  return q;
+}
+
 struct Drawn {
   int token;
   float prob;
@@ -401,9 +417,21 @@ __device__ __attribute__((noinline)) Drawn sample_general(const Row<DT> row, con
           (float)((double)W / (double)S)};
 }
 
+constexpr uint32_t kLowest16 = 0x007Fu;   // the key of -inf; smaller ones are NaN
+__device__ inline uint32_t key16(float x) { return value_key(__float_as_uint(x)) >> 16; }
+// the whole key of a 16-bit one: it ends in zeros, or ones where the value is negative
+__device__ inline uint32_t key32(uint32_t k) { return (k << 16) | ((k & 0x8000u) ? 0u : 0xFFFFu); }
+// the 16-bit keys of both halves: sign ? ~bits : bits | 0x8000
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ inline u16x2 keys16(uint32_t w) {
+  const uint32_t sign = __builtin_bit_cast(uint32_t, (s16x2)(__builtin_bit_cast(s16x2, w) >> 15));
+  return __builtin_bit_cast(u16x2, w ^ (sign | 0x80008000u));
+}
+
 // Passes over a row: its whole aligned 16-byte units, kAhead of them in flight per thread, and
-// the elements of its unaligned ends, one per thread.  Places without an element are NaN, which
-// no pass counts.  A row is read from HBM once; the passes after the first find it in the
+// the elements of its unaligned ends, one per thread.  Places without an element are negative
+// NaN, whose key is the smallest and which no pass counts.  A row is read from HBM once; the passes after the first find it in the
 // caches, and most of them read only the units of the threads that hold values above a bound.
 // (Registers for a row of 150000 bf16 values leave too few for the passes: at every share kept
 // there, the compiler spilled as much.)
@@ -412,7 +440,7 @@ constexpr int kAhead = 10;
 template <int DT, int NT>
 struct Passes {
   static constexpr int U = Row<DT>::U;
-  static constexpr uint32_t kNone = DT == TAPS_BF16 ? 0x7FC07FC0u : 0x7FC00000u;
+  static constexpr uint32_t kNone = 0xFFFFFFFFu;
   const Row<DT>& row;
   int head, full;      // elements before the first whole unit, whole units
 
@@ -425,16 +453,19 @@ struct Passes {
   template <class F>
   __device__ __attribute__((always_inline)) inline void units(F&& f) const {
     const int tid = threadIdx.x;
+    const uint32_t last = (uint32_t)(full - 1) * 16u;   // a row is below 2^32 bytes
+    const char* const p = first();
     for (int u0 = 0; u0 < full; u0 += kAhead * NT) {
       uint4 x[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j)
-        x[j] = *(const uint4*)(first() + (int64_t)min(u0 + j * NT + tid, full - 1) * 16);
+        if (u0 + j * NT < full)   // uniform
+          x[j] = *(const uint4*)(p + min((uint32_t)(u0 + j * NT + tid) * 16u, last));
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
+        if (u0 + j * NT >= full) break;
         const int u = u0 + j * NT + tid;
-        if (u0 + j * NT >= full) break;   // uniform
-        if (u >= full) x[j] = make_uint4(kNone, kNone, kNone, kNone);
+        if (u0 + (j + 1) * NT > full && u >= full) x[j] = make_uint4(kNone, kNone, kNone, kNone);
         f(x[j], u * U + head);
       }
     }
@@ -449,22 +480,35 @@ struct Passes {
     if (tid >= U && rest + tid - U < row.vocab) e = rest + tid - U;   // fewer than U of them
     uint32_t b = kNone;
     if (e >= 0)
-      b = DT == TAPS_BF16 ? 0x7FC00000u | ((const uint16_t*)row.base)[e]
+      b = DT == TAPS_BF16 ? 0xFFFF0000u | ((const uint16_t*)row.base)[e]
                           : ((const uint32_t*)row.base)[e];
     f(make_uint4(b, kNone, kNone, kNone), max(e, 0));
   }
-  // the largest value of this thread's units (NaN left out; -inf where there is none)
+  // the largest value of this thread's units (NaN left out; -inf where there is none).  bf16:
+  // the largest 16-bit key, two at a time (three instructions; as floats the halves would be
+  // unpacked and made quiet first, five); a positive NaN in any unit sends the wave through the
+  // floats after all.
   __device__ __attribute__((always_inline)) inline float max_value() const {
+    if constexpr (DT == TAPS_BF16) {
+      u16x2 mk = {0, 0};
+      units([&](const uint4& w, int) {
+        mk = __builtin_elementwise_max(
+            mk, __builtin_elementwise_max(__builtin_elementwise_max(keys16(w.x), keys16(w.y)),
+                                          __builtin_elementwise_max(keys16(w.z), keys16(w.w))));
+      });
+      const uint32_t k = max((uint32_t)mk[0], (uint32_t)mk[1]);
+      // +inf's key is 0xFF80; -inf's 0x7F (smaller: NaN or nothing)
+      if (!__syncthreads_or(k > 0xFF80u)) return k > 0x7Fu ? key_value(key32(k)) : -INFINITY;
+    }
     float mx = -INFINITY;
     units([&](const uint4& w, int) {
       const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+      float t[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (DT == TAPS_BF16)
-          mx = fmaxf(mx, fmaxf(__uint_as_float(ww[q] << 16), __uint_as_float(ww[q] & 0xFFFF0000u)));
-        else
-          mx = fmaxf(mx, __uint_as_float(ww[q]));
-      }
+      for (int q = 0; q < 4; ++q)
+        t[q] = DT == TAPS_BF16 ? fmaxf(__uint_as_float(ww[q] << 16), __uint_as_float(ww[q] & 0xFFFF0000u))
+                               : __uint_as_float(ww[q]);
+      mx = fmaxf(mx, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
     });
     return mx;
   }
@@ -490,14 +534,20 @@ struct Passes {
     __syncthreads();
     auto one = [&](const uint4& w, int e0) {
       const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+      float x[U];
+      bool in[U], any = false;   // one branch for the unit, which mostly holds none
 #pragma unroll
       for (int q = 0; q < U; ++q) {
-        const uint32_t b = DT == TAPS_BF16
-                               ? ((q & 1) ? ww[q >> 1] & 0xFFFF0000u : ww[q >> 1] << 16)
-                               : ww[q & 3];
-        const float x = __uint_as_float(b);
-        if (x >= lo && x <= hi) f(x, e0 + q);
+        x[q] = __uint_as_float(DT == TAPS_BF16
+                                   ? ((q & 1) ? ww[q >> 1] & 0xFFFF0000u : ww[q >> 1] << 16)
+                                   : ww[q & 3]);
+        in[q] = x[q] >= lo && x[q] <= hi;
+        any |= in[q];
       }
+      if (!any) return;
+#pragma unroll
+      for (int q = 0; q < U; ++q)
+        if (in[q]) f(x[q], e0 + q);
     };
     const int n = (int)sh.n_hot, per = (full + NT - 1) / NT;
     if (2 * n > NT) {
@@ -548,8 +598,15 @@ __device__ inline void sort_list(uint32_t n, Shared<DT, NT>& sh) {
   ListScratch& ls = sh.u.l;
   for (uint32_t i = threadIdx.x; i < n; i += NT) {
     const uint64_t mine = ls.list[i];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) rank += ls.list[j] > mine ? 1u : 0u;
+    uint32_t rank = 0, j = 0;
+    for (; j + 8 <= n; j += 8) {   // eight at a time, every lane the same ones
+      ulonglong2 v[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[t] = *(const ulonglong2*)&ls.list[j + 2 * t];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) rank += (v[t].x > mine ? 1u : 0u) + (v[t].y > mine ? 1u : 0u);
+    }
+    for (; j < n; ++j) rank += ls.list[j] > mine ? 1u : 0u;
     ls.sorted[rank] = mine;
   }
   __syncthreads();
@@ -598,11 +655,9 @@ __device__ inline uint32_t count_list(uint32_t n, Shared<DT, NT>& sh, F&& in) {
   return (uint32_t)block_sum_u64<Shared<DT, NT>, NT>(c, sh);
 }
 
-// A float bound rounded down by more than the arithmetic can be off; M where it is not a number
-// (an infinite maximum)
+// A float bound rounded down by more than the arithmetic can be off
 __device__ inline float bound_below(double x, float M) {
-  const float b = (float)(x - 1e-6 * (fabs(x) + fabs((double)M)));
-  return b == b ? b : M;
+  return (float)(x - 1e-6 * (fabs(x) + fabs((double)M)));
 }
 
 // A small top_k, or min_p: the elements above a bound, ranked.  False: more than kList of them.
@@ -612,7 +667,8 @@ __device__ __attribute__((always_inline)) inline bool sample_listed(
     Shared<DT, NT>& sh, Drawn* out) {
   const double least = st.least();
   float thr = -INFINITY;
-  if (st.cut_by_min_p()) thr = bound_below((double)w.top + least / w.scale, w.top);
+  if (st.cut_by_min_p() && w.scale > 0.0)   // (an infinite temperature: all weights are equal)
+    thr = w.top == INFINITY ? w.top : bound_below((double)w.top + least / w.scale, w.top);
   if (st.few()) {
     const uint32_t key = top_k_bound<DT, NT>(mx, st.k, sh);
     if (key) thr = fmaxf(thr, key_value(key));
@@ -648,11 +704,6 @@ __device__ __attribute__((always_inline)) inline bool sample_listed(
 // value that occurs, none per element, and a crossing is exact at once.  Returns false where
 // the window is too wide or a value occurs 65536 times.
 // 16 bits per count let two workgroups share a CU's LDS.
-constexpr uint32_t kLowest16 = 0x007Fu;   // the key of -inf; smaller ones are NaN
-__device__ inline uint32_t key16(float x) { return value_key(__float_as_uint(x)) >> 16; }
-// the whole key of a 16-bit one: it ends in zeros, or ones where the value is negative
-__device__ inline uint32_t key32(uint32_t k) { return (k << 16) | ((k & 0x8000u) ? 0u : 0xFFFFu); }
-
 template <int DT, int NT>
 __device__ __attribute__((always_inline)) inline bool sample_counted(
     const Passes<DT, NT>& passes, float mx, const Weights& w, const RowSettings& st,
@@ -676,20 +727,16 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
   uint32_t in_window = 0;   // of the wave
   passes.units([&](const uint4& v, int) {
     const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
-    typedef short s16x2 __attribute__((ext_vector_type(2)));
-    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     const u16x2 top = {(unsigned short)kM, (unsigned short)kM};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      // both halves: key = sign ? ~bits : bits | 0x8000; NaN keys fall outside the window
-      const s16x2 b = __builtin_bit_cast(s16x2, ww[q]);
-      const uint32_t sign = __builtin_bit_cast(uint32_t, (s16x2)(b >> 15));
-      const u16x2 key = __builtin_bit_cast(u16x2, ww[q] ^ (sign | 0x80008000u));
-      const uint32_t idx = __builtin_bit_cast(uint32_t, (u16x2)(top - key));
+      // NaN keys fall outside the window
+      const uint32_t idx = __builtin_bit_cast(uint32_t, (u16x2)(top - keys16(ww[q])));
       const uint32_t i0 = idx & 0xFFFFu, i1 = idx >> 16;
       in_window += __popcll(__ballot(i0 < Wn)) + __popcll(__ballot(i1 < Wn));
-      if (i0 < Wn) atomicAdd(&cs.count[i0 >> 1], 1u + (i0 & 1u) * 0xFFFFu);
-      if (i1 < Wn) atomicAdd(&cs.count[i1 >> 1], 1u + (i1 & 1u) * 0xFFFFu);
+      // a shift counts its amount's low five bits only: 16 (i & 1)
+      if (i0 < Wn) atomicAdd(&cs.count[i0 >> 1], 1u << ((i0 << 4) & 31u));
+      if (i1 < Wn) atomicAdd(&cs.count[i1 >> 1], 1u << ((i1 << 4) & 31u));
     }
   });
   __syncthreads();
@@ -710,7 +757,7 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
     uint32_t c[4];
     uint64_t W[4], m[4];
   };
-  auto four = [&](int r, bool by_count) -> Four {
+  auto four = [&](int r) -> Four {
     const uint2 p = ((const uint2*)cs.count)[r * kWave + lane];
     Four f;
     f.c[0] = p.x & 0xFFFFu;
@@ -719,8 +766,8 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
     f.c[3] = p.y >> 16;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      f.W[j] = f.c[j] ? w(key32(kM - (uint32_t)(r * kRun + 4 * lane + j))) : 0ull;
-      f.m[j] = by_count ? (uint64_t)f.c[j] : f.W[j] * f.c[j];
+      f.W[j] = w(key32(kM - (uint32_t)(r * kRun + 4 * lane + j)));
+      f.m[j] = f.W[j] * f.c[j];
     }
     return f;
   };
@@ -729,7 +776,7 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
     uint64_t m = 0;
     uint32_t n = 0;
     if (__ballot((p.x | p.y) != 0u)) {
-      const Four f = four(r, false);
+      const Four f = four(r);
       m = wave_sum_u64(f.m[0] + f.m[1] + f.m[2] + f.m[3]);
       n = __builtin_amdgcn_readlane(wave_scan_u32(f.c[0] + f.c[1] + f.c[2] + f.c[3]), kWave - 1);
     }
@@ -749,9 +796,10 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
 
   struct Cross {
     uint32_t pos, ties, nth;     // window position, elements there, the crossing one among them
-    uint64_t above, W;           // sum (count) before them, weight of each
+    uint64_t through, W;         // sum with the crossing one, weight of each
   };
-  // where the running sum (count) first exceeds target
+  // Where the running sum (count) first exceeds target.  One wave looks into the run (all of
+  // them would share its evaluation of 256 weights' worth of vector time).
   auto crossing = [&](uint64_t target, bool by_count) -> Cross {
     if (tid < runs) {
       const uint64_t a = by_count ? cs.num[tid] : cs.mass[tid];
@@ -760,34 +808,46 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
       if (a <= target && target < b) sh.out32[0] = (uint32_t)tid;
     }
     __syncthreads();
-    const int r = __builtin_amdgcn_readfirstlane(sh.out32[0]);
-    __syncthreads();
-    const Four f = four(r, by_count);
-    const uint64_t mine = f.m[0] + f.m[1] + f.m[2] + f.m[3];
-    const uint64_t incl = (by_count ? (uint64_t)cs.num[r] : cs.mass[r]) + wave_scan_u64(mine);
-    const int l = __ffsll((long long)__ballot(incl > target)) - 1;
-    uint64_t above = incl - mine, W = f.W[0];
-    uint32_t j = 0, ties = f.c[0];
+    if (wave == 0) {
+      const int r = __builtin_amdgcn_readfirstlane(sh.out32[0]);
+      const Four f = four(r);
+      uint64_t m[4];   // what is counted
 #pragma unroll
-    for (int t = 0; t < 3; ++t)
-      if (j == (uint32_t)t && above + f.m[t] <= target) {
-        above += f.m[t];
-        j = t + 1;
-        W = f.W[t + 1];
-        ties = f.c[t + 1];
+      for (int j = 0; j < 4; ++j) m[j] = by_count ? (uint64_t)f.c[j] : f.m[j];
+      const uint64_t mine = m[0] + m[1] + m[2] + m[3];
+      const uint64_t incl = (by_count ? (uint64_t)cs.num[r] : cs.mass[r]) + wave_scan_u64(mine);
+      const uint64_t sums = by_count ? wave_scan_u64(f.m[0] + f.m[1] + f.m[2] + f.m[3]) : 0ull;
+      const int l = __ffsll((long long)__ballot(incl > target)) - 1;
+      if (lane == l) {
+        uint64_t above = incl - mine, sum = cs.mass[r] + sums - (f.m[0] + f.m[1] + f.m[2] + f.m[3]);
+        uint64_t W = f.W[0];
+        uint32_t j = 0, ties = f.c[0];
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+          if (j == (uint32_t)t && above + m[t] <= target) {
+            above += m[t];
+            sum += f.m[t];
+            j = t + 1;
+            W = f.W[t + 1];
+            ties = f.c[t + 1];
+          }
+        const uint32_t nth = by_count ? (uint32_t)(target - above) : quotient(target - above, W);
+        sh.out32[1] = (uint32_t)(r * kRun + 4 * lane) + j;
+        sh.out32[2] = ties;
+        sh.out32[3] = nth;
+        sh.out64[0] = (by_count ? sum : above) + (nth + 1ull) * W;
+        sh.out64[1] = W;
       }
-    Cross x;
-    x.pos = __builtin_amdgcn_readlane((uint32_t)(r * kRun + 4 * lane) + j, l);
-    x.ties = __builtin_amdgcn_readlane(ties, l);
-    x.W = lane_u64(W, l);
-    x.above = lane_u64(above, l);
-    x.nth = by_count ? (uint32_t)(target - x.above) : (uint32_t)((target - x.above) / x.W);
+    }
+    __syncthreads();
+    const Cross x{sh.out32[1], sh.out32[2], sh.out32[3], sh.out64[0], sh.out64[1]};
+    __syncthreads();
     return x;
   };
   // sum of the weights before window position i
   auto sum_before = [&](uint32_t i) -> uint64_t {
     const int r = (int)(i / kRun);
-    const Four f = four(r, false);
+    const Four f = four(r);
     uint64_t m = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) m += (uint32_t)(r * kRun + 4 * lane + j) < i ? f.m[j] : 0ull;
@@ -796,12 +856,10 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
 
   uint64_t kept = S;
   if (st.k > 0 && (uint64_t)st.k < have) {
-    const Cross c = crossing((uint64_t)(st.k - 1), true);
-    kept = sum_before(c.pos) + (uint64_t)(c.nth + 1u) * c.W;
+    kept = crossing((uint64_t)(st.k - 1), true).through;
   }
   if (st.p < 1.f) {
-    const Cross c = crossing(top_p_sum(st.p, kept) - 1, false);
-    kept = c.above + (uint64_t)(c.nth + 1u) * c.W;
+    kept = crossing(top_p_sum(st.p, kept) - 1, false).through;
   }
   if (st.mp > 0.f) {
     const double least = st.least();
@@ -838,7 +896,8 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
 // octave.  Weight 2^-(z / 32), z = 32 log2(e) (M - x) / T, is the bin's 2^-(b / 32), b = floor
 // z, times a factor 2^-((z - b) / 32) from a short series; a bin adds up its factors (integers
 // of 2^-43), and its sum is that times 2^-(b / 32), rounded down.  The bin where a running sum
-// passes its target is then ranked one by one.  False: more than kList elements in it.
+// passes its target is then ranked one by one.  False: more than kList elements in it, or an
+// infinite maximum or temperature.
 template <int DT, int NT>
 __device__ __attribute__((always_inline)) inline bool sample_binned(
     const Passes<DT, NT>& passes, float mx, const Weights& w, const RowSettings& st,
@@ -846,36 +905,40 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   const int tid = threadIdx.x;
   BinScratch& bs = sh.u.b;
   const float M = w.top;
+  // differences to an infinite maximum are not 0 even for its equals, and at an infinite
+  // temperature all weights are equal
+  if (M == INFINITY || !(w.scale > 0.0)) return false;
   const double scale = kPerOctave * w.scale;
   for (int i = tid; i < kWeightBins; i += NT) bs.mass[i] = 0ull;
   __syncthreads();
-  // an infinite maximum: its equals have depth 0, not NaN
-  const bool inf = M == INFINITY;
-  auto depth = [&](float x) -> double {
-    const double d = (double)M - (double)x;
-    return (inf && x == M ? 0.0 : d) * scale;
-  };
-  // 512 + the factor: the double's low bits are the factor in units of 2^-43, rounded
+  auto depth = [&](float x) -> double { return ((double)M - (double)x) * scale; };
   auto factor = [&](double z) -> uint64_t {
     constexpr double c = -0.69314718055994530942 / kPerOctave;
     const double t = __builtin_amdgcn_fract(z);
-    double p = c * c * c * c * c * c / 720.0;
-    p = fma(p, t, c * c * c * c * c / 120.0);
-    p = fma(p, t, c * c * c * c / 24.0);
-    p = fma(p, t, c * c * c / 6.0);
-    p = fma(p, t, c * c * 0.5);
-    p = fma(p, t, c);
-    p = fma(p, t, 513.0);
-    return (uint64_t)(__double_as_longlong(p) - __double_as_longlong(512.0));
+    double p = scalar(c * c * c * c * c * c / 720.0);
+    p = fma(p, t, scalar(c * c * c * c * c / 120.0));
+    p = fma(p, t, scalar(c * c * c * c / 24.0));
+    p = fma(p, t, scalar(c * c * c / 6.0));
+    p = fma(p, t, scalar(c * c * 0.5));
+    p = fma(p, t, scalar(c));
+    return fixed43(fma(p, t, scalar(513.0)));
   };
   passes.units([&](const uint4& v, int) {
     const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
+    double z[4];
+    uint64_t f[4];
+    // the four series side by side; elements past the last bin (or NaN) add nothing
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const double z = depth(__uint_as_float(ww[q]));
-      if (z < (double)kWeightBins)
-        atomicAdd((unsigned long long*)&bs.mass[(int)z], (unsigned long long)factor(z));
+      z[q] = depth(__uint_as_float(ww[q]));
+      f[q] = factor(z[q]);
     }
+    // (kept out of the branches, where each would wait for its own chain of products)
+    asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]));
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (z[q] < (double)kWeightBins)
+        atomicAdd((unsigned long long*)&bs.mass[(int)z[q]], (unsigned long long)f[q]);
   });
   __syncthreads();
   auto bin_scale = [&](int b) -> double { return exp2_neg(-(double)b / kPerOctave); };
@@ -909,14 +972,12 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     if (tid == 0) sh.n = 0u;
     __syncthreads();
     const float lo = bound_below((double)M - (double)(bin + 1) / scale, M);
-    const float hi = -bound_below((double)bin / scale - (double)M, -M);
+    const float hi = -bound_below((double)bin / scale - (double)M, M);
+    // (the bounds may let neighbours in: they add nothing to the running sums)
     passes.between(mx, lo, hi, sh, [&](float x, int e) {
-      const double z = depth(x);
-      if (z >= (double)bin && z < (double)(bin + 1)) {
-        const uint32_t i = atomicAdd(&sh.n, 1u);
-        if (i < (uint32_t)kList)
-          bs.l.list[i] = cand_key(value_key(__float_as_uint(x)), (uint32_t)e);
-      }
+      const uint32_t i = atomicAdd(&sh.n, 1u);
+      if (i < (uint32_t)kList)
+        bs.l.list[i] = cand_key(value_key(__float_as_uint(x)), (uint32_t)e);
     });
     __syncthreads();
     const uint32_t n = sh.n;
@@ -925,7 +986,11 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     const double bsc = bin_scale(bin);
     const uint64_t before = bs.before[bin];
     sum_list<DT, NT>(
-        n, sh, [&](uint32_t key) { return factor(depth(key_value(key))); },
+        n, sh,
+        [&](uint32_t key) {
+          const double z = depth(key_value(key));
+          return z >= (double)bin && z < (double)(bin + 1) ? factor(z) : 0ull;
+        },
         [&](uint64_t c) { return before + (uint64_t)(bsc * (double)c); });
     return n;
   };
