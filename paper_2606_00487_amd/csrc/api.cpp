@@ -565,8 +565,9 @@ taps_status decode_attn_paged_validate(int32_t batch, int32_t Hq, int32_t Hkv, i
   if ((int64_t)batch * Hkv > 65535 || Hq > 65535) return TAPS_ERR_UNSUPPORTED;
   // a tile's 32 rows are addressed with 32-bit offsets
   if ((int64_t)Hkv * head_dim * 4 > ((int64_t)1 << 24)) return TAPS_ERR_UNSUPPORTED;
-  const DecodePlan p = plan_decode(batch, Hq, Hkv, max_len);
-  if ((int64_t)batch * Hkv * p.splits * p.htiles > (int64_t)1 << 30) return TAPS_ERR_UNSUPPORTED;
+  // workgroups and units of 128 keys are counted in 32 bits
+  if ((int64_t)batch * Hkv * (Hq / Hkv / 16 + 1) > (int64_t)1 << 28) return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)batch * (max_len / 128 + 1) > (int64_t)1 << 30) return TAPS_ERR_UNSUPPORTED;
   return TAPS_OK;
 }
 
@@ -576,7 +577,7 @@ size_t decode_attn_paged_workspace_bytes(int32_t batch, int32_t Hq, int32_t Hkv,
           TAPS_OK ||
       batch == 0)
     return 0;
-  return decode_ws_bytes(plan_decode(batch, Hq, Hkv, max_len), batch, Hq, head_dim);
+  return decode_ws_bytes(plan_decode(batch, Hq, Hkv, max_len), batch, Hkv, head_dim);
 }
 
 taps_status decode_attn_paged(const void* Q, int64_t q_stride, const void* K_pages,
@@ -601,7 +602,7 @@ taps_status decode_attn_paged(const void* Q, int64_t q_stride, const void* K_pag
   if ((a16 & 15) != 0 || (((uintptr_t)block_table | (uintptr_t)kv_len) & 3) != 0)
     return TAPS_ERR_INVALID_ARG;
   const DecodePlan p = plan_decode(batch, Hq, Hkv, max_len);
-  const size_t need = decode_ws_bytes(p, batch, Hq, head_dim);
+  const size_t need = decode_ws_bytes(p, batch, Hkv, head_dim);
   if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return TAPS_ERR_WORKSPACE;
   const PagedKV pk{block_table, max_pages, num_pages, page_shift_of(page_rows)};
   return launch_decode(Q, q_stride, K_pages, V_pages, pk, kv_len, batch, Hq, Hkv, head_dim,

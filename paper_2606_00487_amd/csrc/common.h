@@ -160,14 +160,14 @@ hipError_t launch_append(const void* K_new, const void* V_new, int64_t k_stride_
                          int64_t v_stride_bytes, const int64_t* slots, int rows, int row_bytes,
                          void* K_pages, void* V_pages, int64_t pool_rows, hipStream_t s);
 
-// One new token per request over a paged cache: requests are cut into splits of split_len keys
+// One new token per request over a paged cache: all requests' keys, in units of 128, are cut into
+// equal parts, one per workgroup and KV head
 struct DecodePlan {
-  int split_len;   // a multiple of 128 (four waves' tiles)
-  int splits;      // splits that max_len keys need
-  int htiles;      // groups of 16 query heads of one KV head
+  int parts;    // per KV head and head tile; 0: one workgroup for each request of them
+  int htiles;   // groups of 16 query heads of one KV head
 };
 DecodePlan plan_decode(int batch, int Hq, int Hkv, int max_len);
-size_t decode_ws_bytes(const DecodePlan& p, int batch, int Hq, int head_dim);
+size_t decode_ws_bytes(const DecodePlan& p, int batch, int Hkv, int head_dim);
 // q_stride in elements; pools [num_pages][2^page_shift][Hkv][head_dim]
 hipError_t launch_decode(const void* Q, int64_t q_stride, const void* K, const void* V,
                          const PagedKV& pk, const int32_t* len, int batch, int Hq, int Hkv,

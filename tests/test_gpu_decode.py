@@ -213,3 +213,18 @@ def test_refuses_wrong_tensors():
         op(Q, K, V, table[:, :1].contiguous(), lens)        # too short for max_len
     with pytest.raises(taps.TapsError):
         taps.PagedDecodeAttention(2, 8, 3, 64, 50, 32)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("batch,lo,hi,Hq,Hkv,hd", [
+    (70, 0, 3000, 8, 2, 64), (130, 0, 900, 4, 1, 128), (9, 0, 2200, 34, 1, 64), (300, 1, 400, 2, 1, 64),
+    (64, 0, 1024, 16, 8, 64), (5, 3000, 3000, 8, 8, 128),
+])
+def test_equal_parts_of_ragged_batches(dtype, batch, lo, hi, Hq, Hkv, hd):
+    """Parts that end inside requests and span several, empty requests among them; more parts
+    than units; batches past 64 requests; one workgroup per request."""
+    rng = np.random.default_rng(batch)
+    lens = [int(x) for x in rng.integers(lo, hi + 1, batch)]
+    if lo == 0:
+        lens[0] = lens[-1] = lens[batch // 2] = lens[batch // 2 + 1] = 0
+    check(*case(batch + hi, lens, Hq, Hkv, hd, 64, dtype, max_len=hi + 5))
