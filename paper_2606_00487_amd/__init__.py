@@ -451,37 +451,44 @@ class PagedVerifyLayer:
         return self.Y
 
 
-def _here(name: str, *tensors):
-    """The calls below run on the current device: their tensors have to live there."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != dev:
-            raise ValueError(f"{name}: tensors on {t.device}, the current device is cuda:{dev}")
+# The calls below run on the current device and refuse tensors of another one (-1: no GPU).
+_current = _device or torch.cuda.current_device
 
 
-def _need_rows(t: torch.Tensor, name: str, dtype, inner):
-    """[rows, *inner] whose rows may be apart; returns the distance of rows in elements."""
+def _need_on(dev: int, t: torch.Tensor, name: str, dtype, shape=None):
+    """_need, and the tensor lives on the current device `dev`."""
+    if (t.dtype is dtype and t.get_device() == dev and (shape is None or t.shape == shape)
+            and t.is_contiguous()):
+        return
+    _need(t, name, dtype, shape)
+    raise ValueError(f"{name}: tensor on {t.device}, the current device is cuda:{dev}")
+
+
+def _need_rows(dev: int, t: torch.Tensor, name: str, dtype, inner, steps) -> int:
+    """[rows, *inner], each row contiguous (its strides are `steps`); the rows may be apart.
+    Returns their distance in elements."""
+    shape, strides = t.shape, t.stride()
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if not t.is_cuda:
-        raise TypeError(f"{name}: expected a GPU tensor")
-    if t.shape[1:] != inner:
-        raise ValueError(f"{name}: expected [rows, {', '.join(map(str, inner))}], "
-                         f"got {tuple(t.shape)}")
-    n = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size > 1 and stride != n:
-            raise ValueError(f"{name}: each row must be contiguous")
-        n *= size
-    return t.stride(0) if t.shape[0] > 1 else n
+    if t.get_device() != dev:
+        if not t.is_cuda:
+            raise TypeError(f"{name}: expected a GPU tensor")
+        raise ValueError(f"{name}: tensor on {t.device}, the current device is cuda:{dev}")
+    if shape[1:] != inner:
+        raise ValueError(f"{name}: expected [rows, {', '.join(map(str, inner))}], got {tuple(shape)}")
+    if strides[1:] != steps and any(n > 1 and a != b
+                                    for n, a, b in zip(inner, strides[1:], steps)):
+        raise ValueError(f"{name}: each row must be contiguous")
+    return strides[0] if shape[0] > 1 else inner[0] * steps[0]
 
 
-def _need_pools(K_pages, V_pages, dtype, page_rows, Hkv, hd):
-    _need(K_pages, "K_pages", dtype)
-    if K_pages.dim() != 4 or K_pages.shape[1:] != (page_rows, Hkv, hd):
-        raise ValueError(f"K_pages: expected [pages, {page_rows}, {Hkv}, {hd}], "
+def _need_pools(dev, K_pages, V_pages, dtype, page):
+    """page: (page_rows, Hkv, head_dim)"""
+    _need_on(dev, K_pages, "K_pages", dtype)
+    if K_pages.shape[1:] != page:
+        raise ValueError(f"K_pages: expected [pages, {page[0]}, {page[1]}, {page[2]}], "
                          f"got {tuple(K_pages.shape)}")
-    _need(V_pages, "V_pages", dtype, K_pages.shape)
+    _need_on(dev, V_pages, "V_pages", dtype, K_pages.shape)
 
 
 class PagedKVReserve:
@@ -499,21 +506,21 @@ class PagedKVReserve:
         Returns new tensors: pages held [batch], free pages [1], requests that are short [1]
         (all int32) and the slot map [batch, max_new] int64 (None without slot_map)."""
         batch, max_pages, num_pages, page_rows, max_new = self.shape
-        _need(block_table, "block_table", torch.int32, (batch, max_pages))
-        _need(held_pages, "held_pages", torch.int32, (batch,))
-        _need(ctx_len, "ctx_len", torch.int32, (batch,))
-        _need(n_new, "n_new", torch.int32, (batch,))
-        _need(free_pages, "free_pages", torch.int32, (num_pages,))
-        _need(n_free, "n_free", torch.int32, (1,))
-        _here("kv_reserve_paged", block_table, held_pages, ctx_len, n_new, free_pages, n_free)
-        held, free, short = (torch.empty_like(held_pages), torch.empty_like(n_free),
-                             torch.empty_like(n_free))
-        slots = torch.empty(batch, max_new, dtype=torch.int64,
-                            device=block_table.device) if self.slot_map else None
+        dev = _current()
+        _need_on(dev, block_table, "block_table", torch.int32, (batch, max_pages))
+        _need_on(dev, held_pages, "held_pages", torch.int32, (batch,))
+        _need_on(dev, ctx_len, "ctx_len", torch.int32, (batch,))
+        _need_on(dev, n_new, "n_new", torch.int32, (batch,))
+        _need_on(dev, free_pages, "free_pages", torch.int32, (num_pages,))
+        _need_on(dev, n_free, "n_free", torch.int32, (1,))
+        counts = block_table.new_empty(batch + 2)   # one allocation for the three
+        held, free, short = counts.split_with_sizes((batch, 1, 1))
+        slots = block_table.new_empty((batch, max_new), dtype=torch.int64) if self.slot_map else None
+        at = counts.data_ptr()
         _lib.check(self.lib, "kv_reserve_paged", self.lib.kv_reserve_paged(
             _ptr(block_table), max_pages, _ptr(held_pages), _ptr(ctx_len), _ptr(n_new), batch,
-            max_new, _ptr(free_pages), _ptr(n_free), num_pages, page_rows, _ptr(held), _ptr(free),
-            _ptr(short), _ptr(slots), _stream()))
+            max_new, _ptr(free_pages), _ptr(n_free), num_pages, page_rows, at, at + 4 * batch,
+            at + 4 * batch + 4, _ptr(slots), _stream()))
         return held, free, short, slots
 
 
@@ -523,21 +530,23 @@ class PagedKVAppend:
     def __init__(self, Hkv, head_dim, page_rows, dtype=BF16):
         self.lib = load()
         self.shape = (Hkv, head_dim, int(page_rows), dtype)
+        self._page = (int(page_rows), Hkv, head_dim)
+        self._row, self._steps = (Hkv, head_dim), (head_dim, 1)
 
     def __call__(self, K_new, V_new, slot_map, K_pages, V_pages):
         """K_new, V_new: [rows, Hkv, head_dim], rows contiguous in themselves (slices of a fused
         projection's rows are fine).  slot_map: int64 of `rows` entries in any shape."""
         Hkv, hd, page_rows, dtype = self.shape
         tdt = _TORCH_DT[dtype]
-        ks = _need_rows(K_new, "K_new", tdt, (Hkv, hd))
-        vs = _need_rows(V_new, "V_new", tdt, (Hkv, hd))
+        dev = _current()
+        ks = _need_rows(dev, K_new, "K_new", tdt, self._row, self._steps)
+        vs = _need_rows(dev, V_new, "V_new", tdt, self._row, self._steps)
         rows = K_new.shape[0]
-        _need(slot_map, "slot_map", torch.int64)
+        _need_on(dev, slot_map, "slot_map", torch.int64)
         if V_new.shape[0] != rows or slot_map.numel() != rows:
             raise ValueError(f"K_new has {rows} rows, V_new {V_new.shape[0]}, slot_map "
                              f"{slot_map.numel()} entries")
-        _need_pools(K_pages, V_pages, tdt, page_rows, Hkv, hd)
-        _here("kv_append_paged", K_new, V_new, slot_map, K_pages, V_pages)
+        _need_pools(dev, K_pages, V_pages, tdt, self._page)
         _lib.check(self.lib, "kv_append_paged", self.lib.kv_append_paged(
             _ptr(K_new), _ptr(V_new), ks, vs, _ptr(slot_map), rows, Hkv, hd, dtype,
             _ptr(K_pages), _ptr(V_pages), K_pages.shape[0], page_rows, _stream()))
@@ -554,25 +563,30 @@ class PagedDecodeAttention:
         _lib.check(self.lib, "decode_attn_paged_validate",
                    self.lib.decode_attn_paged_validate(*self.shape, self.scale))
         self.ws_bytes = self.lib.decode_attn_paged_workspace_bytes(*self.shape)
+        self._page = (int(page_rows), Hkv, head_dim)
+        self._row, self._steps = (Hq, head_dim), (head_dim, 1)
 
     def __call__(self, Q, K_pages, V_pages, block_table, kv_len, out=None):
         """Q: [batch, Hq, head_dim], requests may be apart.  Each call has scratch of its own
         (from torch's allocator, on the current stream), so calls may overlap."""
         batch, Hq, Hkv, hd, max_len, page_rows, dtype = self.shape
         tdt = _TORCH_DT[dtype]
-        qs = _need_rows(Q, "Q", tdt, (Hq, hd))
+        dev = _current()
+        qs = _need_rows(dev, Q, "Q", tdt, self._row, self._steps)
         if Q.shape[0] != batch:
             raise ValueError(f"Q: expected {batch} requests, got {Q.shape[0]}")
-        _need_pools(K_pages, V_pages, tdt, page_rows, Hkv, hd)
-        _need(block_table, "block_table", torch.int32)
+        _need_pools(dev, K_pages, V_pages, tdt, self._page)
+        _need_on(dev, block_table, "block_table", torch.int32)
         if block_table.dim() != 2 or block_table.shape[0] != batch:
             raise ValueError(f"block_table: expected [{batch}, max_pages], "
                              f"got {tuple(block_table.shape)}")
-        _need(kv_len, "kv_len", torch.int32, (batch,))
-        O = out if out is not None else torch.empty(batch, Hq, hd, dtype=tdt, device=Q.device)
-        _need(O, "O", tdt, (batch, Hq, hd))
-        _here("decode_attn_paged", Q, K_pages, V_pages, block_table, kv_len, O)
-        ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=Q.device) if self.ws_bytes else None
+        _need_on(dev, kv_len, "kv_len", torch.int32, (batch,))
+        if out is None:
+            O = Q.new_empty((batch, Hq, hd))
+        else:
+            O = out
+            _need_on(dev, O, "O", tdt, (batch, Hq, hd))
+        ws = Q.new_empty(self.ws_bytes, dtype=torch.uint8) if self.ws_bytes else None
         _lib.check(self.lib, "decode_attn_paged", self.lib.decode_attn_paged(
             _ptr(Q), qs, _ptr(K_pages), _ptr(V_pages), K_pages.shape[0], page_rows,
             _ptr(block_table), block_table.shape[1], _ptr(kv_len), batch, Hq, Hkv, hd, max_len,
@@ -604,18 +618,21 @@ class TokenSampler:
                              f"got {tuple(logits.shape)}")
         if batch > 1 and budget > 1 and logits.stride(0) != budget * logits.stride(1):
             raise ValueError("logits: all rows must be the same distance apart")
-        rows = logits[0] if batch == 1 else logits[:, 0] if budget == 1 else logits.flatten(0, 1)
-        stride = _need_rows(rows, "logits", _TORCH_DT[dtype], (vocab,))
-        _need(u, "u", torch.float32, (batch, budget))
+        dev, tdt = _current(), _TORCH_DT[dtype]
+        if logits.is_contiguous():
+            _need_on(dev, logits, "logits", tdt)
+            stride = vocab
+        else:
+            rows = logits[0] if batch == 1 else logits[:, 0] if budget == 1 else logits.flatten(0, 1)
+            stride = _need_rows(dev, rows, "logits", tdt, (vocab,), (1,))
+        _need_on(dev, u, "u", torch.float32, (batch, budget))
         for t, name, dt in ((n_nodes, "n_nodes", torch.int32), (top_k, "top_k", torch.int32),
                             (temperature, "temperature", torch.float32),
                             (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
             if t is not None:
-                _need(t, name, dt, (batch,))
-        _here("taps_sample", logits, u, n_nodes, temperature, top_k, top_p, min_p)
-        tokens = torch.empty(batch, budget, dtype=torch.int32, device=u.device)
-        probs = torch.empty(batch, budget, dtype=torch.float32, device=u.device)
-        ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=u.device) if self.ws_bytes else None
+                _need_on(dev, t, name, dt, (batch,))
+        tokens, probs = u.new_empty((batch, budget), dtype=torch.int32), torch.empty_like(u)
+        ws = u.new_empty(self.ws_bytes, dtype=torch.uint8) if self.ws_bytes else None
         st = _lib.Sampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
         _lib.check(self.lib, "taps_sample", self.lib.taps_sample(
             _ptr(logits), stride, batch, budget, vocab, dtype, _ptr(n_nodes), ctypes.byref(st),

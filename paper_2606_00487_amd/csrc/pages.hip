@@ -20,11 +20,13 @@ namespace {
 // workgroup adds them up itself: one launch without a word between workgroups.  A take at or
 // above n_free is a page that this call pushes; it is read from the table row that gives it
 // (found by its place in the prefix sums), which no other workgroup writes, so that the kernel
-// nowhere reads what it writes.  Grid (requests, slices of the slot map).
-// Bound: latency (two dependent reads, a block scan, the page reads), then the slot map's
-// bytes.
+// nowhere reads what it writes.  Grid (runs of requests, slices of the slot map).
+// Bound: latency (two dependent reads, a block scan, the page reads): 7 us for 16 requests; then
+// the slot map's bytes.  (Looked up for every slot and not once a page: 27 us for 1024 requests
+// with 4096 slots each instead of 14.)
 constexpr int kReserveThreads = 256;
 constexpr int kSlotsPerGroup = 4096;   // slot map columns per workgroup
+constexpr int kReserveGroups = 512;    // runs of requests, at most
 
 struct Lengths {
   int held, ctx, nnew, want;
@@ -56,27 +58,35 @@ __device__ inline int64_t shfl_up_i64(int64_t v, int d) {
 
 __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(
     int32_t* __restrict__ table, int max_pages, const int32_t* __restrict__ held,
-    const int32_t* __restrict__ ctx, const int32_t* __restrict__ nnew, int batch,
+    const int32_t* __restrict__ ctx, const int32_t* __restrict__ nnew, int batch, int run,
     int32_t* __restrict__ stack, const int32_t* __restrict__ n_free, int num_pages, int shift,
     int max_new, int64_t* __restrict__ slots, int32_t* __restrict__ held_out,
     int32_t* __restrict__ n_free_out, int32_t* __restrict__ n_short) {
   __shared__ int64_t s_rel[kMaxReserveBatch];   // pages given back by the requests before
+  __shared__ int32_t s_want[kMaxReserveBatch];
+  __shared__ int64_t s_need[kMaxReserveBatch / kReserveGroups];   // pages taken before, this run
+  __shared__ int32_t s_page[kSlotsPerGroup / 32 + 1];             // a slice's pages
   __shared__ int64_t s_wave[2][kReserveThreads / kWave];
-  __shared__ int64_t s_need_before, s_taken;
+  __shared__ int64_t s_taken;
   __shared__ int s_unfit, s_unserved;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int run0 = blockIdx.x * run, run1 = min(run0 + run, batch);
   const int per = (batch + kReserveThreads - 1) / kReserveThreads;
   if (tid == 0) s_unfit = s_unserved = 0, s_taken = 0;
+  const int nf = min(max(*n_free, 0), num_pages);
 
   // this thread's requests [first, last): their sums, then their prefix over the block
   const int first = min(tid * per, batch), last = min(first + per, batch);
   int64_t rel = 0, need = 0;
   int unfit = 0;
+#pragma unroll 4
   for (int j = first; j < last; ++j) {
     const Lengths r = lengths(held, ctx, nnew, j, max_pages, shift, max_new);
     rel += r.rel;
     need += r.need;
     unfit += r.fits ? 0 : 1;
+    s_want[j] = r.want;
+    s_rel[j] = ((int64_t)r.rel << 32) | (uint32_t)r.need;   // both for the second loop
   }
   int64_t irel = rel, ineed = need;
 #pragma unroll
@@ -94,38 +104,34 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(
     need_all += s_wave[1][w];
   }
   if (unfit) atomicAdd(&s_unfit, unfit);
-  const int nf = min(max(*n_free, 0), num_pages);
   const int64_t size = min((int64_t)nf + rel_all, (int64_t)num_pages);
   {
     int64_t r0 = irel - rel, n0 = ineed - need, taken = 0;
     int unserved = 0;
     for (int j = first; j < last; ++j) {
-      const Lengths r = lengths(held, ctx, nnew, j, max_pages, shift, max_new);
+      const int64_t both = s_rel[j];
+      const int jneed = (int)(uint32_t)both;
       s_rel[j] = r0;
-      if (j == b) s_need_before = n0;
-      r0 += r.rel;
-      n0 += r.need;
-      if (r.need > 0) {
+      if (j >= run0 && j < run1) s_need[j - run0] = n0;
+      r0 += both >> 32;
+      n0 += jneed;
+      if (jneed > 0) {
         if (n0 <= size) taken = n0;
         else ++unserved;
       }
     }
     // the sums grow with the request: the last one served has taken the most
-    if (b == 0 && need_all > size) {
+    if (need_all > size) {
       if (taken) atomicMax((unsigned long long*)&s_taken, (unsigned long long)taken);
       if (unserved) atomicAdd(&s_unserved, unserved);
     }
   }
   __syncthreads();
-  if (b == 0 && blockIdx.y == 0 && tid == 0) {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) {
     *n_free_out = (int32_t)(size - (need_all > size ? s_taken : need_all));
     *n_short = s_unfit + s_unserved;
   }
 
-  const Lengths me = lengths(held, ctx, nnew, b, max_pages, shift, max_new);
-  const int64_t n0 = s_need_before;
-  const bool served = me.fits && (me.need == 0 || n0 + me.need <= size);
-  int32_t* const row = table + (size_t)b * max_pages;
   // the nth page that the batch takes, from the top of the stack after the pushes
   auto take = [&](int64_t nth) -> int32_t {
     const int64_t e = size - 1 - nth;
@@ -137,29 +143,40 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(
       if (s_rel[mid] <= r) lo = mid;
       else hi = mid - 1;
     }
-    const Lengths g = lengths(held, ctx, nnew, lo, max_pages, shift, max_new);
-    return table[(size_t)lo * max_pages + g.want + (r - s_rel[lo])];
+    return table[(size_t)lo * max_pages + s_want[lo] + (r - s_rel[lo])];
   };
-  if (blockIdx.y == 0) {
-    if (tid == 0) held_out[b] = served ? me.want : me.held;
-    const int64_t p0 = nf + s_rel[b];
-    for (int i = tid; i < me.rel && p0 + i < num_pages; i += kReserveThreads)
-      stack[p0 + i] = row[me.want + i];
-    if (served)
-      for (int i = tid; i < me.need; i += kReserveThreads) row[me.held + i] = take(n0 + i);
-  }
-  if (slots == nullptr) return;
-  const int i0 = blockIdx.y * kSlotsPerGroup, i1 = min(i0 + kSlotsPerGroup, max_new);
-  int64_t* const out = slots + (size_t)b * max_new;
-  const int have = served ? me.nnew : 0;
-  for (int i = i0 + tid; i < i1; i += kReserveThreads) {
-    int64_t s = -1;
-    if (i < have) {
-      const int r = me.ctx + i, q = r >> shift;   // below max_pages << shift: 32 bits hold it
-      const int32_t page = q < me.held ? row[q] : take(n0 + (q - me.held));
-      s = ((int64_t)page << shift) | (r & ((1 << shift) - 1));
+  for (int b = run0; b < run1; ++b) {
+    const Lengths me = lengths(held, ctx, nnew, b, max_pages, shift, max_new);
+    const int64_t n0 = s_need[b - run0];
+    const bool served = me.fits && (me.need == 0 || n0 + me.need <= size);
+    int32_t* const row = table + (size_t)b * max_pages;
+    if (blockIdx.y == 0) {
+      if (tid == 0) held_out[b] = served ? me.want : me.held;
+      const int64_t p0 = nf + s_rel[b];
+      for (int i = tid; i < me.rel && p0 + i < num_pages; i += kReserveThreads)
+        stack[p0 + i] = row[me.want + i];
+      if (served)
+        for (int i = tid; i < me.need; i += kReserveThreads) row[me.held + i] = take(n0 + i);
     }
-    out[i] = s;
+    if (slots == nullptr) continue;
+    const int i0 = blockIdx.y * kSlotsPerGroup, i1 = min(i0 + kSlotsPerGroup, max_new);
+    int64_t* const out = slots + (size_t)b * max_new;
+    const int have = min(served ? me.nnew : 0, i1);
+    // the slice's pages, once each (rows are below max_pages << shift: 32 bits hold them)
+    const int q0 = (me.ctx + i0) >> shift;
+    if (b > run0) __syncthreads();   // the last request's pages are read
+    if (i0 < have) {
+      const int pages = ((me.ctx + have - 1) >> shift) - q0 + 1;
+      for (int i = tid; i < pages; i += kReserveThreads)
+        s_page[i] = q0 + i < me.held ? row[q0 + i] : take(n0 + (q0 + i - me.held));
+    }
+    __syncthreads();
+    for (int i = i0 + tid; i < i1; i += kReserveThreads) {
+      const int r = me.ctx + i;
+      out[i] = i < have
+                   ? ((int64_t)s_page[(r >> shift) - q0] << shift) | (r & ((1 << shift) - 1))
+                   : (int64_t)-1;
+    }
   }
 }
 
@@ -195,9 +212,11 @@ hipError_t launch_reserve(int32_t* table, int max_pages, const int32_t* held, co
                           int32_t* held_out, int32_t* n_free_out, int32_t* n_short,
                           hipStream_t s) {
   if (batch <= 0) return hipSuccess;
+  const int run = (batch + kReserveGroups - 1) / kReserveGroups;
   const int slices = slots ? std::max(1, (max_new + kSlotsPerGroup - 1) / kSlotsPerGroup) : 1;
-  reserve_kernel<<<dim3((unsigned)batch, (unsigned)slices), kReserveThreads, 0, s>>>(
-      table, max_pages, held, ctx, n_new, batch, stack, n_free, num_pages, page_shift, max_new,
+  const dim3 grid((unsigned)((batch + run - 1) / run), (unsigned)slices);
+  reserve_kernel<<<grid, kReserveThreads, 0, s>>>(
+      table, max_pages, held, ctx, n_new, batch, run, stack, n_free, num_pages, page_shift, max_new,
       slots, held_out, n_free_out, n_short);
   return hipGetLastError();
 }
