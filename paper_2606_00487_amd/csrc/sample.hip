@@ -144,7 +144,7 @@ struct Shared {
   uint64_t out64[2];
   uint32_t out32[4];
   uint32_t n, n_hot;
-  uint16_t hot[NT];
+  uint16_t hot[4 * NT];
 };
 
 template <class S, int NT>
@@ -435,7 +435,12 @@ __device__ inline u16x2 keys16(uint32_t w) {
 // caches, and most of them read only the units of the threads that hold values above a bound.
 // (Registers for a row of 150000 bf16 values leave too few for the passes: at every share kept
 // there, the compiler spilled as much.)
-constexpr int kAhead = 10;
+constexpr int kAhead = 8;
+constexpr int kParts = 4;   // a thread's unit j counts to its part j % kParts
+static_assert(kAhead % kParts == 0, "a unit's part is known when the loop is unrolled");
+struct Maxima {
+  float part[kParts], all;   // largest values of the parts, and of all
+};
 
 template <int DT, int NT>
 struct Passes {
@@ -449,7 +454,7 @@ struct Passes {
     full = (x.vocab - head) / U;
   }
   __device__ inline const char* first() const { return row.base + (int64_t)head * (16 / U); }
-  // f(unit's 16 bytes, index of its first element); the trip count is the workgroup's
+  // f(unit's 16 bytes, index of its first element, part); the trip count is the workgroup's
   template <class F>
   __device__ __attribute__((always_inline)) inline void units(F&& f) const {
     const int tid = threadIdx.x;
@@ -466,7 +471,7 @@ struct Passes {
         if (u0 + j * NT >= full) break;
         const int u = u0 + j * NT + tid;
         if (u0 + (j + 1) * NT > full && u >= full) x[j] = make_uint4(kNone, kNone, kNone, kNone);
-        f(x[j], u * U + head);
+        f(x[j], u * U + head, j % kParts);
       }
     }
     ends(f);
@@ -482,57 +487,84 @@ struct Passes {
     if (e >= 0)
       b = DT == TAPS_BF16 ? 0xFFFF0000u | ((const uint16_t*)row.base)[e]
                           : ((const uint32_t*)row.base)[e];
-    f(make_uint4(b, kNone, kNone, kNone), max(e, 0));
+    f(make_uint4(b, kNone, kNone, kNone), max(e, 0), 0);
   }
-  // the largest value of this thread's units (NaN left out; -inf where there is none).  bf16:
+  // The largest values of this thread's units (NaN left out; -inf where there is none).  bf16:
   // the largest 16-bit key, two at a time (three instructions; as floats the halves would be
-  // unpacked and made quiet first, five); a positive NaN in any unit sends the wave through the
-  // floats after all.
-  __device__ __attribute__((always_inline)) inline float max_value() const {
+  // unpacked and made quiet first, five); a positive NaN in any unit sends the workgroup through
+  // the floats after all.
+  __device__ __attribute__((always_inline)) inline Maxima max_value() const {
+    Maxima m;
+    bool done = false;
     if constexpr (DT == TAPS_BF16) {
-      u16x2 mk = {0, 0};
-      units([&](const uint4& w, int) {
-        mk = __builtin_elementwise_max(
-            mk, __builtin_elementwise_max(__builtin_elementwise_max(keys16(w.x), keys16(w.y)),
-                                          __builtin_elementwise_max(keys16(w.z), keys16(w.w))));
+      u16x2 mk[kParts] = {};
+      units([&](const uint4& w, int, int s) {
+        mk[s] = __builtin_elementwise_max(
+            mk[s],
+            __builtin_elementwise_max(__builtin_elementwise_max(keys16(w.x), keys16(w.y)),
+                                      __builtin_elementwise_max(keys16(w.z), keys16(w.w))));
       });
-      const uint32_t k = max((uint32_t)mk[0], (uint32_t)mk[1]);
-      // +inf's key is 0xFF80; -inf's 0x7F (smaller: NaN or nothing)
-      if (!__syncthreads_or(k > 0xFF80u)) return k > 0x7Fu ? key_value(key32(k)) : -INFINITY;
-    }
-    float mx = -INFINITY;
-    units([&](const uint4& w, int) {
-      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-      float t[4];
+      uint32_t top = 0;
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        t[q] = DT == TAPS_BF16 ? fmaxf(__uint_as_float(ww[q] << 16), __uint_as_float(ww[q] & 0xFFFF0000u))
-                               : __uint_as_float(ww[q]);
-      mx = fmaxf(mx, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
-    });
-    return mx;
+      for (int s = 0; s < kParts; ++s) {
+        const uint32_t k = max((uint32_t)mk[s][0], (uint32_t)mk[s][1]);
+        top = max(top, k);
+        // -inf's key is 0x7F (smaller: NaN or nothing)
+        m.part[s] = k > 0x7Fu ? key_value(key32(k)) : -INFINITY;
+      }
+      done = !__syncthreads_or(top > 0xFF80u);   // +inf's key
+    }
+    if (!done) {
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) m.part[s] = -INFINITY;
+      units([&](const uint4& w, int, int s) {
+        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+        float t[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          t[q] = DT == TAPS_BF16
+                     ? fmaxf(__uint_as_float(ww[q] << 16), __uint_as_float(ww[q] & 0xFFFF0000u))
+                     : __uint_as_float(ww[q]);
+        m.part[s] = fmaxf(m.part[s], fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
+      });
+    }
+    m.all = fmaxf(fmaxf(m.part[0], m.part[1]), fmaxf(m.part[2], m.part[3]));
+    return m;
   }
-  // f(value, index) for the elements with lo <= value <= hi: only the units of threads whose
-  // largest value `mx` reaches lo can hold one.  They are shared out to all threads; where they
-  // are most of the threads, every unit is read.  Callers synchronize before the next call.
+  // f(value, index) for the elements with lo <= value <= hi: only the parts (of a thread's
+  // units) whose largest value reaches lo can hold one.  They are shared out to all threads;
+  // where they are most of the parts, every unit is read.  Callers synchronize before the next
+  // call.  (Whole threads instead of quarters: with 60 of 512 threads in question, their units
+  // touch two thirds of the row's cache lines again.)
   template <class F>
-  __device__ __attribute__((always_inline)) inline void between(float mx, float lo, float hi,
-                                                                Shared<DT, NT>& sh,
+  __device__ __attribute__((always_inline)) inline void between(const Maxima& mx, float lo,
+                                                                float hi, Shared<DT, NT>& sh,
                                                                 F&& f) const {
     const int tid = threadIdx.x;
     if (tid == 0) sh.n_hot = 0u;
     __syncthreads();
-    const uint64_t hot = __ballot(mx >= lo);
-    if (hot) {
+    if (__ballot(mx.all >= lo)) {
+      uint64_t hot[kParts];
+      uint32_t num = 0;
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) {
+        hot[s] = __ballot(mx.part[s] >= lo);
+        num += (uint32_t)__popcll(hot[s]);
+      }
       uint32_t at = 0;
-      if ((tid & (kWave - 1)) == 0) at = atomicAdd(&sh.n_hot, (uint32_t)__popcll(hot));
+      if ((tid & (kWave - 1)) == 0) at = atomicAdd(&sh.n_hot, num);
       at = __builtin_amdgcn_readfirstlane(at);
-      at += __builtin_amdgcn_mbcnt_hi((uint32_t)(hot >> 32),
-                                      __builtin_amdgcn_mbcnt_lo((uint32_t)hot, 0u));
-      if (mx >= lo) sh.hot[at] = (uint16_t)tid;
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) {
+        const uint32_t i =
+            at + __builtin_amdgcn_mbcnt_hi((uint32_t)(hot[s] >> 32),
+                                           __builtin_amdgcn_mbcnt_lo((uint32_t)hot[s], 0u));
+        if (mx.part[s] >= lo) sh.hot[i] = (uint16_t)(s * NT + tid);
+        at += (uint32_t)__popcll(hot[s]);
+      }
     }
     __syncthreads();
-    auto one = [&](const uint4& w, int e0) {
+    auto one = [&](const uint4& w, int e0, int) {
       const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
       float x[U];
       bool in[U], any = false;   // one branch for the unit, which mostly holds none
@@ -549,14 +581,15 @@ struct Passes {
       for (int q = 0; q < U; ++q)
         if (in[q]) f(x[q], e0 + q);
     };
-    const int n = (int)sh.n_hot, per = (full + NT - 1) / NT;
-    if (2 * n > NT) {
+    constexpr int kAll = kParts * NT;
+    const int n = (int)sh.n_hot, per = (full + kAll - 1) / kAll;
+    if (2 * n > kAll) {
       units(one);
       return;
     }
     for (int i = tid; i < n * per; i += NT) {
-      const int j = i / n, u = j * NT + (int)sh.hot[i - j * n];
-      if (u < full) one(*(const uint4*)(first() + (int64_t)u * 16), u * U + head);
+      const int j = i / n, u = j * kAll + (int)sh.hot[i - j * n];
+      if (u < full) one(*(const uint4*)(first() + (int64_t)u * 16), u * U + head, 0);
     }
     ends(one);
   }
@@ -663,14 +696,14 @@ __device__ inline float bound_below(double x, float M) {
 // A small top_k, or min_p: the elements above a bound, ranked.  False: more than kList of them.
 template <int DT, int NT>
 __device__ __attribute__((always_inline)) inline bool sample_listed(
-    const Passes<DT, NT>& passes, float mx, const Weights& w, const RowSettings& st,
+    const Passes<DT, NT>& passes, const Maxima& mx, const Weights& w, const RowSettings& st,
     Shared<DT, NT>& sh, Drawn* out) {
   const double least = st.least();
   float thr = -INFINITY;
   if (st.cut_by_min_p() && w.scale > 0.0)   // (an infinite temperature: all weights are equal)
     thr = w.top == INFINITY ? w.top : bound_below((double)w.top + least / w.scale, w.top);
   if (st.few()) {
-    const uint32_t key = top_k_bound<DT, NT>(mx, st.k, sh);
+    const uint32_t key = top_k_bound<DT, NT>(mx.all, st.k, sh);
     if (key) thr = fmaxf(thr, key_value(key));
   }
   ListScratch& ls = sh.u.l;
@@ -706,7 +739,7 @@ __device__ __attribute__((always_inline)) inline bool sample_listed(
 // 16 bits per count let two workgroups share a CU's LDS.
 template <int DT, int NT>
 __device__ __attribute__((always_inline)) inline bool sample_counted(
-    const Passes<DT, NT>& passes, float mx, const Weights& w, const RowSettings& st,
+    const Passes<DT, NT>& passes, const Maxima& mx, const Weights& w, const RowSettings& st,
     Shared<DT, NT>& sh, Drawn* out) {
   constexpr int kWaves = NT / kWave;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
@@ -725,7 +758,7 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
     ((uint4*)cs.count)[i] = make_uint4(0u, 0u, 0u, 0u);
   __syncthreads();
   uint32_t in_window = 0;   // of the wave
-  passes.units([&](const uint4& v, int) {
+  passes.units([&](const uint4& v, int, int) {
     const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
     const u16x2 top = {(unsigned short)kM, (unsigned short)kM};
 #pragma unroll
@@ -900,7 +933,7 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
 // infinite maximum or temperature.
 template <int DT, int NT>
 __device__ __attribute__((always_inline)) inline bool sample_binned(
-    const Passes<DT, NT>& passes, float mx, const Weights& w, const RowSettings& st,
+    const Passes<DT, NT>& passes, const Maxima& mx, const Weights& w, const RowSettings& st,
     Shared<DT, NT>& sh, Drawn* out) {
   const int tid = threadIdx.x;
   BinScratch& bs = sh.u.b;
@@ -923,7 +956,7 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     p = fma(p, t, scalar(c));
     return fixed43(fma(p, t, scalar(513.0)));
   };
-  passes.units([&](const uint4& v, int) {
+  passes.units([&](const uint4& v, int, int) {
     const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
     double z[4];
     uint64_t f[4];
@@ -1055,8 +1088,8 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(
   st.p = s.top_p ? s.top_p[b] : 1.f;
   st.mp = s.min_p ? s.min_p[b] : 0.f;
   st.u = u[r];
-  const float mx = passes.max_value();
-  float M = block_max_f32<Shared<DT, NT>, NT>(mx, sh);
+  const Maxima mx = passes.max_value();
+  float M = block_max_f32<Shared<DT, NT>, NT>(mx.all, sh);
   if (M == 0.f) M = 0.f;   // not -0
   Drawn d;
   bool done = false;
