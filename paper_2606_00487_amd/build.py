@@ -26,6 +26,8 @@ COMMON = ["-O3", "-fPIC", "-std=c++17", "-Wall", f"--offload-arch={ARCH}",
 PER_FILE = {
     "select.hip": ["-ffp-contract=off"],
     "api.cpp": ["-ffp-contract=off"],
+    # the same weight in every pass: a product fused into a sum here and not there differs
+    "sample.hip": ["-ffp-contract=off"],
     # MFMA accumulators in ordinary VGPRs: the attention kernel fits in 256 of them, and
     # the AGPR form would copy its accumulators back and forth around every softmax
     "attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],

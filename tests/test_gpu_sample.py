@@ -191,3 +191,41 @@ def test_refuses_wrong_tensors():
         op(x, u, temperature=torch.zeros(3, device="cuda"))
     with pytest.raises(taps.TapsError):
         taps.TokenSampler(1, 1, (1 << 20) + 1)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("rows", [3, 40, 65])
+def test_long_rows_shared_out(dtype, rows):
+    """Few rows of long vocabularies: steep and flat temperatures, values far from 0, whole
+    stretches masked, NaN and infinities, the largest value at either end."""
+    V = 33000
+    x = normal(20 + rows, 1, rows, V, dtype, raised=30)
+    x[0, 0, 100:30000] = -INF
+    x[0, 1, :32990] = torch.finfo(dtype).min
+    x[0, 2, ::5] = NAN
+    if rows > 3:
+        x[0, 3, 20000], x[0, 3, 7] = INF, INF
+        x[0, 4] = NAN
+        x[0, 5] += 3000.0
+        x[0, 6] -= 3000.0
+        x[0, 7] = 0.5
+        x[0, 8, -1] = 30.0
+        x[0, 9, 0] = 30.0
+        x[0, 10] *= 1000.0
+        x[0, 11] = -INF
+        x[0, 12, 5:] = -INF
+    u = uniform(rows, 1, rows)
+    for T, k, p, m in ((1.0, 0, 0.9, 0.0), (0.6, 0, 1.0, 0.0), (2.5, 0, 0.97, 0.0), (0.9, 0, 0.9, 0.02),
+                       (1e-3, 0, 0.9, 0.0), (0.02, 0, 0.5, 0.0), (300.0, 0, 0.5, 0.0), (1.0, 1000, 0.9, 0.0),
+                       (0.8, 50, 0.9, 0.0), (1.0, 0, 1.0, 0.3), (0.0, 0, 1.0, 0.0), (INF, 0, 0.7, 0.0)):
+        check(x, u, None, [T], [k], [p], [m])
+
+
+def test_min_p_borders_with_top_p():
+    """min_p and top_p together, on values an equal step apart, so that borders fall on values."""
+    for dtype in (BF, FP):
+        for V in (500, 40000):
+            x = (torch.arange(V, device="cuda") % 97).mul(-0.0625).to(dtype).view(1, 1, V).repeat(1, 8, 1)
+            for m in (0.5, 0.0625 / 2, 0.9, 1.0, 1e-3):
+                check(x, uniform(V, 1, 8), None, [1.0], None, [0.95], [m])
+                check(x, uniform(V + 1, 1, 8), None, [0.25], [90], [0.99], [m])
