@@ -816,16 +816,18 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
     if (lane == 0) cs.mass[r] = m, cs.num[r] = n;
   }
   __syncthreads();
-  uint64_t S, have, counted;
+  uint64_t S, have;
   {
+    // the runs' counts, and above them the elements that the waves have seen in the window
     const uint64_t m = tid < runs ? cs.mass[tid] : 0ull, n = tid < runs ? cs.num[tid] : 0ull;
+    const uint64_t seen = lane == 0 ? (uint64_t)in_window << 32 : 0ull;
     const uint64_t pm = block_scan_u64<Shared<DT, NT>, NT>(m, sh, &S) - m;
-    const uint64_t pn = block_scan_u64<Shared<DT, NT>, NT>(n, sh, &have) - n;
+    const uint64_t pn = block_scan_u64<Shared<DT, NT>, NT>(n + seen, sh, &have) - n;
     if (tid < runs) cs.mass[tid] = pm, cs.num[tid] = (uint32_t)pn;
-    counted = block_sum_u64<Shared<DT, NT>, NT>(lane == 0 ? in_window : 0u, sh);
   }
   // a count past 16 bits loses 65536, or turns them into one of its neighbour's
-  if (counted != have) return false;
+  if ((have >> 32) != (have & 0xFFFFFFFFull)) return false;
+  have &= 0xFFFFFFFFull;
 
   struct Cross {
     uint32_t pos, ties, nth;     // window position, elements there, the crossing one among them
