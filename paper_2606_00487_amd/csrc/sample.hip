@@ -93,6 +93,36 @@ __device__ inline uint64_t lane_u64(uint64_t v, int lane) {   // lane uniform
 __device__ inline uint64_t wave_sum_u64(uint64_t v) {
   return lane_u64(wave_scan_u64(v), kWave - 1);
 }
+// the same over rows of 16 lanes
+__device__ inline uint32_t row_scan_u32(uint32_t x) {
+  int v = (int)x;
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  return (uint32_t)v;
+}
+__device__ inline uint64_t row_scan_u64(uint64_t v) {
+  const uint32_t a = row_scan_u32((uint32_t)v & 0x3FFFFFu);
+  const uint32_t b = row_scan_u32((uint32_t)(v >> 22) & 0x3FFFFFu);
+  const uint32_t c = row_scan_u32((uint32_t)(v >> 44));
+  return (uint64_t)a + ((uint64_t)b << 22) + ((uint64_t)c << 44);
+}
+// maximum over the lanes, in the last one (a lane without a source compares with itself)
+template <int CTRL, int ROWS>
+__device__ inline float dpp_max(float v) {
+  const int x = (int)__float_as_uint(v);
+  return fmaxf(v, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(x, x, CTRL, ROWS, 0xf, false)));
+}
+__device__ inline float row_max_f32(float v) {
+  v = dpp_max<0x111, 0xf>(v);
+  v = dpp_max<0x112, 0xf>(v);
+  v = dpp_max<0x114, 0xf>(v);
+  return dpp_max<0x118, 0xf>(v);
+}
+__device__ inline float lane_f32(float v, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
 
 constexpr int kBins = 2048;         // radix digits of the general path
 constexpr int kWindow = 36864;      // bf16 values counted one by one, from the largest down
@@ -100,6 +130,7 @@ constexpr int kRun = 256;           // values whose sums are kept together: four
 constexpr int kRuns = kWindow / kRun;
 constexpr int kPerOctave = 32;      // fp32: bins of the weight per factor of two
 constexpr int kWeightBins = 1424;   // 44.5 octaves: smaller weights round to 0
+constexpr int kSub = 1024;          // parts of a bin with more elements than the list takes
 constexpr int kList = 1024;         // elements that are ranked one by one
 constexpr int kGroups = 256;        // thread groups whose maxima bound a small top_k
 constexpr int kFewTopK = 192;       // ... up to this one
@@ -119,8 +150,10 @@ struct CountScratch {
 };
 struct BinScratch {
   ListScratch l;
-  uint64_t mass[kWeightBins];
-  uint64_t before[kWeightBins];
+  uint64_t mass[kWeightBins];       // sums of the bins; then those before them
+  uint32_t num[kWeightBins];        // elements, the same way
+  uint64_t sub[kSub];
+  uint32_t sub_num[kSub];
 };
 template <int DT>
 union PathScratch {
@@ -147,47 +180,41 @@ struct Shared {
   uint16_t hot[4 * NT];
 };
 
-template <class S, int NT>
-__device__ inline uint64_t block_sum_u64(uint64_t v, S& sh) {
-  v = wave_sum_u64(v);
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  __syncthreads();
-  if (lane == 0) sh.red[wave] = v;
-  __syncthreads();
-  uint64_t s = 0;
-#pragma unroll
-  for (int w = 0; w < NT / kWave; ++w) s += sh.red[w];
-  return s;
-}
-
+// Over the workgroup: each wave's sum through LDS, one read per wave and a scan over its lanes
+// (every wave adding up all of them: 16 reads each, a microsecond of LDS time a call).
 template <class S, int NT>
 __device__ inline uint64_t block_scan_u64(uint64_t v, S& sh, uint64_t* total) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  constexpr int kWaves = NT / kWave;
+  static_assert(kWaves <= 16 && (kWaves & (kWaves - 1)) == 0, "one row of lanes holds the waves");
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   v = wave_scan_u64(v);
   __syncthreads();
   if (lane == kWave - 1) sh.red[wave] = v;
   __syncthreads();
-  uint64_t before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < NT / kWave; ++w) {
-    if (w < wave) before += sh.red[w];
-    all += sh.red[w];
-  }
-  *total = all;
-  return v + before;
+  const uint64_t x = sh.red[lane & (kWaves - 1)], incl = row_scan_u64(x);
+  *total = lane_u64(incl, kWaves - 1);
+  return v + lane_u64(incl - x, wave);
+}
+
+template <class S, int NT>
+__device__ inline uint64_t block_sum_u64(uint64_t v, S& sh) {
+  uint64_t total;
+  block_scan_u64<S, NT>(v, sh, &total);
+  return total;
 }
 
 template <class S, int NT>
 __device__ inline float block_max_f32(float v, S& sh) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
+  constexpr int kWaves = NT / kWave;
+  v = row_max_f32(v);
+  v = dpp_max<0x142, 0xa>(v);
+  v = dpp_max<0x143, 0xc>(v);
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   __syncthreads();
-  if (lane == 0) sh.red32[wave] = __float_as_uint(v);
+  if (lane == kWave - 1) sh.red32[wave] = __float_as_uint(v);
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < NT / kWave; ++w) v = fmaxf(v, __uint_as_float(sh.red32[w]));
-  return v;
+  return lane_f32(row_max_f32(__uint_as_float(sh.red32[lane & (kWaves - 1)])), kWaves - 1);
 }
 
 // One row of logits, read 16 bytes at a time; f(key, index) for the elements of this thread.
@@ -927,12 +954,13 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
 }
 
 // ----------------------------------------------------------------------------------
-// fp32, the whole vocabulary's sum (top_p or no filter): weights are added up by bins of 1/32
-// octave.  Weight 2^-(z / 32), z = 32 log2(e) (M - x) / T, is the bin's 2^-(b / 32), b = floor
-// z, times a factor 2^-((z - b) / 32) from a short series; a bin adds up its factors (integers
-// of 2^-43), and its sum is that times 2^-(b / 32), rounded down.  The bin where a running sum
-// passes its target is then ranked one by one.  False: more than kList elements in it, or an
-// infinite maximum or temperature.
+// fp32, the whole vocabulary's sum (a larger top_k, top_p or no filter): weights are added up by
+// bins of 1/32 octave.  Weight 2^-(z / 32), z = 32 log2(e) (M - x) / T, is the bin's 2^-(b / 32),
+// b = floor z, times a factor 2^-((z - b) / 32) from a short series; a bin adds up its factors
+// (integers of 2^-43), and its sum is that times 2^-(b / 32), rounded down.  The bin where a
+// running sum or count passes its target is then ranked one by one; of one that the list does not
+// hold, 1/1024 is, found the same way, or that has one value only (logits that were bf16 once).
+// False: anything denser, or an infinite maximum or temperature.
 template <int DT, int NT>
 __device__ __attribute__((always_inline)) inline bool sample_binned(
     const Passes<DT, NT>& passes, const Maxima& mx, const Weights& w, const RowSettings& st,
@@ -944,7 +972,7 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   // temperature all weights are equal
   if (M == INFINITY || !(w.scale > 0.0)) return false;
   const double scale = kPerOctave * w.scale;
-  for (int i = tid; i < kWeightBins; i += NT) bs.mass[i] = 0ull;
+  for (int i = tid; i < kWeightBins; i += NT) bs.mass[i] = 0ull, bs.num[i] = 0u;
   __syncthreads();
   auto depth = [&](float x) -> double { return ((double)M - (double)x) * scale; };
   auto factor = [&](double z) -> uint64_t {
@@ -958,6 +986,7 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     p = fma(p, t, scalar(c));
     return fixed43(fma(p, t, scalar(513.0)));
   };
+  const bool counts = st.k > 0;
   passes.units([&](const uint4& v, int, int) {
     const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
     double z[4];
@@ -974,97 +1003,193 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     for (int q = 0; q < 4; ++q)
       if (z[q] < (double)kWeightBins)
         atomicAdd((unsigned long long*)&bs.mass[(int)z[q]], (unsigned long long)f[q]);
+    if (counts) {   // uniform
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (z[q] < (double)kWeightBins) atomicAdd(&bs.num[(int)z[q]], 1u);
+    }
   });
   __syncthreads();
   auto bin_scale = [&](int b) -> double { return exp2_neg(-(double)b / kPerOctave); };
-  uint64_t S;
+  uint64_t S, have = 0;
   {
     constexpr int E = (kWeightBins + NT - 1) / NT;
-    uint64_t m[E], sum = 0;
+    uint64_t m[E], n[E], sum = 0, num = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int b = tid * E + e;
       m[e] = b < kWeightBins ? (uint64_t)(bin_scale(b) * (double)bs.mass[b]) : 0ull;
+      n[e] = b < kWeightBins ? bs.num[b] : 0u;
       sum += m[e];
+      num += n[e];
     }
     uint64_t run = block_scan_u64<Shared<DT, NT>, NT>(sum, sh, &S) - sum;
+    uint64_t nrun = counts ? block_scan_u64<Shared<DT, NT>, NT>(num, sh, &have) - num : 0ull;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int b = tid * E + e;
-      if (b < kWeightBins) bs.before[b] = run;
+      if (b < kWeightBins) bs.mass[b] = run, bs.num[b] = (uint32_t)nrun;
       run += m[e];
+      nrun += n[e];
     }
   }
   __syncthreads();
 
-  // Ranks the elements of a bin: sorted[], and the running sums with each of them in cum[].
-  // Returns their number; above kList nothing is ranked.
-  int ranked = -1;
-  auto rank_bin = [&](int bin) -> uint32_t {
-    if (bin == ranked) return sh.n;
-    ranked = bin;
+  // f(x, z, index) for the elements whose depth z is in [zlo, zhi)
+  auto within = [&](double zlo, double zhi, auto&& f) {
+    passes.between(mx, bound_below((double)M - zhi / scale, M),
+                   -bound_below(zlo / scale - (double)M, M), sh, [&](float x, int e) {
+                     const double z = depth(x);
+                     if (z >= zlo && z < zhi) f(x, z, e);
+                   });
+    __syncthreads();
+  };
+  // list[] from the elements whose depth is in [zlo, zhi); their number
+  auto collect = [&](double zlo, double zhi) -> uint32_t {
     __syncthreads();
     if (tid == 0) sh.n = 0u;
-    __syncthreads();
-    const float lo = bound_below((double)M - (double)(bin + 1) / scale, M);
-    const float hi = -bound_below((double)bin / scale - (double)M, M);
-    // (the bounds may let neighbours in: they add nothing to the running sums)
-    passes.between(mx, lo, hi, sh, [&](float x, int e) {
+    within(zlo, zhi, [&](float x, double, int e) {
       const uint32_t i = atomicAdd(&sh.n, 1u);
       if (i < (uint32_t)kList)
         bs.l.list[i] = cand_key(value_key(__float_as_uint(x)), (uint32_t)e);
     });
-    __syncthreads();
-    const uint32_t n = sh.n;
-    if (n > (uint32_t)kList) return n;
-    sort_list<DT, NT>(n, sh);
-    const double bsc = bin_scale(bin);
-    const uint64_t before = bs.before[bin];
-    sum_list<DT, NT>(
-        n, sh,
-        [&](uint32_t key) {
-          const double z = depth(key_value(key));
-          return z >= (double)bin && z < (double)(bin + 1) ? factor(z) : 0ull;
-        },
-        [&](uint64_t c) { return before + (uint64_t)(bsc * (double)c); });
-    return n;
+    return sh.n;
   };
-  // the bin where the running sum first exceeds target
-  auto bin_of = [&](uint64_t target) -> int {
+  struct Found {
+    uint32_t key, nth;   // the element's key; its place among its equals where token is -1
+    int token, bin;
+    uint64_t through;    // the running sum with it
+  };
+  // The element where the running sum (count) in rank order first exceeds target
+  auto locate = [&](uint64_t target, bool by_count, Found& f) -> bool {
     for (int b = tid; b < kWeightBins; b += NT) {
-      const uint64_t hi = b + 1 < kWeightBins ? bs.before[b + 1] : S;
-      if (bs.before[b] <= target && target < hi) sh.out32[0] = (uint32_t)b;
+      const bool more = b + 1 < kWeightBins;
+      const uint64_t lo = by_count ? (uint64_t)bs.num[b] : bs.mass[b];
+      const uint64_t hi = by_count ? (more ? (uint64_t)bs.num[b + 1] : have)
+                                   : (more ? bs.mass[b + 1] : S);
+      if (lo <= target && target < hi) sh.out32[0] = (uint32_t)b;
     }
     __syncthreads();
-    return (int)sh.out32[0];
-  };
-  uint64_t kept = S;
-  if (st.p < 1.f) {
-    const uint64_t target = top_p_sum(st.p, S) - 1;
-    const uint32_t n = rank_bin(bin_of(target));
-    if (n > (uint32_t)kList) return false;
-    kept = bs.l.cum[first_above<DT, NT>(target, n, sh)];
-  }
-  if (st.mp > 0.f) {
-    const double last = -kPerOctave * st.least();   // the depth down to which tokens are kept
-    if (last < (double)kWeightBins) {
-      const uint32_t n = rank_bin((int)last);
-      if (n > (uint32_t)kList) return false;
-      // kept ones of the bin come first; without any, all before it
-      const uint32_t in =
-          count_list<DT, NT>(n, sh, [&](uint32_t key) { return depth(key_value(key)) <= last; });
-      kept = min(kept, in ? bs.l.cum[in - 1] : bs.before[(int)last]);
+    const int bin = (int)sh.out32[0];
+    f.bin = bin;
+    const double bsc = bin_scale(bin);
+    const uint64_t before = bs.mass[bin];
+    // the running sum after the bin's factors c
+    auto through = [&](uint64_t c) -> uint64_t { return before + (uint64_t)(bsc * (double)c); };
+    double zlo = (double)bin, zhi = (double)(bin + 1);
+    uint64_t c0 = 0;                      // factors and elements of the bin before the list
+    uint32_t n0 = bs.num[bin];
+    uint32_t n = collect(zlo, zhi);
+    if (n > (uint32_t)kList) {
       __syncthreads();
+      for (int i = tid; i < kSub; i += NT) bs.sub[i] = 0ull, bs.sub_num[i] = 0u;
+      __syncthreads();
+      within(zlo, zhi, [&](float, double z, int) {
+        const int i = (int)(__builtin_amdgcn_fract(z) * kSub);
+        atomicAdd((unsigned long long*)&bs.sub[i], (unsigned long long)factor(z));
+        atomicAdd(&bs.sub_num[i], 1u);
+      });
+      constexpr int E = kSub / NT;
+      uint64_t m[E], k[E], sum = 0, num = 0, all;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        m[e] = bs.sub[tid * E + e];
+        k[e] = bs.sub_num[tid * E + e];
+        sum += m[e];
+        num += k[e];
+      }
+      uint64_t run = block_scan_u64<Shared<DT, NT>, NT>(sum, sh, &all) - sum;
+      uint64_t nrun = n0 + block_scan_u64<Shared<DT, NT>, NT>(num, sh, &all) - num;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint64_t lo = by_count ? nrun : through(run);
+        const uint64_t hi = by_count ? nrun + k[e] : through(run + m[e]);
+        if (lo <= target && target < hi) {
+          sh.out32[1] = (uint32_t)(tid * E + e);
+          sh.out32[2] = (uint32_t)nrun;
+          sh.out64[0] = run;
+        }
+        run += m[e];
+        nrun += k[e];
+      }
+      __syncthreads();
+      zlo += (double)sh.out32[1] / kSub;
+      zhi = zlo + 1.0 / kSub;
+      n0 = sh.out32[2];
+      c0 = sh.out64[0];
+      n = collect(zlo, zhi);
+    }
+    if (n > (uint32_t)kList) {   // more than the list holds: equals?
+      const uint32_t key = (uint32_t)(bs.l.list[0] >> 32);
+      if (tid == 0) sh.out32[3] = 0u;
+      within(zlo, zhi, [&](float x, double, int) {
+        if (value_key(__float_as_uint(x)) != key) sh.out32[3] = 1u;
+      });
+      if (sh.out32[3]) return false;
+      const uint64_t W = factor(depth(key_value(key)));
+      uint32_t nth = (uint32_t)(target - n0);
+      if (!by_count) {
+        uint32_t hi = n - 1;   // the crossing one is in [nth, hi]
+        nth = 0;
+        while (nth < hi) {
+          const uint32_t mid = (nth + hi) / 2;
+          if (through(c0 + (mid + 1ull) * W) > target) hi = mid;
+          else nth = mid + 1;
+        }
+      }
+      f.key = key;
+      f.nth = nth;
+      f.token = -1;
+      f.through = through(c0 + (nth + 1ull) * W);
+      return true;
+    }
+    sort_list<DT, NT>(n, sh);
+    sum_list<DT, NT>(
+        n, sh, [&](uint32_t key) { return factor(depth(key_value(key))); },
+        [&](uint64_t c) { return through(c0 + c); });
+    const uint32_t i = by_count ? (uint32_t)(target - n0) : first_above<DT, NT>(target, n, sh);
+    const uint64_t e = bs.l.sorted[i];
+    f.key = (uint32_t)(e >> 32);
+    f.token = (int)cand_index(e);
+    f.through = bs.l.cum[i];
+    return true;
+  };
+
+  // what min_p keeps (before the loop: inside, the compiler evaluates its logarithm and bounds
+  // for every row, 1 us)
+  uint64_t Sm = S;
+  if (st.mp > 0.f) {
+    const double last = -kPerOctave * st.least();   // the depth of the last one kept
+    if (last < (double)kWeightBins) {
+      const int bin = (int)last;
+      uint64_t c = 0;   // of the bin, what is kept
+      within((double)bin, (double)(bin + 1), [&](float, double z, int) {
+        if (z <= last) c += factor(z);
+      });
+      c = block_sum_u64<Shared<DT, NT>, NT>(c, sh);
+      Sm = bs.mass[bin] + (uint64_t)(bin_scale(bin) * (double)c);
     }
   }
-  const uint64_t target = draw_target(st.u, kept);
-  const int bin = bin_of(target);
-  const uint32_t n = rank_bin(bin);
-  if (n > (uint32_t)kList) return false;
-  const uint64_t key = bs.l.sorted[first_above<DT, NT>(target, n, sh)];
-  out->token = (int)cand_index(key);
-  out->prob = (float)(bin_scale(bin) * (double)factor(depth(key_value((uint32_t)(key >> 32)))) /
-                      (double)kept);
+  uint64_t kept = S;
+  Found f;
+#pragma unroll 1
+  for (int step = 0; step < 3; ++step) {   // top_k, top_p, the drawn one
+    uint64_t target;
+    if (step == 0) {
+      if (!counts || (uint64_t)st.k >= have) continue;
+      target = (uint64_t)(st.k - 1);
+    } else if (step == 1) {
+      if (!(st.p < 1.f)) continue;
+      target = top_p_sum(st.p, kept) - 1;
+    } else {
+      kept = min(kept, Sm);
+      target = draw_target(st.u, kept);
+    }
+    if (!locate(target, step == 0, f)) return false;
+    if (step < 2) kept = f.through;
+  }
+  out->token = f.token >= 0 ? f.token : nth_index<DT, NT>(passes.row, f.key, f.nth, sh);
+  out->prob = (float)(bin_scale(f.bin) * (double)factor(depth(key_value(f.key))) / (double)kept);
   return true;
 }
 
@@ -1112,7 +1237,7 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(
           __syncthreads();
           done = sample_counted<DT, NT>(passes, mx, w, st, sh, &d);
         }
-      } else if (!done && (st.k <= 0 || st.k >= vocab)) {
+      } else if (!done) {
         __syncthreads();
         done = sample_binned<DT, NT>(passes, mx, w, st, sh, &d);
       }

@@ -229,3 +229,19 @@ def test_min_p_borders_with_top_p():
             for m in (0.5, 0.0625 / 2, 0.9, 1.0, 1e-3):
                 check(x, uniform(V, 1, 8), None, [1.0], None, [0.95], [m])
                 check(x, uniform(V + 1, 1, 8), None, [0.25], [90], [0.99], [m])
+
+
+@pytest.mark.parametrize("sigma", [1e-5, 0.02, 1.0])
+@pytest.mark.parametrize("rounded", [False, True])
+def test_dense_rows(sigma, rounded):
+    """fp32 rows with thousands of values within a few percent of one another's weight, exact
+    ties among them where the logits were bf16 once."""
+    B, V = 8, 70001
+    x = normal(30, B, 3, V, FP, sigma)
+    if rounded:
+        x = x.to(BF).to(FP)
+    T, k = [1.0, 1.0, 10.0, 0.7, 1.0, 1.0, 2.0, 1.0], [0, 0, 0, 500, 30000, V - 1, 1200, 193]
+    p, m = [1.0, 0.9, 0.5, 1.0, 0.9, 1.0, 0.3, 1.0], [0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.9, 0.5]
+    check(x, uniform(31, B, 3), None, T, k, p, m)
+    check(x, uniform(32, B, 3), None, T, k, p, None)
+    check(x.repeat(1, 14, 1)[:, :40].contiguous(), uniform(33, B, 40), None, T, k, p, m)
