@@ -437,14 +437,15 @@ taps_status verify_layer_paged(const void *X, const taps_layer_weights *w, void 
  *                ones are written from entry n_free on (none past num_pages)
  *   n_free       [1] int32, clamped to [0, num_pages]
  *   num_pages, page_rows  as for tree_verify_attn_paged; max_pages * page_rows at most 2^30
- *   held_out     [batch] pages held afterwards; must not be the held_pages array
- *   n_free_out   [1] free pages afterwards; must not be the n_free array
+ *   held_out     [batch] pages held afterwards; not in the held_pages array
+ *   n_free_out   [1] free pages afterwards; not the n_free array
  *   n_short      [1] number of requests that did not get what they need
  *   slot_map     [batch][max_new] int64, or NULL: the pool row of logical row ctx + i, page id
  *                * page_rows + (ctx + i) % page_rows, for i < new; -1 from new on, and for
  *                every row of a request that is short
- * batch at most 4096.  The call is one kernel and needs no workspace; a page id must not be in
- * two places (the tables' held entries and the stack). */
+ * batch at most 4096; a batch of 0 writes nothing, n_free_out and n_short neither.  The call is
+ * one kernel and needs no workspace; a page id must not be in two places (the tables' held
+ * entries and the stack). */
 taps_status kv_reserve_paged(int32_t *block_table, int32_t max_pages, const int32_t *held_pages,
                              const int32_t *ctx_len, const int32_t *n_new, int32_t batch,
                              int32_t max_new, int32_t *free_pages, const int32_t *n_free,
@@ -490,7 +491,7 @@ size_t decode_attn_paged_workspace_bytes(int32_t batch, int32_t Hq, int32_t Hkv,
  *   max_len      [host] upper bound of kv_len, sizes the grid
  *   dtype        TAPS_BF16 (fp32 accumulation, output rounded to nearest even) or TAPS_FP32
  *   scale        softmax scale, finite and > 0
- *   O            [batch][Hq][head_dim] in dtype, 16-byte aligned
+ *   O            [batch][Hq][head_dim] in dtype, 16-byte aligned; not in Q's memory
  *   ws           decode_attn_paged_workspace_bytes(...) bytes, 16-byte aligned */
 taps_status decode_attn_paged(const void *Q, int64_t q_stride, const void *K_pages,
                               const void *V_pages, int32_t num_pages, int32_t page_rows,

@@ -513,7 +513,9 @@ class PagedKVReserve:
         _need_on(dev, n_new, "n_new", torch.int32, (batch,))
         _need_on(dev, free_pages, "free_pages", torch.int32, (num_pages,))
         _need_on(dev, n_free, "n_free", torch.int32, (1,))
-        counts = block_table.new_empty(batch + 2)   # one allocation for the three
+        # one allocation for the three; without requests the call writes nothing
+        counts = block_table.new_empty(batch + 2) if batch else torch.cat(
+            (n_free.clamp(0, num_pages), torch.zeros_like(n_free)))
         held, free, short = counts.split_with_sizes((batch, 1, 1))
         slots = block_table.new_empty((batch, max_new), dtype=torch.int64) if self.slot_map else None
         at = counts.data_ptr()

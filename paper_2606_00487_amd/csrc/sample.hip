@@ -386,14 +386,14 @@ struct Drawn {
   float prob;
 };
 
-// floor(u S), below S
+// floor(u S), below S; NaN counts as 0
 __device__ inline uint64_t draw_target(float u, uint64_t S) {
-  const double t = floor((double)fminf(fmaxf(u, 0.f), 1.f) * (double)S);
+  const double t = floor((u > 0.f ? (double)fminf(u, 1.f) : 0.0) * (double)S);
   return min((uint64_t)t, S - 1);
 }
 // the running sum that top_p asks for: ceil(p S), 1 .. S
 __device__ inline uint64_t top_p_sum(float p, uint64_t S) {
-  return min(max((uint64_t)ceil((double)fmaxf(p, 0.f) * (double)S), (uint64_t)1), S);
+  return min(max((uint64_t)ceil((p > 0.f ? (double)p : 0.0) * (double)S), (uint64_t)1), S);
 }
 
 // Any row: every question by a radix descent over the row in memory
@@ -546,13 +546,14 @@ struct Passes {
       for (int s = 0; s < kParts; ++s) m.part[s] = -INFINITY;
       units([&](const uint4& w, int, int s) {
         const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-        float t[4];
+        // (compared and selected: the compiler leaves operands of a maximum of three unquieted,
+        // and a signalling NaN among them becomes the result)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          t[q] = DT == TAPS_BF16
-                     ? fmaxf(__uint_as_float(ww[q] << 16), __uint_as_float(ww[q] & 0xFFFF0000u))
-                     : __uint_as_float(ww[q]);
-        m.part[s] = fmaxf(m.part[s], fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
+        for (int q = 0; q < U; ++q) {
+          const float x = __uint_as_float(
+              DT == TAPS_BF16 ? ((q & 1) ? ww[q >> 1] & 0xFFFF0000u : ww[q >> 1] << 16) : ww[q & 3]);
+          m.part[s] = x > m.part[s] ? x : m.part[s];
+        }
       });
     }
     m.all = fmaxf(fmaxf(m.part[0], m.part[1]), fmaxf(m.part[2], m.part[3]));

@@ -151,3 +151,75 @@ def test_round_with_sampled_targets():
     want = oracle.kv_reserve_paged(table, held, nc, [N] * B, free, 40 - at, pr, N)
     np.testing.assert_array_equal(t_dev.cpu().numpy(), want[0])
     assert h.tolist() == want[1].tolist() and nf.tolist() == [want[3]] and short.tolist() == [0]
+
+
+def test_captured_step():
+    """One decoding step (reserve, append, attention, sampling, lengths) captured once and
+    replayed per token: the same pages, caches and tokens as the step run eagerly, also where
+    requests end in between and eager work runs beside the replays."""
+    B, Hq, Hkv, hd, pr, width, pages = 5, 8, 2, 64, 32, 20, 60
+    V = Hq * hd                                   # the attention's output serves as logits
+    g = torch.Generator(device="cuda").manual_seed(7)
+    emb = torch.randn(V, (Hq + 2 * Hkv) * hd, generator=g, device="cuda") * 2
+    T, top_p, top_k = (torch.tensor(a, device="cuda") for a in (
+        [0.3, 1.0, 0.0, 0.5, 0.8], [0.9, 1.0, 1.0, 0.8, 0.95], [0, 0, 0, 20, 300]))
+    top_k = top_k.int()
+    u = torch.rand(64, B, 1, generator=g, device="cuda")
+    res = taps.PagedKVReserve(B, width, pages, pr, 1)
+    app = taps.PagedKVAppend(Hkv, hd, pr, dtype=taps.FP32)
+    att = taps.PagedDecodeAttention(B, Hq, Hkv, hd, width * pr, pr, dtype=taps.FP32)
+    smp = taps.TokenSampler(B, 1, V, dtype=taps.FP32)
+
+    def state():
+        return dict(table=torch.zeros(B, width, dtype=torch.int32, device="cuda"),
+                    held=i32([0] * B), ctx=i32([0] * B), new=i32([1] * B),
+                    free=i32(range(pages)), n_free=i32([pages]), tok=i32([[b] for b in range(B)]),
+                    K=torch.zeros(pages, pr, Hkv, hd, device="cuda"),
+                    V=torch.zeros(pages, pr, Hkv, hd, device="cuda"), u=u[0].clone())
+
+    def step(s):
+        held, n_free, _, slots = res(s["table"], s["held"], s["ctx"], s["new"], s["free"], s["n_free"])
+        x = emb.index_select(0, s["tok"].view(-1)).unflatten(1, (Hq + 2 * Hkv, hd))
+        app(x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], slots, s["K"], s["V"])
+        s["ctx"].add_(s["new"])
+        O = att(x[:, :Hq], s["K"], s["V"], s["table"], s["ctx"])
+        tok, _ = smp(O.view(B, 1, V), s["u"], temperature=T, top_p=top_p, top_k=top_k)
+        s["tok"].copy_(tok), s["held"].copy_(held), s["n_free"].copy_(n_free)
+
+    eager, caught = state(), state()
+    warm = state()
+    step(warm)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(caught)
+    torch.cuda.synchronize()
+    for t in range(64):
+        for s in (eager, caught):
+            s["u"].copy_(u[t])
+            if t in (20, 41):                     # a request ends, and starts again as a new one
+                s["ctx"][t % B] = 0
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        for k in eager:
+            assert torch.equal(eager[k], caught[k]), (t, k)
+    assert int(eager["held"].sum()) + int(eager["n_free"]) == pages
+    assert eager["ctx"].tolist() == [64 - 20, 64 - 41, 64, 64, 64]
+
+
+def test_empty_batches():
+    """A batch of no requests: nothing is taken, and the stack's length is passed on."""
+    e = lambda *s: torch.empty(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+    held, n_free, short, slots = taps.PagedKVReserve(0, 4, 8, 32, 3)(
+        e(0, 4), e(0), e(0), e(0), i32(range(8)), i32([5]))
+    assert held.shape == (0,) and n_free.tolist() == [5] and short.tolist() == [0]
+    assert slots.shape == (0, 3)
+    pool = torch.ones(8, 32, 2, 64, dtype=BF, device="cuda")
+    row = torch.empty(0, 2, 64, dtype=BF, device="cuda")
+    taps.PagedKVAppend(2, 64, 32)(row, row, torch.empty(0, dtype=torch.int64, device="cuda"), pool, pool.clone())
+    assert taps.PagedDecodeAttention(0, 4, 2, 64, 128, 32)(
+        torch.empty(0, 4, 64, dtype=BF, device="cuda"), pool, pool, e(0, 4), e(0)).shape == (0, 4, 64)
+    tok, probs = taps.TokenSampler(0, 3, 50)(torch.empty(0, 3, 50, dtype=BF, device="cuda"),
+                                            torch.empty(0, 3, device="cuda"))
+    assert tok.shape == (0, 3) and probs.shape == (0, 3)

@@ -245,3 +245,28 @@ def test_dense_rows(sigma, rounded):
     check(x, uniform(31, B, 3), None, T, k, p, m)
     check(x, uniform(32, B, 3), None, T, k, p, None)
     check(x.repeat(1, 14, 1)[:, :40].contiguous(), uniform(33, B, 40), None, T, k, p, m)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_signalling_nan(dtype):
+    """NaN of every kind (quiet, signalling, either sign) in the largest values' places."""
+    V = 5000
+    x = normal(40, 1, 8, V, dtype)
+    bits = [0x7F81, -0x7F, 0x7FC0, -0x40] if dtype == BF else [0x7F800001, -0x7FFFFF, 0x7FC00000, -0x400000]
+    for i, b in enumerate(bits):
+        x.view(torch.int16 if dtype == BF else torch.int32)[0, :, i::9] = b
+        for T, k, p, m in ((1.0, 0, 1.0, 0.0), (0.7, 40, 0.9, 0.0), (1.0, 0, 0.9, 0.0), (0.0, 0, 1.0, 0.0),
+                           (1.0, 0, 1.0, 0.1), (1.0, 700, 0.9, 0.01)):
+            check(x, uniform(41 + i, 1, 8), None, [T], [k], [p], [m])
+
+
+@pytest.mark.parametrize("T", [1e-38, 1e-6, 1e4, 3e38])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_extreme_temperatures(dtype, T):
+    """Temperatures whose weights are one-hot, or so flat that a bin holds the whole row."""
+    x = normal(42, 1, 6, 4000, dtype)
+    x[0, 1] *= 1e30
+    x[0, 2] *= 1e-30
+    x[0, 3, :2000] = -INF
+    for k, p, m in ((0, 1.0, 0.0), (0, 0.6, 0.0), (300, 1.0, 0.0), (300, 0.5, 0.0), (0, 1.0, 0.999), (5, 0.9, 0.5)):
+        check(x, uniform(43, 1, 6), None, [T], [k], [p], [m])
