@@ -143,15 +143,17 @@ struct GeneralScratch {
 struct alignas(16) ListScratch {
   uint64_t list[kList], sorted[kList], cum[kList];
 };
+// (the elements outside a histogram are added too, into a word per lane behind it: a branch for
+// each element costs more, and one word for all of them would take them one by one)
 struct CountScratch {
-  uint32_t count[kWindow / 2];      // elements per value, 16 bits each, the largest value first
+  uint32_t count[kWindow / 2 + kWave];   // elements per value, 16 bits each, the largest first
   uint64_t mass[kRuns];             // sums of the runs; then those before them
   uint32_t num[kRuns];
 };
 struct BinScratch {
   ListScratch l;
-  uint64_t mass[kWeightBins];       // sums of the bins; then those before them
-  uint32_t num[kWeightBins];        // elements, the same way
+  uint64_t mass[kWeightBins + kWave];   // sums of the bins; then those before them
+  uint32_t num[kWeightBins + kWave];    // elements, the same way
   uint64_t sub[kSub];
   uint32_t sub_num[kSub];
 };
@@ -796,8 +798,8 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
       const uint32_t i0 = idx & 0xFFFFu, i1 = idx >> 16;
       in_window += __popcll(__ballot(i0 < Wn)) + __popcll(__ballot(i1 < Wn));
       // a shift counts its amount's low five bits only: 16 (i & 1)
-      if (i0 < Wn) atomicAdd(&cs.count[i0 >> 1], 1u << ((i0 << 4) & 31u));
-      if (i1 < Wn) atomicAdd(&cs.count[i1 >> 1], 1u << ((i1 << 4) & 31u));
+      atomicAdd(&cs.count[i0 < Wn ? i0 >> 1 : kWindow / 2 + lane], 1u << ((i0 << 4) & 31u));
+      atomicAdd(&cs.count[i1 < Wn ? i1 >> 1 : kWindow / 2 + lane], 1u << ((i1 << 4) & 31u));
     }
   });
   __syncthreads();
@@ -957,16 +959,19 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
 // ----------------------------------------------------------------------------------
 // fp32, the whole vocabulary's sum (a larger top_k, top_p or no filter): weights are added up by
 // bins of 1/32 octave.  Weight 2^-(z / 32), z = 32 log2(e) (M - x) / T, is the bin's 2^-(b / 32),
-// b = floor z, times a factor 2^-((z - b) / 32) from a short series; a bin adds up its factors
-// (integers of 2^-43), and its sum is that times 2^-(b / 32), rounded down.  The bin where a
-// running sum or count passes its target is then ranked one by one; of one that the list does not
-// hold, 1/1024 is, found the same way, or that has one value only (logits that were bf16 once).
+// b = z rounded to an integer, times a factor 2^-(t / 32), t = z - b, from a short series; a bin
+// adds up its factors (integers of 2^-43), and its sum is that times 2^-(b / 32), rounded down.
+// The bin where a running sum or count passes its target is then ranked one by one; of one that
+// the list does not hold, 1/1024 is, found the same way, or that has one value only (logits that
+// were bf16 once).  b comes from adding 1.5 * 2^52: its low word is the integer.  (Conversions and
+// the fraction of a double run at a quarter of the rate of products: with them, and bins from b to
+// b + 1, the pass over 50257 values took 8.3 us.)
 // False: anything denser, or an infinite maximum or temperature.
 template <int DT, int NT>
 __device__ __attribute__((always_inline)) inline bool sample_binned(
     const Passes<DT, NT>& passes, const Maxima& mx, const Weights& w, const RowSettings& st,
     Shared<DT, NT>& sh, Drawn* out) {
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
   BinScratch& bs = sh.u.b;
   const float M = w.top;
   // differences to an infinite maximum are not 0 even for its equals, and at an infinite
@@ -975,12 +980,15 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   const double scale = kPerOctave * w.scale;
   for (int i = tid; i < kWeightBins; i += NT) bs.mass[i] = 0ull, bs.num[i] = 0u;
   __syncthreads();
+  constexpr double kInt = 6755399441055744.0;   // 1.5 * 2^52
+  constexpr double kDeepest = kWeightBins - 1;   // depths from here on add nothing
   auto depth = [&](float x) -> double { return ((double)M - (double)x) * scale; };
-  auto factor = [&](double z) -> uint64_t {
+  auto offset = [&](double z) -> double { return z - ((z + kInt) - kInt); };
+  auto bin_at = [&](double z) -> int { return (int)__double_as_longlong(z + kInt); };
+  // 2^-(t / 32) to 2^-48 for |t| <= 1/2
+  auto factor = [&](double t) -> uint64_t {
     constexpr double c = -0.69314718055994530942 / kPerOctave;
-    const double t = __builtin_amdgcn_fract(z);
-    double p = scalar(c * c * c * c * c * c / 720.0);
-    p = fma(p, t, scalar(c * c * c * c * c / 120.0));
+    double p = scalar(c * c * c * c * c / 120.0);
     p = fma(p, t, scalar(c * c * c * c / 24.0));
     p = fma(p, t, scalar(c * c * c / 6.0));
     p = fma(p, t, scalar(c * c * 0.5));
@@ -996,18 +1004,19 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       z[q] = depth(__uint_as_float(ww[q]));
-      f[q] = factor(z[q]);
+      f[q] = factor(offset(z[q]));
     }
     // (kept out of the branches, where each would wait for its own chain of products)
     asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]));
+    int at[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (z[q] < (double)kWeightBins)
-        atomicAdd((unsigned long long*)&bs.mass[(int)z[q]], (unsigned long long)f[q]);
+    for (int q = 0; q < 4; ++q) {
+      at[q] = z[q] < kDeepest ? bin_at(z[q]) : kWeightBins + lane;
+      atomicAdd((unsigned long long*)&bs.mass[at[q]], (unsigned long long)f[q]);
+    }
     if (counts) {   // uniform
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (z[q] < (double)kWeightBins) atomicAdd(&bs.num[(int)z[q]], 1u);
+      for (int q = 0; q < 4; ++q) atomicAdd(&bs.num[at[q]], 1u);
     }
   });
   __syncthreads();
@@ -1036,20 +1045,26 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   }
   __syncthreads();
 
-  // f(x, z, index) for the elements whose depth z is in [zlo, zhi)
-  auto within = [&](double zlo, double zhi, auto&& f) {
-    passes.between(mx, bound_below((double)M - zhi / scale, M),
-                   -bound_below(zlo / scale - (double)M, M), sh, [&](float x, int e) {
-                     const double z = depth(x);
-                     if (z >= zlo && z < zhi) f(x, z, e);
+  // the part of its bin that an element with offset t is in
+  auto sub_at = [&](double t) -> int { return min((int)((t + 0.5) * kSub), kSub - 1); };
+  // f(x, z, t, index) for the elements of a bin's parts lo .. hi
+  auto within = [&](int bin, int lo, int hi, auto&& f) {
+    const double z0 = (double)bin - 0.5;
+    passes.between(mx, bound_below((double)M - (z0 + (double)(hi + 1) / kSub) / scale, M),
+                   -bound_below((z0 + (double)lo / kSub) / scale - (double)M, M), sh,
+                   [&](float x, int e) {
+                     const double z = depth(x), t = offset(z);
+                     if (!(z < kDeepest) || bin_at(z) != bin) return;
+                     const int i = sub_at(t);
+                     if (i >= lo && i <= hi) f(x, z, t, e);
                    });
     __syncthreads();
   };
-  // list[] from the elements whose depth is in [zlo, zhi); their number
-  auto collect = [&](double zlo, double zhi) -> uint32_t {
+  // list[] from the elements of a bin's parts lo .. hi; their number
+  auto collect = [&](int bin, int lo, int hi) -> uint32_t {
     __syncthreads();
     if (tid == 0) sh.n = 0u;
-    within(zlo, zhi, [&](float x, double, int e) {
+    within(bin, lo, hi, [&](float x, double, double, int e) {
       const uint32_t i = atomicAdd(&sh.n, 1u);
       if (i < (uint32_t)kList)
         bs.l.list[i] = cand_key(value_key(__float_as_uint(x)), (uint32_t)e);
@@ -1077,17 +1092,17 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     const uint64_t before = bs.mass[bin];
     // the running sum after the bin's factors c
     auto through = [&](uint64_t c) -> uint64_t { return before + (uint64_t)(bsc * (double)c); };
-    double zlo = (double)bin, zhi = (double)(bin + 1);
-    uint64_t c0 = 0;                      // factors and elements of the bin before the list
+    int sub0 = 0, sub1 = kSub - 1;
+    uint64_t c0 = 0;                      // factors of the bin, elements, before the list
     uint32_t n0 = bs.num[bin];
-    uint32_t n = collect(zlo, zhi);
+    uint32_t n = collect(bin, sub0, sub1);
     if (n > (uint32_t)kList) {
       __syncthreads();
       for (int i = tid; i < kSub; i += NT) bs.sub[i] = 0ull, bs.sub_num[i] = 0u;
       __syncthreads();
-      within(zlo, zhi, [&](float, double z, int) {
-        const int i = (int)(__builtin_amdgcn_fract(z) * kSub);
-        atomicAdd((unsigned long long*)&bs.sub[i], (unsigned long long)factor(z));
+      within(bin, sub0, sub1, [&](float, double, double t, int) {
+        const int i = sub_at(t);
+        atomicAdd((unsigned long long*)&bs.sub[i], (unsigned long long)factor(t));
         atomicAdd(&bs.sub_num[i], 1u);
       });
       constexpr int E = kSub / NT;
@@ -1114,20 +1129,19 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
         nrun += k[e];
       }
       __syncthreads();
-      zlo += (double)sh.out32[1] / kSub;
-      zhi = zlo + 1.0 / kSub;
+      sub0 = sub1 = (int)sh.out32[1];
       n0 = sh.out32[2];
       c0 = sh.out64[0];
-      n = collect(zlo, zhi);
+      n = collect(bin, sub0, sub1);
     }
     if (n > (uint32_t)kList) {   // more than the list holds: equals?
       const uint32_t key = (uint32_t)(bs.l.list[0] >> 32);
       if (tid == 0) sh.out32[3] = 0u;
-      within(zlo, zhi, [&](float x, double, int) {
+      within(bin, sub0, sub1, [&](float x, double, double, int) {
         if (value_key(__float_as_uint(x)) != key) sh.out32[3] = 1u;
       });
       if (sh.out32[3]) return false;
-      const uint64_t W = factor(depth(key_value(key)));
+      const uint64_t W = factor(offset(depth(key_value(key))));
       uint32_t nth = (uint32_t)(target - n0);
       if (!by_count) {
         uint32_t hi = n - 1;   // the crossing one is in [nth, hi]
@@ -1146,7 +1160,7 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     }
     sort_list<DT, NT>(n, sh);
     sum_list<DT, NT>(
-        n, sh, [&](uint32_t key) { return factor(depth(key_value(key))); },
+        n, sh, [&](uint32_t key) { return factor(offset(depth(key_value(key)))); },
         [&](uint64_t c) { return through(c0 + c); });
     const uint32_t i = by_count ? (uint32_t)(target - n0) : first_above<DT, NT>(target, n, sh);
     const uint64_t e = bs.l.sorted[i];
@@ -1161,11 +1175,11 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   uint64_t Sm = S;
   if (st.mp > 0.f) {
     const double last = -kPerOctave * st.least();   // the depth of the last one kept
-    if (last < (double)kWeightBins) {
-      const int bin = (int)last;
+    if (last < kDeepest) {
+      const int bin = bin_at(last);
       uint64_t c = 0;   // of the bin, what is kept
-      within((double)bin, (double)(bin + 1), [&](float, double z, int) {
-        if (z <= last) c += factor(z);
+      within(bin, 0, kSub - 1, [&](float, double z, double t, int) {
+        if (z <= last) c += factor(t);
       });
       c = block_sum_u64<Shared<DT, NT>, NT>(c, sh);
       Sm = bs.mass[bin] + (uint64_t)(bin_scale(bin) * (double)c);
@@ -1190,7 +1204,8 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     if (step < 2) kept = f.through;
   }
   out->token = f.token >= 0 ? f.token : nth_index<DT, NT>(passes.row, f.key, f.nth, sh);
-  out->prob = (float)(bin_scale(f.bin) * (double)factor(depth(key_value(f.key))) / (double)kept);
+  out->prob = (float)(bin_scale(f.bin) * (double)factor(offset(depth(key_value(f.key)))) /
+                      (double)kept);
   return true;
 }
 
