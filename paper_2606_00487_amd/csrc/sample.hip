@@ -464,7 +464,7 @@ __device__ inline u16x2 keys16(uint32_t w) {
 // caches, and most of them read only the units of the threads that hold values above a bound.
 // (Registers for a row of 150000 bf16 values leave too few for the passes: at every share kept
 // there, the compiler spilled as much.)
-constexpr int kAhead = 8;
+constexpr int kAhead = 4;
 constexpr int kParts = 4;   // a thread's unit j counts to its part j % kParts
 static_assert(kAhead % kParts == 0, "a unit's part is known when the loop is unrolled");
 struct Maxima {
@@ -483,23 +483,36 @@ struct Passes {
     full = (x.vocab - head) / U;
   }
   __device__ inline const char* first() const { return row.base + (int64_t)head * (16 / U); }
-  // f(unit's 16 bytes, index of its first element, part); the trip count is the workgroup's
-  template <class F>
+  // f(unit's 16 bytes, index of its first element, part); the trip count is the workgroup's.
+  // A unit's registers take the one kAhead later as soon as it is done with: loads past the row
+  // read its last unit.  (kAhead loads, all waited for, then their work: the memory idles while a
+  // workgroup works.)
+  template <int A, class F>
   __device__ __attribute__((always_inline)) inline void units(F&& f) const {
-    const int tid = threadIdx.x;
-    const uint32_t last = (uint32_t)(full - 1) * 16u;   // a row is below 2^32 bytes
-    const char* const p = first();
-    for (int u0 = 0; u0 < full; u0 += kAhead * NT) {
-      uint4 x[kAhead];
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));   // (or the addresses of every pass are kept from the start)
+    if (full > 0) {
+      const uint32_t last = (uint32_t)(full - 1) * 16u;   // a row is below 2^32 bytes
+      const char* const p = first();
+      auto load = [&](int u) { return *(const uint4*)(p + min((uint32_t)u * 16u, last)); };
+      uint4 x[A];
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j)
-        if (u0 + j * NT < full)   // uniform
-          x[j] = *(const uint4*)(p + min((uint32_t)(u0 + j * NT + tid) * 16u, last));
+      for (int j = 0; j < A; ++j) x[j] = load(j * NT + tid);
+      int u0 = 0;
+      for (; u0 + A * NT <= full; u0 += A * NT) {
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
+        for (int j = 0; j < A; ++j) {
+          const int u = u0 + j * NT + tid;
+          f(x[j], u * U + head, j % kParts);
+          x[j] = load(u + A * NT);
+          __builtin_amdgcn_sched_barrier(0);   // (or the loads gather at the loop's end)
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < A; ++j) {
         if (u0 + j * NT >= full) break;
         const int u = u0 + j * NT + tid;
-        if (u0 + (j + 1) * NT > full && u >= full) x[j] = make_uint4(kNone, kNone, kNone, kNone);
+        if (u >= full) x[j] = make_uint4(kNone, kNone, kNone, kNone);
         f(x[j], u * U + head, j % kParts);
       }
     }
@@ -518,6 +531,38 @@ struct Passes {
                           : ((const uint32_t*)row.base)[e];
     f(make_uint4(b, kNone, kNone, kNone), max(e, 0), 0);
   }
+  __device__ static inline u16x2 unit_max(const uint4& w) {
+    return __builtin_elementwise_max(__builtin_elementwise_max(keys16(w.x), keys16(w.y)),
+                                     __builtin_elementwise_max(keys16(w.z), keys16(w.w)));
+  }
+  // false (in all threads) where a positive NaN is among the workgroup's largest keys
+  __device__ static inline bool from_keys(const u16x2 (&mk)[kParts], Maxima* m) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < kParts; ++s) {
+      const uint32_t k = max((uint32_t)mk[s][0], (uint32_t)mk[s][1]);
+      top = max(top, k);
+      // -inf's key is 0x7F (smaller: NaN or nothing)
+      m->part[s] = k > 0x7Fu ? key_value(key32(k)) : -INFINITY;
+    }
+    m->all = fmaxf(fmaxf(m->part[0], m->part[1]), fmaxf(m->part[2], m->part[3]));
+    return !__syncthreads_or(top > 0xFF80u);   // +inf's key
+  }
+  // The largest value of the first units, kAhead per thread; NaN where a positive NaN is there
+  __device__ __attribute__((always_inline)) inline float first_max(Shared<DT, NT>& sh) const {
+    u16x2 mk[kParts] = {};
+    uint4 x[kAhead];
+    const char* const p = first();
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      x[j] = *(const uint4*)(p + min((uint32_t)(j * NT + (int)threadIdx.x), (uint32_t)(full - 1)) * 16u);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      mk[j % kParts] = __builtin_elementwise_max(mk[j % kParts], unit_max(x[j]));
+    Maxima m;
+    if (!from_keys(mk, &m)) return NAN;
+    return block_max_f32<Shared<DT, NT>, NT>(m.all, sh);
+  }
   // The largest values of this thread's units (NaN left out; -inf where there is none).  bf16:
   // the largest 16-bit key, two at a time (three instructions; as floats the halves would be
   // unpacked and made quiet first, five); a positive NaN in any unit sends the workgroup through
@@ -527,26 +572,15 @@ struct Passes {
     bool done = false;
     if constexpr (DT == TAPS_BF16) {
       u16x2 mk[kParts] = {};
-      units([&](const uint4& w, int, int s) {
-        mk[s] = __builtin_elementwise_max(
-            mk[s],
-            __builtin_elementwise_max(__builtin_elementwise_max(keys16(w.x), keys16(w.y)),
-                                      __builtin_elementwise_max(keys16(w.z), keys16(w.w))));
+      units<8>([&](const uint4& w, int, int s) {
+        mk[s] = __builtin_elementwise_max(mk[s], unit_max(w));
       });
-      uint32_t top = 0;
-#pragma unroll
-      for (int s = 0; s < kParts; ++s) {
-        const uint32_t k = max((uint32_t)mk[s][0], (uint32_t)mk[s][1]);
-        top = max(top, k);
-        // -inf's key is 0x7F (smaller: NaN or nothing)
-        m.part[s] = k > 0x7Fu ? key_value(key32(k)) : -INFINITY;
-      }
-      done = !__syncthreads_or(top > 0xFF80u);   // +inf's key
+      done = from_keys(mk, &m);
     }
     if (!done) {
 #pragma unroll
       for (int s = 0; s < kParts; ++s) m.part[s] = -INFINITY;
-      units([&](const uint4& w, int, int s) {
+      units<DT == TAPS_FP32 ? 8 : 4>([&](const uint4& w, int, int s) {
         const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
         // (compared and selected: the compiler leaves operands of a maximum of three unquieted,
         // and a signalling NaN among them becomes the result)
@@ -614,7 +648,7 @@ struct Passes {
     constexpr int kAll = kParts * NT;
     const int n = (int)sh.n_hot, per = (full + kAll - 1) / kAll;
     if (2 * n > kAll) {
-      units(one);
+      units<4>(one);
       return;
     }
     for (int i = tid; i < n * per; i += NT) {
@@ -764,23 +798,35 @@ __device__ __attribute__((always_inline)) inline bool sample_listed(
 // ----------------------------------------------------------------------------------
 // bf16: a row holds few distinct values, so the elements are counted by value (16-bit keys from
 // the largest down, as far as weights reach) and every sum is over values: one exponential per
-// value that occurs, none per element, and a crossing is exact at once.  Returns false where
-// the window is too wide or a value occurs 65536 times.
-// 16 bits per count let two workgroups share a CU's LDS.
+// value that occurs, none per element, and a crossing is exact at once.
+// Without a known maximum the row is read once: the window's upper end lies above the largest of
+// the first values by a factor of 256 (1024 keys), or by 64, and the pass finds the maximum as it
+// counts.
+// Returns false where the window is too wide, a value lies above it or occurs 65536 times, or a
+// positive NaN takes part.  16 bits per count let two workgroups share a CU's LDS.
 template <int DT, int NT>
 __device__ __attribute__((always_inline)) inline bool sample_counted(
-    const Passes<DT, NT>& passes, const Maxima& mx, const Weights& w, const RowSettings& st,
+    const Passes<DT, NT>& passes, Maxima& mx, bool known, float M, const RowSettings& st,
     Shared<DT, NT>& sh, Drawn* out) {
   constexpr int kWaves = NT / kWave;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  const uint32_t kM = w.key >> 16;
+  Weights w{M, 0u, 1.4426950408889634074 / (double)st.T};
   CountScratch& cs = sh.u.c;
+  if (!known) {
+    if (passes.full == 0) return false;
+    M = passes.first_max(sh);
+    if (!(M > -INFINITY)) return false;
+  }
   // down to the values whose weight rounds to 0 (two more: the bound is rounded to bf16)
-  const float low = (float)((double)w.top - 44.5 / w.scale);
+  const float low = (float)((double)M - 44.5 / w.scale);
   uint32_t klow = low > -INFINITY ? key16(low) : 0u;
   klow = klow > kLowest16 + 2u ? klow - 2u : kLowest16;
   if (klow == 0x8000u) klow = 0x7FFFu;   // +0 and -0 are equal
-  klow = min(klow, kM);
+  klow = min(klow, key16(M));
+  uint32_t kM = key16(M);   // the window's upper end
+  if (!known) {
+    kM = min(max(kM + 1024u, key16(M + 64.f)), 0xFF80u);   // +inf's key
+  }
   const uint32_t Wn = kM - klow + 1u;
   if (Wn > (uint32_t)kWindow) return false;
   const int runs = (int)((Wn + kRun - 1) / kRun);
@@ -788,13 +834,16 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
     ((uint4*)cs.count)[i] = make_uint4(0u, 0u, 0u, 0u);
   __syncthreads();
   uint32_t in_window = 0;   // of the wave
-  passes.units([&](const uint4& v, int, int) {
+  u16x2 mk[kParts] = {};
+  passes.template units<4>([&](const uint4& v, int, int s) {
     const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
     const u16x2 top = {(unsigned short)kM, (unsigned short)kM};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       // NaN keys fall outside the window
-      const uint32_t idx = __builtin_bit_cast(uint32_t, (u16x2)(top - keys16(ww[q])));
+      const u16x2 k = keys16(ww[q]);
+      mk[s] = __builtin_elementwise_max(mk[s], k);
+      const uint32_t idx = __builtin_bit_cast(uint32_t, (u16x2)(top - k));
       const uint32_t i0 = idx & 0xFFFFu, i1 = idx >> 16;
       in_window += __popcll(__ballot(i0 < Wn)) + __popcll(__ballot(i1 < Wn));
       // a shift counts its amount's low five bits only: 16 (i & 1)
@@ -802,6 +851,14 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
       atomicAdd(&cs.count[i1 < Wn ? i1 >> 1 : kWindow / 2 + lane], 1u << ((i1 << 4) & 31u));
     }
   });
+  if (!known) {
+    if (!passes.from_keys(mk, &mx)) return false;
+    M = block_max_f32<Shared<DT, NT>, NT>(mx.all, sh);
+    if (key16(M) > kM) return false;
+  }
+  if (M == 0.f) M = 0.f;   // not -0
+  w.top = M;
+  w.key = value_key(__float_as_uint(M));
   __syncthreads();
   auto count_at = [&](uint32_t i) -> uint32_t {
     return (cs.count[i >> 1] >> (16 * (i & 1u))) & 0xFFFFu;
@@ -996,7 +1053,7 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     return fixed43(fma(p, t, scalar(513.0)));
   };
   const bool counts = st.k > 0;
-  passes.units([&](const uint4& v, int, int) {
+  passes.template units<4>([&](const uint4& v, int, int) {
     const uint32_t ww[4] = {v.x, v.y, v.z, v.w};
     double z[4];
     uint64_t f[4];
@@ -1226,17 +1283,26 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(
   const Row<DT> row((const char*)logits + (size_t)r * row_bytes, vocab);
   const Passes<DT, NT> passes(row);
   RowSettings st;
-  st.T = s.temperature ? s.temperature[b] : 1.f;
-  st.k = s.top_k ? s.top_k[b] : 0;
-  st.p = s.top_p ? s.top_p[b] : 1.f;
-  st.mp = s.min_p ? s.min_p[b] : 0.f;
-  st.u = u[r];
-  const Maxima mx = passes.max_value();
-  float M = block_max_f32<Shared<DT, NT>, NT>(mx.all, sh);
-  if (M == 0.f) M = 0.f;   // not -0
+  auto uniform = [](float x) {
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+  };
+  st.T = uniform(s.temperature ? s.temperature[b] : 1.f);
+  st.k = __builtin_amdgcn_readfirstlane(s.top_k ? s.top_k[b] : 0);
+  st.p = uniform(s.top_p ? s.top_p[b] : 1.f);
+  st.mp = uniform(s.min_p ? s.min_p[b] : 0.f);
+  st.u = uniform(u[r]);
   Drawn d;
   bool done = false;
-  if (M > -INFINITY) {
+  const bool listed = st.few() || st.cut_by_min_p();
+  Maxima mx;
+  float M = 0.f;
+  // The largest value, and with it greedy rows and the ranked few; false: nothing is left to do
+  // here
+  auto with_max = [&]() -> bool {
+    mx = passes.max_value();
+    M = block_max_f32<Shared<DT, NT>, NT>(mx.all, sh);
+    if (M == 0.f) M = 0.f;   // not -0
+    if (!(M > -INFINITY)) return false;
     if (!(st.T > 0.f)) {
       if (tid == 0) sh.n = 0xFFFFFFFFu;
       __syncthreads();
@@ -1244,20 +1310,27 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(
       __syncthreads();
       d = {(int)sh.n, 1.f};
       done = true;
-    } else {
+    } else if (listed) {
       const Weights w{M, value_key(__float_as_uint(M)), 1.4426950408889634074 / (double)st.T};
-      if (st.few() || st.cut_by_min_p())
-        done = sample_listed<DT, NT>(passes, mx, w, st, sh, &d);
-      if constexpr (DT == TAPS_BF16) {
-        if (!done) {
-          __syncthreads();
-          done = sample_counted<DT, NT>(passes, mx, w, st, sh, &d);
-        }
-      } else if (!done) {
-        __syncthreads();
-        done = sample_binned<DT, NT>(passes, mx, w, st, sh, &d);
-      }
+      done = sample_listed<DT, NT>(passes, mx, w, st, sh, &d);
+      __syncthreads();
     }
+    return !done;
+  };
+  if constexpr (DT == TAPS_BF16) {
+    // rows whose whole sum counts are read once, and again only where that fails
+    for (int known = __builtin_amdgcn_readfirstlane(st.T > 0.f && !listed ? 0 : 1);; known = 1) {
+      // (or the compiler lays the loop out twice, and evaluates before it all that any path
+      // makes of the settings)
+      asm volatile("" : "+s"(known), "+s"(st.T), "+s"(st.p), "+s"(st.mp), "+s"(st.u), "+s"(st.k));
+      if (known && !with_max()) break;
+      done = sample_counted<DT, NT>(passes, mx, known != 0, M, st, sh, &d);
+      if (done || known) break;
+      __syncthreads();
+    }
+  } else if (with_max()) {
+    const Weights w{M, value_key(__float_as_uint(M)), 1.4426950408889634074 / (double)st.T};
+    done = sample_binned<DT, NT>(passes, mx, w, st, sh, &d);
   }
   if (!done) {   // uniform
     __syncthreads();
