@@ -458,15 +458,13 @@ __device__ inline u16x2 keys16(uint32_t w) {
   return __builtin_bit_cast(u16x2, w ^ (sign | 0x80008000u));
 }
 
-// Passes over a row: its whole aligned 16-byte units, kAhead of them in flight per thread, and
+// Passes over a row: its whole aligned 16-byte units, several of them in flight per thread, and
 // the elements of its unaligned ends, one per thread.  Places without an element are negative
 // NaN, whose key is the smallest and which no pass counts.  A row is read from HBM once; the passes after the first find it in the
 // caches, and most of them read only the units of the threads that hold values above a bound.
 // (Registers for a row of 150000 bf16 values leave too few for the passes: at every share kept
 // there, the compiler spilled as much.)
-constexpr int kAhead = 4;
 constexpr int kParts = 4;   // a thread's unit j counts to its part j % kParts
-static_assert(kAhead % kParts == 0, "a unit's part is known when the loop is unrolled");
 struct Maxima {
   float part[kParts], all;   // largest values of the parts, and of all
 };
@@ -484,13 +482,14 @@ struct Passes {
   }
   __device__ inline const char* first() const { return row.base + (int64_t)head * (16 / U); }
   // f(unit's 16 bytes, index of its first element, part); the trip count is the workgroup's.
-  // A unit's registers take the one kAhead later as soon as it is done with: loads past the row
-  // read its last unit.  (kAhead loads, all waited for, then their work: the memory idles while a
-  // workgroup works.)
+  // A unit's registers take the one A later as soon as it is done with; loads past the row read
+  // its last unit.  (A loads, all waited for, then their work: the memory idles meanwhile.  A 8
+  // where a unit is little work, 4 otherwise; 16 and 8 take as long.)
   template <int A, class F>
   __device__ __attribute__((always_inline)) inline void units(F&& f) const {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));   // (or the addresses of every pass are kept from the start)
+    static_assert(A % kParts == 0, "a unit's part is known when the loop is unrolled");
     if (full > 0) {
       const uint32_t last = (uint32_t)(full - 1) * 16u;   // a row is below 2^32 bytes
       const char* const p = first();
@@ -548,17 +547,10 @@ struct Passes {
     m->all = fmaxf(fmaxf(m->part[0], m->part[1]), fmaxf(m->part[2], m->part[3]));
     return !__syncthreads_or(top > 0xFF80u);   // +inf's key
   }
-  // The largest value of the first units, kAhead per thread; NaN where a positive NaN is there
+  // The largest value of the first units, one per thread; NaN where a positive NaN is there
   __device__ __attribute__((always_inline)) inline float first_max(Shared<DT, NT>& sh) const {
     u16x2 mk[kParts] = {};
-    uint4 x[kAhead];
-    const char* const p = first();
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      x[j] = *(const uint4*)(p + min((uint32_t)(j * NT + (int)threadIdx.x), (uint32_t)(full - 1)) * 16u);
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      mk[j % kParts] = __builtin_elementwise_max(mk[j % kParts], unit_max(x[j]));
+    mk[0] = unit_max(*(const uint4*)(first() + min((uint32_t)threadIdx.x, (uint32_t)(full - 1)) * 16u));
     Maxima m;
     if (!from_keys(mk, &m)) return NAN;
     return block_max_f32<Shared<DT, NT>, NT>(m.all, sh);
