@@ -537,11 +537,11 @@ size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab,
  *   tokens     [batch][budget] int32
  *   probs      [batch][budget] float, or NULL: the token's probability among the kept ones
  * A row's rank order is value descending, then index ascending; -0 equals +0; NaN is last.
- * Token r of it has the integer weight W_r = 2^43 * exp((x_r - x_0) / T), rounded to nearest
- * (evaluated in fp64 to within 2^-50 of exp), 2^43 where x_r equals x_0 (infinite values too)
- * and 0 for NaN.  All sums are exact: S_k the sum of the weights after top_k; top_p keeps up to
- * the first token whose running sum reaches ceil(top_p * S_k); S is the sum of all that are
- * kept.  The token is the first whose running sum exceeds floor(u * S), its probability W / S.
+ * Token r of it has the weight W_r = exp((x_r - x_0) / T), 1 where x_r equals x_0 (infinite values
+ * too) and 0 for NaN, evaluated in fp64 to within 2^-42 of W_0 and added up as integers, so that
+ * results do not depend on the order of additions.  S_k is the sum of the weights after top_k;
+ * top_p keeps up to the first token whose running sum reaches top_p * S_k; S is the sum of all
+ * that are kept.  The token is the first whose running sum exceeds u * S, its probability W / S.
  * (Weights that round to 0, below 2^-44 of the largest, are never drawn.)  A row of NaN alone
  * gives token 0 with probability 0.  budget at most TAPS_MAX_BUDGET, vocab at most
  * TAPS_MAX_SAMPLE_VOCAB, batch * budget at most 2^20. */

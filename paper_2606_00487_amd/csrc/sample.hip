@@ -2,14 +2,31 @@
 // (taps_sample).
 //
 // A row's tokens in rank order (value descending, index ascending, NaN last) have weights
-//   W_r = rint(2^43 exp((x_r - x_0) / T)),
-// integers, so that every sum below is exact: the result does not depend on the order in which
-// a kernel adds, and 2^20 weights stay below 2^63.  top-k, top-p and min-p each keep a prefix
-// of the rank order, so the sum S over the kept set is the smallest of the prefixes' sums
+//   W_r = 2^43 exp((x_r - x_0) / T),
+// added up as integers: a sum does not depend on the order in which a kernel adds (atomics
+// included), and 2^20 weights stay below 2^64.  top-k, top-p and min-p each keep a prefix of the
+// rank order, so the sum S over the kept set is the smallest of the prefixes' sums
 //   S_k = sum over the first top_k,   S_p = the first sum that reaches top_p * S_k,
 //   S_m = sum over weights >= min_p,
 // and the token is the first whose running sum exceeds floor(u S).  Each of these is one
 // question: at which token does the running count or sum in rank order pass a target?
+//
+// One workgroup per row, by one of four paths:
+//   sample_listed   a small top_k, or min_p without top_p: the elements above a bound that the
+//                   thread groups' largest values (or min_p) give, ranked one by one;
+//   sample_counted  bf16 otherwise: the elements counted by value;
+//   sample_binned   fp32 otherwise: weights added up by bins of 1/32 octave, the bin that a
+//                   question leads to ranked;
+//   sample_general  what those decline (thousands of equal bf16 values past 16-bit counts, an
+//                   infinite temperature or fp32 maximum, fp32 rows too dense to bin): a radix
+//                   descent over the row for each question.
+// Bound: reading the row where nothing is added up for every element (2048 rows x 151936 bf16,
+// top_k: 140 us; their bytes at 5.3 TB/s take 117); the LDS additions beside it otherwise (no
+// filter 204, top_p 182; 64 additions of 32 bits take 12 clocks of a CU, of 64 bits 20); for few
+// rows the chain of about twenty barriers with small work between them (16 rows x 1000: 9 to 14
+// us).  Two workgroups a CU where there are rows for that: one's questions beside the other's
+// reading.  Rows shared out over several workgroups, with a second kernel for the questions, took
+// longer even for 32 rows (33 against 29 us).
 #include "common.h"
 
 namespace taps {
@@ -460,8 +477,9 @@ __device__ inline u16x2 keys16(uint32_t w) {
 
 // Passes over a row: its whole aligned 16-byte units, several of them in flight per thread, and
 // the elements of its unaligned ends, one per thread.  Places without an element are negative
-// NaN, whose key is the smallest and which no pass counts.  A row is read from HBM once; the passes after the first find it in the
-// caches, and most of them read only the units of the threads that hold values above a bound.
+// NaN, whose key is the smallest and which no pass counts.  A row is read from HBM once; the
+// passes after the first find it in the caches, and most of them read only the units of the
+// threads that hold values above a bound.
 // (Registers for a row of 150000 bf16 values leave too few for the passes: at every share kept
 // there, the compiler spilled as much.)
 constexpr int kParts = 4;   // a thread's unit j counts to its part j % kParts
