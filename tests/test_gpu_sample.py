@@ -270,3 +270,34 @@ def test_extreme_temperatures(dtype, T):
     x[0, 3, :2000] = -INF
     for k, p, m in ((0, 1.0, 0.0), (0, 0.6, 0.0), (300, 1.0, 0.0), (300, 0.5, 0.0), (0, 1.0, 0.999), (5, 0.9, 0.5)):
         check(x, uniform(43, 1, 6), None, [T], [k], [p], [m])
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("rows", [8, 264])
+def test_late_largest_values(dtype, rows):
+    """Rows whose first values say little about the largest: masked, tiny, negative, NaN, or
+    thousands of times smaller than a later one."""
+    V = 20000
+    x = normal(50, 1, 8, V, dtype)
+    x[0, 0, :15000] = -INF
+    x[0, 1, :15000] = torch.finfo(dtype).min
+    x[0, 2, :15000] *= 1e-6
+    x[0, 3, :] = -x[0, 3].abs() * 100
+    x[0, 3, 17000:17010] = -0.0
+    x[0, 4, 19990] = 60000.0
+    x[0, 4, 19991:] = 59904.0
+    x[0, 5, :15000] = NAN
+    x[0, 6, :] *= 1e-3
+    x[0, 6, 12345], x[0, 6, 18001] = 500.0, 500.0
+    x[0, 7, :15000], x[0, 7, 15000:] = -1e30, x[0, 7, 15000:] - 1e4
+    B = rows // 8
+    xs, u = x.repeat(B, 1, 1), uniform(51, B, 8)
+    u[1:] = u[0]                               # (one oracle row stands for its repeats)
+    for T, k, p, m in ((1.0, 0, 1.0, 0.0), (1.0, 0, 0.9, 0.0), (0.3, 900, 0.95, 0.0), (2.0, 0, 0.9, 0.02)):
+        want, wp = check(x, u[:1], None, [T], [k], [p], [m])
+        if B > 1:
+            op = taps.TokenSampler(B, 8, V, dtype=taps.BF16 if dtype == BF else taps.FP32)
+            full = lambda v, t=torch.float32: torch.full((B,), v, dtype=t, device="cuda")  # noqa: E731
+            tok, pr = op(xs, dev(u), None, temperature=full(T), top_k=full(k, torch.int32),
+                         top_p=full(p), min_p=full(m))
+            assert torch.equal(tok, want.expand(B, 8)) and torch.equal(pr, wp.expand(B, 8))
