@@ -30,6 +30,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "scan.h"
 
 namespace taps {
 namespace {
@@ -231,16 +232,7 @@ __device__ inline int len_of(const int32_t* lenp, int b, int max_len) {
 }
 __device__ inline int units_of(int len) { return (len + kUnit - 1) / kUnit; }
 
-// inclusive prefix sum over the lanes of a wave (DPP row shifts, then row broadcasts)
-__device__ inline int wave_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr:1
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);  // row_shr:2
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);  // row_shr:4
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);  // row_shr:8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast:15
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast:31
-  return v;
-}
+__device__ inline int wave_scan(int v) { return (int)wave_scan_u32((uint32_t)v); }
 
 // first unit of part j when `total` units are cut into `parts`
 __device__ inline int part_begin(int j, int total, int parts) {

@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "scan.h"
 
 namespace taps {
 
@@ -52,11 +53,6 @@ __device__ inline Lengths lengths(const int32_t* held, const int32_t* ctx, const
   return r;
 }
 
-__device__ inline int64_t shfl_up_i64(int64_t v, int d) {
-  const uint32_t lo = __shfl_up((uint32_t)v, d), hi = __shfl_up((uint32_t)((uint64_t)v >> 32), d);
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
 __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(
     int32_t* __restrict__ table, int max_pages, const int32_t* __restrict__ held,
     const int32_t* __restrict__ ctx, const int32_t* __restrict__ nnew, int batch, int run,
@@ -89,12 +85,8 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(
     s_want[j] = r.want;
     s_rel[j] = ((int64_t)r.rel << 32) | (uint32_t)r.need;   // both for the second loop
   }
-  int64_t irel = rel, ineed = need;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int64_t a = shfl_up_i64(irel, d), c = shfl_up_i64(ineed, d);
-    if (lane >= d) irel += a, ineed += c;
-  }
+  int64_t irel = (int64_t)wave_scan_u64((uint64_t)rel);
+  int64_t ineed = (int64_t)wave_scan_u64((uint64_t)need);
   if (lane == kWave - 1) s_wave[0][wave] = irel, s_wave[1][wave] = ineed;
   __syncthreads();
   int64_t rel_all = 0, need_all = 0;
