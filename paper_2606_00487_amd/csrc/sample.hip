@@ -169,7 +169,7 @@ struct Shared {
   PathScratch<DT> u;
   uint32_t group[kGroups];
   uint64_t red[NT / kWave];
-  uint32_t red32[NT / kWave];
+  uint32_t red32[NT / kWave], other32[NT / kWave];
   uint64_t out64[2];
   uint32_t out32[4];
   uint32_t n, n_hot;
@@ -582,7 +582,8 @@ struct Passes {
     m.all = fmaxf(fmaxf(m.part[0], m.part[1]), fmaxf(m.part[2], m.part[3]));
     return m;
   }
-  // f(value, index) for the elements with lo <= value <= hi: only the parts (of a thread's
+  // f(values, whether each has lo <= value <= hi, index of the first) for the units that hold such
+  // elements: only the parts (of a thread's
   // units) whose largest value reaches lo can hold one.  They are shared out to all threads;
   // where they are most of the parts, every unit is read.  Callers synchronize before the next
   // call.  (Whole threads instead of quarters: with 60 of 512 threads in question, their units
@@ -627,10 +628,7 @@ struct Passes {
         in[q] = x[q] >= lo && x[q] <= hi;
         any |= in[q];
       }
-      if (!any) return;
-#pragma unroll
-      for (int q = 0; q < U; ++q)
-        if (in[q]) f(x[q], e0 + q);
+      if (any) f(x, in, e0);
     };
     constexpr int kAll = kParts * NT;
     const int n = (int)sh.n_hot, per = (full + kAll - 1) / kAll;
@@ -638,6 +636,7 @@ struct Passes {
       units<4>(one);
       return;
     }
+    // (neighbours take the same unit of their parts, whose cache lines many parts share)
     for (int i = tid; i < n * per; i += NT) {
       const int j = i / n, u = j * kAll + (int)sh.hot[i - j * n];
       if (u < full) one(*(const uint4*)(first() + (int64_t)u * 16), u * U + head, 0);
@@ -645,6 +644,44 @@ struct Passes {
     ends(one);
   }
 };
+
+// For `between`: f(value, index) element by element, which is the faster where units hold few
+template <class F>
+__device__ inline auto each(F&& f) {
+  return [f](const auto& x, const auto& in, int e0) {
+    constexpr int U = sizeof(in) / sizeof(in[0]);
+#pragma unroll
+    for (int q = 0; q < U; ++q)
+      if (in[q]) f(x[q], e0 + q);
+  };
+}
+
+// ... and a unit's elements into list[], past which sh.n only counts: one addition per wave, not
+// one per element, where many come at once (16 rows x 1000: 12.6 -> 9.7 us with the bound below)
+template <int DT, int NT, int U>
+__device__ inline void append(Shared<DT, NT>& sh, const float (&x)[U], const bool (&in)[U], int e0) {
+  uint64_t m[U];
+  uint32_t num = 0;
+#pragma unroll
+  for (int q = 0; q < U; ++q) {
+    m[q] = __ballot(in[q]);
+    num += (uint32_t)__popcll(m[q]);
+  }
+  const uint64_t active = __ballot(true);
+  uint32_t at = 0;
+  if ((threadIdx.x & (kWave - 1)) == (uint32_t)__ffsll((long long)active) - 1u)
+    at = atomicAdd(&sh.n, num);
+  at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+  for (int q = 0; q < U; ++q) {
+    if (!m[q]) continue;   // uniform
+    const uint32_t i = at + __builtin_amdgcn_mbcnt_hi(
+                                (uint32_t)(m[q] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m[q], 0u));
+    if (in[q] && i < (uint32_t)kList)
+      sh.u.l.list[i] = cand_key(value_key(__float_as_uint(x[q])), (uint32_t)(e0 + q));
+    at += (uint32_t)__popcll(m[q]);
+  }
+}
 
 // A key that at least k elements reach: the k-th largest of the maxima of kGroups groups of
 // threads (0 where fewer groups hold a value).  k <= kFewTopK.
@@ -660,17 +697,25 @@ __device__ inline uint32_t top_k_bound(float mx, int k, Shared<DT, NT>& sh) {
   uint32_t g[kGroups / kWave];
 #pragma unroll
   for (int i = 0; i < kGroups / kWave; ++i) g[i] = sh.group[i * kWave + lane];
+  // the key's upper 16 bits, a wave for each candidate of the next 3 or 4 (for fp32 rows the bound
+  // comes out a little low)
+  constexpr int kWaves = NT / kWave, kBits = kWaves == 16 ? 4 : 3;
+  static_assert(kWaves == 1 << kBits, "a wave per candidate");
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   uint32_t T = 0;
-  for (int bit = 30; bit >= (DT == TAPS_BF16 ? 16 : 0); bit -= 2) {   // two bits a step
-    const uint32_t c1 = T | (1u << bit), c2 = T | (2u << bit), c3 = T | (3u << bit);
-    int n1 = 0, n2 = 0, n3 = 0;
 #pragma unroll
-    for (int i = 0; i < kGroups / kWave; ++i) {
-      n1 += __popcll(__ballot(g[i] >= c1));
-      n2 += __popcll(__ballot(g[i] >= c2));
-      n3 += __popcll(__ballot(g[i] >= c3));
-    }
-    T = n3 >= k ? c3 : (n2 >= k ? c2 : (n1 >= k ? c1 : T));
+  for (int s = 0; s * kBits < 16; ++s) {
+    const int bits = min(kBits, 16 - s * kBits), bit = 32 - s * kBits - bits;
+    const uint32_t c = T | ((uint32_t)wave << bit);
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < kGroups / kWave; ++i) n += (uint32_t)__popcll(__ballot(g[i] >= c));
+    uint32_t* const num = (s & 1) ? sh.other32 : sh.red32;   // the last step's may still be read
+    if (lane == 0) num[wave] = n;
+    __syncthreads();
+    const uint64_t hit = __ballot(lane < (1 << bits) && num[lane & (kWaves - 1)] >= (uint32_t)k);
+    // 0 reaches all groups, of which there are more than k
+    T |= (uint32_t)(63 - __clzll((long long)hit)) << bit;
   }
   return T;
 }
@@ -760,10 +805,8 @@ __device__ __attribute__((always_inline)) inline bool sample_listed(
   ListScratch& ls = sh.u.l;
   if (threadIdx.x == 0) sh.n = 0u;
   __syncthreads();
-  passes.between(mx, thr, INFINITY, sh, [&](float x, int e) {
-    const uint32_t i = atomicAdd(&sh.n, 1u);
-    if (i < (uint32_t)kList) ls.list[i] = cand_key(value_key(__float_as_uint(x)), (uint32_t)e);
-  });
+  passes.between(mx, thr, INFINITY, sh,
+                 [&](const auto& x, const auto& in, int e0) { append<DT, NT>(sh, x, in, e0); });
   __syncthreads();
   const uint32_t n = sh.n;
   if (n > (uint32_t)kList) return false;
@@ -991,9 +1034,9 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
   if (tid == 0) sh.n = 0u;
   __syncthreads();   // the counts are read: the list may take their place
   const float value = key_value(key);
-  passes.between(mx, value, value, sh, [&](float, int e) {
+  passes.between(mx, value, value, sh, each([&](float, int e) {
     sh.u.l.list[atomicAdd(&sh.n, 1u)] = (uint64_t)(0xFFFFFFFFu - (uint32_t)e);
-  });
+  }));
   __syncthreads();
   sort_list<DT, NT>(c.ties, sh);
   out->token = (int)(0xFFFFFFFFu - (uint32_t)sh.u.l.sorted[c.nth]);
@@ -1096,12 +1139,12 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     const double z0 = (double)bin - 0.5;
     passes.between(mx, bound_below((double)M - (z0 + (double)(hi + 1) / kSub) / scale, M),
                    -bound_below((z0 + (double)lo / kSub) / scale - (double)M, M), sh,
-                   [&](float x, int e) {
+                   each([&](float x, int e) {
                      const double z = depth(x), t = offset(z);
                      if (!(z < kDeepest) || bin_at(z) != bin) return;
                      const int i = sub_at(t);
                      if (i >= lo && i <= hi) f(x, z, t, e);
-                   });
+                   }));
     __syncthreads();
   };
   // list[] from the elements of a bin's parts lo .. hi; their number
@@ -1293,7 +1336,12 @@ __global__ __launch_bounds__(NT, 4) void sample_kernel(
     if (!(st.T > 0.f)) {
       if (tid == 0) sh.n = 0xFFFFFFFFu;
       __syncthreads();
-      passes.between(mx, M, INFINITY, sh, [&](float, int e) { atomicMin(&sh.n, (uint32_t)e); });
+      passes.between(mx, M, INFINITY, sh, [&](const auto&, const auto& in, int e0) {
+        int least = 0x7FFFFFFF;
+#pragma unroll
+        for (int q = Row<DT>::U - 1; q >= 0; --q) least = in[q] ? e0 + q : least;
+        atomicMin(&sh.n, (uint32_t)least);
+      });
       __syncthreads();
       d = {(int)sh.n, 1.f};
       done = true;
