@@ -763,16 +763,23 @@ __device__ inline uint64_t sum_list(uint32_t n, Shared<DT, NT>& sh, W&& w, F&& f
   return all;
 }
 
-// the first position of cum[0 .. n) that exceeds target (one does)
+// The first i < n whose value(i) exceeds target, n if none does (values do not fall; n at most
+// 64 B).  Two reads, by every wave for itself: no barrier.
+template <int B, class F>
+__device__ inline int first_above(uint64_t target, int n, F&& value) {
+  static_assert(B <= kWave, "a block per lane, then a lane per element of one");
+  const int lane = threadIdx.x & (kWave - 1);
+  const int end = lane * B + B - 1;
+  const uint64_t blocks = __ballot(end >= n || value(end) > target);
+  const int i = (blocks ? (int)__ffsll((long long)blocks) - 1 : kWave - 1) * B + lane;
+  const uint64_t hit = __ballot(lane < B && (i >= n || value(i) > target));
+  return min(i - lane + (hit ? (int)__ffsll((long long)hit) - 1 : B), n);
+}
+// ... in cum[0 .. n), where one does
 template <int DT, int NT>
-__device__ inline uint32_t first_above(uint64_t target, uint32_t n, Shared<DT, NT>& sh) {
-  const ListScratch& ls = sh.u.l;
-  for (uint32_t i = threadIdx.x; i < n; i += NT)
-    if (ls.cum[i] > target && (i == 0 || ls.cum[i - 1] <= target)) sh.out32[1] = i;
-  __syncthreads();
-  const uint32_t r = sh.out32[1];
-  __syncthreads();
-  return r;
+__device__ inline uint32_t first_in_list(uint64_t target, uint32_t n, Shared<DT, NT>& sh) {
+  return (uint32_t)first_above<kList / kWave>(target, (int)n,
+                                             [&](int i) { return sh.u.l.cum[i]; });
 }
 
 // how many of the list's first elements satisfy `in` (those that do come first)
@@ -813,13 +820,13 @@ __device__ __attribute__((always_inline)) inline bool sample_listed(
   sort_list<DT, NT>(n, sh);
   uint64_t S = sum_list<DT, NT>(n, sh, w, [](uint64_t c) { return c; });
   if (st.k > 0 && (uint32_t)st.k < n) S = ls.cum[st.k - 1];
-  if (st.p < 1.f) S = ls.cum[first_above<DT, NT>(top_p_sum(st.p, S) - 1, n, sh)];
+  if (st.p < 1.f) S = ls.cum[first_in_list<DT, NT>(top_p_sum(st.p, S) - 1, n, sh)];
   if (st.mp > 0.f) {
     const uint32_t in =
         count_list<DT, NT>(n, sh, [&](uint32_t key) { return w.log2w(key) >= least; });
     S = min(S, ls.cum[in - 1]);
   }
-  const uint32_t r = first_above<DT, NT>(draw_target(st.u, S), n, sh);
+  const uint32_t r = first_in_list<DT, NT>(draw_target(st.u, S), n, sh);
   out->token = (int)cand_index(ls.sorted[r]);
   out->prob = (float)((double)(ls.cum[r] - (r ? ls.cum[r - 1] : 0ull)) / (double)S);
   return true;
@@ -942,6 +949,7 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
     const uint64_t pn = block_scan_u64<Shared<DT, NT>, NT>(n + seen, sh, &have) - n;
     if (tid < runs) cs.mass[tid] = pm, cs.num[tid] = (uint32_t)pn;
   }
+  __syncthreads();
   // a count past 16 bits loses 65536, or turns them into one of its neighbour's
   if ((have >> 32) != (have & 0xFFFFFFFFull)) return false;
   have &= 0xFFFFFFFFull;
@@ -953,15 +961,12 @@ __device__ __attribute__((always_inline)) inline bool sample_counted(
   // Where the running sum (count) first exceeds target.  One wave looks into the run (all of
   // them would share its evaluation of 256 weights' worth of vector time).
   auto crossing = [&](uint64_t target, bool by_count) -> Cross {
-    if (tid < runs) {
-      const uint64_t a = by_count ? cs.num[tid] : cs.mass[tid];
-      const uint64_t b = tid + 1 < runs ? (by_count ? cs.num[tid + 1] : cs.mass[tid + 1])
-                                        : (by_count ? have : S);
-      if (a <= target && target < b) sh.out32[0] = (uint32_t)tid;
-    }
-    __syncthreads();
     if (wave == 0) {
-      const int r = __builtin_amdgcn_readfirstlane(sh.out32[0]);
+      // the last run before which the sum does not exceed it
+      constexpr int kBlock = (kRuns + kWave - 1) / kWave;
+      const int r =
+          (by_count ? first_above<kBlock>(target, runs, [&](int i) { return (uint64_t)cs.num[i]; })
+                    : first_above<kBlock>(target, runs, [&](int i) { return cs.mass[i]; })) - 1;
       const Four f = four(r);
       uint64_t m[4];   // what is counted
 #pragma unroll
@@ -1165,15 +1170,11 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   };
   // The element where the running sum (count) in rank order first exceeds target
   auto locate = [&](uint64_t target, bool by_count, Found& f) -> bool {
-    for (int b = tid; b < kWeightBins; b += NT) {
-      const bool more = b + 1 < kWeightBins;
-      const uint64_t lo = by_count ? (uint64_t)bs.num[b] : bs.mass[b];
-      const uint64_t hi = by_count ? (more ? (uint64_t)bs.num[b + 1] : have)
-                                   : (more ? bs.mass[b + 1] : S);
-      if (lo <= target && target < hi) sh.out32[0] = (uint32_t)b;
-    }
-    __syncthreads();
-    const int bin = (int)sh.out32[0];
+    // the last bin before which the sum does not exceed it
+    constexpr int kBlock = (kWeightBins + kWave - 1) / kWave;
+    const int bin =
+        (by_count ? first_above<kBlock>(target, kWeightBins, [&](int b) { return (uint64_t)bs.num[b]; })
+                  : first_above<kBlock>(target, kWeightBins, [&](int b) { return bs.mass[b]; })) - 1;
     f.bin = bin;
     const double bsc = bin_scale(bin);
     const uint64_t before = bs.mass[bin];
@@ -1249,7 +1250,7 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
     sum_list<DT, NT>(
         n, sh, [&](uint32_t key) { return factor(offset(depth(key_value(key)))); },
         [&](uint64_t c) { return through(c0 + c); });
-    const uint32_t i = by_count ? (uint32_t)(target - n0) : first_above<DT, NT>(target, n, sh);
+    const uint32_t i = by_count ? (uint32_t)(target - n0) : first_in_list<DT, NT>(target, n, sh);
     const uint64_t e = bs.l.sorted[i];
     f.key = (uint32_t)(e >> 32);
     f.token = (int)cand_index(e);
