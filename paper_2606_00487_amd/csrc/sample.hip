@@ -21,8 +21,8 @@
 //                   infinite temperature or fp32 maximum, fp32 rows too dense to bin): a radix
 //                   descent over the row for each question.
 // Bound: reading the row where nothing is added up for every element (2048 rows x 151936 bf16,
-// top_k: 140 us; their bytes at 5.3 TB/s take 117); the LDS additions beside it otherwise (no
-// filter 204, top_p 182; 64 additions of 32 bits take 12 clocks of a CU, of 64 bits 20); for few
+// top_k: 139 us; their bytes at 5.3 TB/s take 117); the LDS additions beside it otherwise (no
+// filter 203, top_p 183; 64 additions of 32 bits take 12 clocks of a CU, of 64 bits 20); for few
 // rows the chain of about twenty barriers with small work between them (16 rows x 1000: 9 to 14
 // us).  Two workgroups a CU where there are rows for that: one's questions beside the other's
 // reading.  Rows shared out over several workgroups, with a second kernel for the questions, took
