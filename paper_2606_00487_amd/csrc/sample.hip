@@ -725,17 +725,28 @@ __device__ inline uint32_t top_k_bound(float mx, int k, Shared<DT, NT>& sh) {
 template <int DT, int NT>
 __device__ inline void sort_list(uint32_t n, Shared<DT, NT>& sh) {
   ListScratch& ls = sh.u.l;
+  const uint32_t whole = n & ~7u;
   for (uint32_t i = threadIdx.x; i < n; i += NT) {
     const uint64_t mine = ls.list[i];
     uint32_t rank = 0, j = 0;
-    for (; j + 8 <= n; j += 8) {   // eight at a time, every lane the same ones
-      ulonglong2 v[4];
+    ulonglong2 v[4];   // eight at a time, every lane the same ones
+    auto read = [&]() {
 #pragma unroll
       for (int t = 0; t < 4; ++t) v[t] = *(const ulonglong2*)&ls.list[j + 2 * t];
+    };
+    for (; j < whole; j += 8) {
+      read();
 #pragma unroll
       for (int t = 0; t < 4; ++t) rank += (v[t].x > mine ? 1u : 0u) + (v[t].y > mine ? 1u : 0u);
     }
-    for (; j < n; ++j) rank += ls.list[j] > mine ? 1u : 0u;
+    if (j < n) {   // (the list has room for eight; what lies past n is not counted)
+      read();
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        rank += j + 2 * t < n && v[t].x > mine ? 1u : 0u;
+        rank += j + 2 * t + 1 < n && v[t].y > mine ? 1u : 0u;
+      }
+    }
     ls.sorted[rank] = mine;
   }
   __syncthreads();
@@ -1069,7 +1080,7 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   // differences to an infinite maximum are not 0 even for its equals, and at an infinite
   // temperature all weights are equal
   if (M == INFINITY || !(w.scale > 0.0)) return false;
-  const double scale = kPerOctave * w.scale;
+  const double scale = kPerOctave * w.scale, inverse = 1.0 / scale;
   for (int i = tid; i < kWeightBins; i += NT) bs.mass[i] = 0ull, bs.num[i] = 0u;
   __syncthreads();
   constexpr double kInt = 6755399441055744.0;   // 1.5 * 2^52
@@ -1142,8 +1153,8 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   // f(x, z, t, index) for the elements of a bin's parts lo .. hi
   auto within = [&](int bin, int lo, int hi, auto&& f) {
     const double z0 = (double)bin - 0.5;
-    passes.between(mx, bound_below((double)M - (z0 + (double)(hi + 1) / kSub) / scale, M),
-                   -bound_below((z0 + (double)lo / kSub) / scale - (double)M, M), sh,
+    passes.between(mx, bound_below((double)M - (z0 + (double)(hi + 1) / kSub) * inverse, M),
+                   -bound_below((z0 + (double)lo / kSub) * inverse - (double)M, M), sh,
                    each([&](float x, int e) {
                      const double z = depth(x), t = offset(z);
                      if (!(z < kDeepest) || bin_at(z) != bin) return;
