@@ -2,9 +2,9 @@
 
     python -m paper_2606_00487_amd.build
 
-Every .hip file is compiled to an object with hipcc, the selection kernel with
--ffp-contract=off (its fp64 scores must round every product and sum separately),
-the attention kernel with MFMA results in ordinary vector registers; then
+Every .hip file is compiled to an object with hipcc, the selection and sampling kernels with
+-ffp-contract=off (the fp64 scores must round every product and sum separately, a weight must be
+the same in every pass), the attention kernels with MFMA results in ordinary vector registers; then
 everything is linked into paper_2606_00487_amd/libtaps.so.
 """
 from __future__ import annotations
