@@ -542,8 +542,11 @@ size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab,
  * results do not depend on the order of additions.  S_k is the sum of the weights after top_k;
  * top_p keeps up to the first token whose running sum reaches top_p * S_k; S is the sum of all
  * that are kept.  The token is the first whose running sum exceeds u * S, its probability W / S.
- * (Weights that round to 0, below 2^-44 of the largest, are never drawn.)  A row of NaN alone
- * gives token 0 with probability 0.  budget at most TAPS_MAX_BUDGET, vocab at most
+ * Weights are rounded to multiples of 2^-43 of W_0, so that those of at most 2^-44 are 0 and
+ * never drawn.  (fp32 rows that neither a small top_k nor min_p bounds: weights above 2^-44 are
+ * added up before they are rounded, in bins of 1/32 octave whose running sums are rounded down; a
+ * token's share of a sum still is within 2^-42 of W_0 of its weight, but a lone weight below
+ * 2^-43 may count 0 there.)  A row of NaN alone gives token 0 with probability 0.  budget at most TAPS_MAX_BUDGET, vocab at most
  * TAPS_MAX_SAMPLE_VOCAB, batch * budget at most 2^20. */
 taps_status taps_sample(const void *logits, int64_t row_stride, int32_t batch, int32_t budget,
                         int32_t vocab, int32_t dtype, const int32_t *n_nodes,

@@ -123,7 +123,8 @@ constexpr int kWindow = 36864;      // bf16 values counted one by one, from the 
 constexpr int kRun = 256;           // values whose sums are kept together: four per lane
 constexpr int kRuns = kWindow / kRun;
 constexpr int kPerOctave = 32;      // fp32: bins of the weight per factor of two
-constexpr int kWeightBins = 1424;   // 44.5 octaves: smaller weights round to 0
+constexpr int kOctaves = 44;        // smaller weights round to 0: at most half of 2^-43
+constexpr int kWeightBins = kOctaves * kPerOctave + 1;   // the last one's upper half lies below
 constexpr int kSub = 1024;          // parts of a bin with more elements than the list takes
 constexpr int kList = 1024;         // elements that are ranked one by one
 constexpr int kGroups = 256;        // thread groups whose maxima bound a small top_k
@@ -1084,7 +1085,9 @@ __device__ __attribute__((always_inline)) inline bool sample_binned(
   for (int i = tid; i < kWeightBins; i += NT) bs.mass[i] = 0ull, bs.num[i] = 0u;
   __syncthreads();
   constexpr double kInt = 6755399441055744.0;   // 1.5 * 2^52
-  constexpr double kDeepest = kWeightBins - 1;   // depths from here on add nothing
+  // depths from here on add nothing (a million of them would add up to more than their weights,
+  // each of which is 0)
+  constexpr double kDeepest = kOctaves * kPerOctave;
   auto depth = [&](float x) -> double { return ((double)M - (double)x) * scale; };
   auto offset = [&](double z) -> double { return z - ((z + kInt) - kInt); };
   auto bin_at = [&](double z) -> int { return (int)__double_as_longlong(z + kInt); };
