@@ -529,7 +529,9 @@ size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab,
  * of it, so the emitted tokens are samples of the target), or, with budget 1, each request's
  * next token.
  *   logits     [batch][budget][vocab] bf16 or fp32, consecutive rows row_stride elements apart
- *              (at least vocab), 16-byte aligned base
+ *              (at least vocab).  Base 16-byte aligned where vocab elements are a multiple of 16
+ *              bytes, otherwise aligned to an element (a view that leaves rows out, of logits
+ *              with an odd vocabulary, needs no copy)
  *   n_nodes    [batch] int32 rows to sample per request, or NULL (all): rows i >= n_nodes[b]
  *              get token -1 and probability 0, their logits are not read
  *   s          the settings
@@ -546,8 +548,9 @@ size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab,
  * never drawn.  (fp32 rows that neither a small top_k nor min_p bounds: weights above 2^-44 are
  * added up before they are rounded, in bins of 1/32 octave whose running sums are rounded down; a
  * token's share of a sum still is within 2^-42 of W_0 of its weight, but a lone weight below
- * 2^-43 may count 0 there.)  A row of NaN alone gives token 0 with probability 0.  budget at most TAPS_MAX_BUDGET, vocab at most
- * TAPS_MAX_SAMPLE_VOCAB, batch * budget at most 2^20. */
+ * 2^-43 may count 0 there.)  A row of NaN alone gives token 0 with probability 0.
+ * budget at most TAPS_MAX_BUDGET, vocab at most TAPS_MAX_SAMPLE_VOCAB, batch * budget at most
+ * 2^20. */
 taps_status taps_sample(const void *logits, int64_t row_stride, int32_t batch, int32_t budget,
                         int32_t vocab, int32_t dtype, const int32_t *n_nodes,
                         const taps_sampling *s, const float *u, int32_t *tokens, float *probs,

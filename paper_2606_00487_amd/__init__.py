@@ -610,8 +610,8 @@ class TokenSampler:
 
     def __call__(self, logits, u, n_nodes=None, temperature=None, top_k=None, top_p=None,
                  min_p=None):
-        """logits: [batch, budget, vocab], rows may be apart (a padded vocabulary's slice); u:
-        [batch, budget] float32; n_nodes: [batch] int32 or None; the settings: [batch] tensors
+        """logits: [batch, budget, vocab], rows may be apart (a padded vocabulary's slice) and
+        begin anywhere unless a row is whole 16-byte units (then at one); u: [batch, budget] float32; n_nodes: [batch] int32 or None; the settings: [batch] tensors
         (top_k int32, the others float32) or None.  Returns the tokens [batch, budget] int32 and
         their probabilities, float32.  Each call has scratch of its own."""
         batch, budget, vocab, dtype = self.shape

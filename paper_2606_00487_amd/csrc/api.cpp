@@ -634,14 +634,17 @@ taps_status taps_sample(const void* logits, int64_t row_stride, int32_t batch, i
   if (st != TAPS_OK) return st;
   if (batch == 0) return TAPS_OK;
   if (!logits || !s || !u || !tokens) return TAPS_ERR_INVALID_ARG;
-  if (((uintptr_t)logits & 15) != 0) return TAPS_ERR_INVALID_ARG;
+  // rows that begin inside 16 bytes are read as well; an odd vocabulary has them anyway
+  const int es = dtype == TAPS_BF16 ? 2 : 4;
+  const uintptr_t unaligned = ((int64_t)vocab * es & 15) == 0 ? 15 : es - 1;
+  if (((uintptr_t)logits & unaligned) != 0) return TAPS_ERR_INVALID_ARG;
   const uintptr_t a4 = (uintptr_t)n_nodes | (uintptr_t)s->temperature | (uintptr_t)s->top_k |
                        (uintptr_t)s->top_p | (uintptr_t)s->min_p | (uintptr_t)u |
                        (uintptr_t)tokens | (uintptr_t)probs;
   if ((a4 & 3) != 0) return TAPS_ERR_INVALID_ARG;
   const size_t need = taps_sample_workspace_bytes(batch, budget, vocab, dtype);
   if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return TAPS_ERR_WORKSPACE;
-  return launch_sample(logits, row_stride * (dtype == TAPS_BF16 ? 2 : 4), batch, budget, vocab,
+  return launch_sample(logits, row_stride * es, batch, budget, vocab,
                        dtype, n_nodes, *s, u, tokens, probs, stream) == hipSuccess
              ? TAPS_OK
              : TAPS_ERR_HIP;
