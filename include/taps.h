@@ -520,8 +520,7 @@ typedef struct {
 taps_status taps_sample_validate(int32_t batch, int32_t budget, int32_t vocab, int64_t row_stride,
                                  int32_t dtype);
 
-/* Bytes of scratch taps_sample needs.  Calls that may overlap on the GPU need scratch of their
- * own. */
+/* Bytes of scratch taps_sample needs: 0 for every size. */
 size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab, int32_t dtype);
 
 /* One token per logits row, from a given random number: the target's token after each node of
@@ -538,6 +537,7 @@ size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab,
  *   u          [batch][budget] float random numbers in [0, 1) (NaN counts 0; others are clamped)
  *   tokens     [batch][budget] int32
  *   probs      [batch][budget] float, or NULL: the token's probability among the kept ones
+ *   ws, ws_bytes  not read (a row's work stays in its workgroup); NULL and 0 will do
  * A row's rank order is value descending, then index ascending; -0 equals +0; NaN is last.
  * Token r of it has the weight W_r = exp((x_r - x_0) / T), 1 where x_r equals x_0 (infinite values
  * too) and 0 for NaN, evaluated in fp64 to within 2^-42 of W_0 and added up as integers, so that

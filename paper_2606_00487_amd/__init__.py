@@ -606,14 +606,14 @@ class TokenSampler:
         self.shape = (batch, budget, vocab, dtype)
         _lib.check(self.lib, "taps_sample_validate",
                    self.lib.taps_sample_validate(batch, budget, vocab, vocab, dtype))
-        self.ws_bytes = self.lib.taps_sample_workspace_bytes(*self.shape)
 
     def __call__(self, logits, u, n_nodes=None, temperature=None, top_k=None, top_p=None,
                  min_p=None):
         """logits: [batch, budget, vocab], rows may be apart (a padded vocabulary's slice) and
-        begin anywhere unless a row is whole 16-byte units (then at one); u: [batch, budget] float32; n_nodes: [batch] int32 or None; the settings: [batch] tensors
-        (top_k int32, the others float32) or None.  Returns the tokens [batch, budget] int32 and
-        their probabilities, float32.  Each call has scratch of its own."""
+        begin anywhere unless a row is whole 16-byte units (then at one); u: [batch, budget]
+        float32; n_nodes: [batch] int32 or None; the settings: [batch] tensors (top_k int32, the
+        others float32) or None.  Returns the tokens [batch, budget] int32 and their
+        probabilities, float32."""
         batch, budget, vocab, dtype = self.shape
         if logits.shape != (batch, budget, vocab):
             raise ValueError(f"logits: expected [{batch}, {budget}, {vocab}], "
@@ -634,9 +634,8 @@ class TokenSampler:
             if t is not None:
                 _need_on(dev, t, name, dt, (batch,))
         tokens, probs = u.new_empty((batch, budget), dtype=torch.int32), torch.empty_like(u)
-        ws = u.new_empty(self.ws_bytes, dtype=torch.uint8) if self.ws_bytes else None
         st = _lib.Sampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
         _lib.check(self.lib, "taps_sample", self.lib.taps_sample(
             _ptr(logits), stride, batch, budget, vocab, dtype, _ptr(n_nodes), ctypes.byref(st),
-            _ptr(u), _ptr(tokens), _ptr(probs), _ptr(ws), self.ws_bytes, _stream()))
+            _ptr(u), _ptr(tokens), _ptr(probs), None, 0, _stream()))
         return tokens, probs

@@ -621,15 +621,12 @@ taps_status taps_sample_validate(int32_t batch, int32_t budget, int32_t vocab, i
   return TAPS_OK;
 }
 
-size_t taps_sample_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab, int32_t dtype) {
-  if (taps_sample_validate(batch, budget, vocab, vocab, dtype) != TAPS_OK || batch == 0) return 0;
-  return 0;
-}
+size_t taps_sample_workspace_bytes(int32_t, int32_t, int32_t, int32_t) { return 0; }
 
 taps_status taps_sample(const void* logits, int64_t row_stride, int32_t batch, int32_t budget,
                         int32_t vocab, int32_t dtype, const int32_t* n_nodes,
                         const taps_sampling* s, const float* u, int32_t* tokens, float* probs,
-                        void* ws, size_t ws_bytes, hipStream_t stream) {
+                        void*, size_t, hipStream_t stream) {
   const taps_status st = taps_sample_validate(batch, budget, vocab, row_stride, dtype);
   if (st != TAPS_OK) return st;
   if (batch == 0) return TAPS_OK;
@@ -642,8 +639,6 @@ taps_status taps_sample(const void* logits, int64_t row_stride, int32_t batch, i
                        (uintptr_t)s->top_p | (uintptr_t)s->min_p | (uintptr_t)u |
                        (uintptr_t)tokens | (uintptr_t)probs;
   if ((a4 & 3) != 0) return TAPS_ERR_INVALID_ARG;
-  const size_t need = taps_sample_workspace_bytes(batch, budget, vocab, dtype);
-  if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return TAPS_ERR_WORKSPACE;
   return launch_sample(logits, row_stride * es, batch, budget, vocab,
                        dtype, n_nodes, *s, u, tokens, probs, stream) == hipSuccess
              ? TAPS_OK
