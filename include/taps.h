@@ -437,9 +437,10 @@ taps_status verify_layer_paged(const void *X, const taps_layer_weights *w, void 
  *                ones are written from entry n_free on (none past num_pages)
  *   n_free       [1] int32, clamped to [0, num_pages]
  *   num_pages, page_rows  as for tree_verify_attn_paged; max_pages * page_rows at most 2^30
- *   held_out     [batch] pages held afterwards; not in the held_pages array
- *   n_free_out   [1] free pages afterwards; not the n_free array
- *   n_short      [1] number of requests that did not get what they need
+ *   held_out     [batch] pages held afterwards
+ *   n_free_out   [1] free pages afterwards
+ *   n_short      [1] number of requests that did not get what they need.  These three share no
+ *                memory with held_pages, ctx_len, n_new and n_free
  *   slot_map     [batch][max_new] int64, or NULL: the pool row of logical row ctx + i, page id
  *                * page_rows + (ctx + i) % page_rows, for i < new; -1 from new on, and for
  *                every row of a request that is short

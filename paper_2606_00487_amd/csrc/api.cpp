@@ -514,12 +514,22 @@ taps_status kv_reserve_paged(int32_t* block_table, int32_t max_pages, const int3
   if (!block_table || !held_pages || !ctx_len || !n_new || !free_pages || !n_free || !held_out ||
       !n_free_out || !n_short)
     return TAPS_ERR_INVALID_ARG;
-  // every workgroup reads the whole batch's counts while others write the new ones
-  if (held_out == held_pages || n_free_out == n_free) return TAPS_ERR_INVALID_ARG;
   const uintptr_t a4 = (uintptr_t)block_table | (uintptr_t)held_pages | (uintptr_t)ctx_len |
                        (uintptr_t)n_new | (uintptr_t)free_pages | (uintptr_t)n_free |
                        (uintptr_t)held_out | (uintptr_t)n_free_out | (uintptr_t)n_short;
   if ((a4 & 3) != 0 || ((uintptr_t)slot_map & 7) != 0) return TAPS_ERR_INVALID_ARG;
+  // every workgroup reads the whole batch's lengths while others write the new counts
+  auto apart = [](const int32_t* out, int64_t n, const int32_t* in, int64_t m) {
+    const uintptr_t a = (uintptr_t)out, b = (uintptr_t)in;
+    return a + 4 * n <= b || b + 4 * m <= a;
+  };
+  auto writes_no_input = [&](const int32_t* out, int64_t n) {
+    return apart(out, n, held_pages, batch) && apart(out, n, ctx_len, batch) &&
+           apart(out, n, n_new, batch) && apart(out, n, n_free, 1);
+  };
+  if (!writes_no_input(held_out, batch) || !writes_no_input(n_free_out, 1) ||
+      !writes_no_input(n_short, 1))
+    return TAPS_ERR_INVALID_ARG;
   return launch_reserve(block_table, max_pages, held_pages, ctx_len, n_new, batch, free_pages,
                         n_free, num_pages, shift, max_new, slot_map, held_out, n_free_out, n_short,
                         stream) == hipSuccess
