@@ -24,8 +24,9 @@
 // made up most of the outputs' error.
 //
 // Bound: HBM (K and V are read once; a group of more than 16 query heads reads them once per 16):
-// 128 requests of 512-32K keys (64/8 heads of 128, bf16) 743 us, 5.5 TB/s; 16 of 512-16K (32/8)
-// 59 us, 5.1 TB/s.  Short batches: latency, two launches and the dependent reads of lengths, page
+// 128 requests of 512-32K keys (64/8 heads of 128, bf16) 742 us, 5.5 TB/s (of 64: 405, 5.0); 16 of
+// 512-16K (32/8) 67 us, 4.5 TB/s, 59 where the last-level cache keeps what it holds of them; fp32,
+// 64 of 512-8K (32/8 of 128) 249 us, 5.8 TB/s.  Short batches: latency, two launches and the dependent reads of lengths, page
 // ids, keys and pieces (one request of 8192 keys 12.7 us; its bytes take 6.3).
 #include <algorithm>
 
@@ -526,12 +527,17 @@ hipError_t launch_t(const void* Q, int64_t q_stride, const void* K, const void* 
 }  // namespace
 
 // Equal parts for two workgroups per CU.  us a call with 256 / 512 / 768 / 1024 workgroups, from
-// graphs: 128 requests of 512-32K keys (64/8 heads of 128, bf16) 720 / 741 / 756 / 752, 16 of
+// graphs over the same inputs: 128 requests of 512-32K keys (64/8 heads of 128, bf16) 720 / 741 / 756 / 752, 16 of
 // 512-16K (32/8) 60 / 58 / 62 / 65, 64 of 256-4K 83 / 80 / 81 / 89, 256 of 64-2K 150 / 137 / 142
-// / 152, 8 of 512-8K in fp32 40 / 36 / 41 / 42, one of 8K 12.9 / 12.7 / 12.6 / 12.7.
-// One workgroup per (request, KV head, head tile) without the second kernel instead: where all
-// requests are short (4/2 heads of 64 over 256 keys, fp32: 7.3 against 9.7) or many and short
-// (64 of 64-300 keys, 32/8 heads: 12 against 17; 256 of 64-2K: 151 against 137).
+// / 152, 8 of 512-8K in fp32 (32/8 of 128) 40 / 36 / 41 / 42, one of 8K 12.9 / 12.7 / 12.6 / 12.7.
+// One workgroup per (request, KV head, head tile) without the second kernel instead where all
+// requests are short, or many and rather short.  At the borders, us a call without / with the
+// second kernel (max_len one more; other inputs every call): 256 keys: one request (32/8 heads of
+// 128) 6.2 / 9.0, 63 of 128-256 15 / 20, 8 in fp32 13 / 13; 1024 keys: 64 requests of 64-300 15 /
+// 19, of 512-1024 47 / 52, 256 of 64-1024 94 / 94, 512 of 64-1024 (4/1 of 64) 20 / 25, 300 (34/1 of
+// 128) 33 / 45, but 64 of 64-1024 in fp32 66 / 52.  By the batch: 63 of 64-1024 32 with the second
+// kernel, 64 of them 35 without; 256 of 64-2K 137 with, 151 without.  max_len is the host's
+// bound: short requests under a long one take the cut all the same (64 of 64-300: 19).
 DecodePlan plan_decode(int batch, int Hq, int Hkv, int max_len) {
   DecodePlan p;
   p.htiles = (Hq / Hkv + kHeads - 1) / kHeads;

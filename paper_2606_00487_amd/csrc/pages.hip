@@ -22,10 +22,10 @@ namespace {
 // above n_free is a page that this call pushes; it is read from the table row that gives it
 // (found by its place in the prefix sums), which no other workgroup writes, so that the kernel
 // nowhere reads what it writes.  Grid (runs of requests, slices of the slot map).
-// Bound: latency (two dependent reads, a block scan, the page reads): 5 us for 16 requests; then
-// the slot map's bytes (34 MB for 1024 requests with 4096 slots: 6 of 14 us) and every workgroup's
-// sums over the batch.  (With a page looked up for every slot of it
-// instead of once: 27 us.)
+// Bound: latency (two dependent reads, a block scan, the page reads): 5 us for 16 requests; 6.5 for
+// 1024, whose sums every workgroup forms; and the slot map's bytes: 14.4 us with 4096 slots a
+// request (34 MB, which take 5.8 at the memory's rate).  (With a page looked up for every slot of
+// it instead of once: 27 us.)
 constexpr int kReserveThreads = 256;
 constexpr int kSlotsPerGroup = 4096;   // slot map columns per workgroup
 constexpr int kReserveGroups = 512;    // runs of requests, at most

@@ -21,10 +21,12 @@
 //                   infinite temperature or fp32 maximum, fp32 rows too dense to bin): a radix
 //                   descent over the row for each question.
 // Bound: reading the row where nothing is added up for every element (2048 rows x 151936 bf16,
-// top_k: 139 us; their bytes at 5.3 TB/s take 117); the LDS additions beside it otherwise (no
-// filter 203, top_p 183; 64 additions of 32 bits take 12 clocks of a CU, of 64 bits 20); for few
-// rows the chain of about twenty barriers with small work between them (16 rows x 1000: 9 to 14
-// us).  Two workgroups a CU where there are rows for that: one's questions beside the other's
+// top_k 40: 134 us; their bytes at 5.8 TB/s take 107); the LDS additions beside it otherwise (no
+// filter 191, top_p 190; 64 additions of 32 bits take 12 clocks of a CU, of 64 bits 20); for few
+// rows the chain of about twenty barriers with small work between them (16 rows x 1000: 10 to 15
+// us).  A small top_k over a row whose finite values (a mask leaves the others -inf) are in fewer
+// thread groups than that finds no bound, and the row is read three times (2048 rows, top_k 40 of
+// 40 finite values: 334 us; top_k 20: 131).  Two workgroups a CU where there are rows for that: one's questions beside the other's
 // reading.  Rows shared out over several workgroups, with a second kernel for the questions, took
 // longer even for 32 rows (33 against 29 us).
 #include "common.h"
@@ -128,7 +130,9 @@ constexpr int kWeightBins = kOctaves * kPerOctave + 1;   // the last one's upper
 constexpr int kSub = 1024;          // parts of a bin with more elements than the list takes
 constexpr int kList = 1024;         // elements that are ranked one by one
 constexpr int kGroups = 256;        // thread groups whose maxima bound a small top_k
-constexpr int kFewTopK = 192;       // ... up to this one
+// ... up to this one.  us with top_k 192 / 193: 512 rows of 151,936 fp32 100 / 140, 32 of 50,257 17 /
+// 26, 64 of 151,936 bf16 22 / 28; 2048 of those 185 / 164 (148 with 100, 165 with 150).
+constexpr int kFewTopK = 192;
 
 // Scratch of the paths, which a row takes one after the other at most
 struct GeneralScratch {
@@ -1397,7 +1401,10 @@ hipError_t launch_dt(const void* logits, int64_t row_bytes, int budget, int voca
                      const int32_t* n_nodes, const Settings& st, const float* u, int32_t* tokens,
                      float* probs, hipStream_t stream) {
   // one row per CU: all its waves; more rows: two workgroups share a CU, one's passes over
-  // memory beside the other's work in LDS
+  // memory beside the other's work in LDS.  us with 1024 / 512 threads, 151,936 values in bf16 with
+  // top_p, with top_k + top_p, in fp32 with top_p, 50,257 in fp32 with top_k: 256 rows 35 / 40, 25 /
+  // 24, 97 / 104, 18 / 17; 257 rows 57 / 48, 37 / 28, 136 / 120, 26 / 19; 500 rows 71 / 60, 49 / 40,
+  // 171 / 172, 37 / 28; 768 rows 102 / 93, 71 / 56, 244 / 264, 55 / 43.
   if (rows <= 256)
     sample_kernel<DT, 1024><<<(unsigned)rows, 1024, 0, stream>>>(logits, row_bytes, budget, vocab,
                                                                  n_nodes, st, u, tokens, probs);
