@@ -23,6 +23,10 @@
  *   kv_append_paged   new K/V rows into the pools through a slot map
  *   decode_attn_paged attention of one new token per request (a step without a draft)
  *   taps_sample       tokens from the target's logits at a temperature (the walk's targets)
+ * Prompts, over the same cache (a request's context before its first round):
+ *   qk_rope_paged     per-head norms and rotary positions of new queries and keys, cache write
+ *   chunk_attn_paged  attention of chunks of new tokens
+ *   taps_logprobs     log probabilities and ranks of given tokens, entropy, top alternatives
  *
  * Conventions shared by every call:
  *   - Pointers are DEVICE memory owned by the caller unless marked [host].
@@ -556,6 +560,140 @@ taps_status taps_sample(const void *logits, int64_t row_stride, int32_t batch, i
                         int32_t vocab, int32_t dtype, const int32_t *n_nodes,
                         const taps_sampling *s, const float *u, int32_t *tokens, float *probs,
                         void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* [host] How positions are stretched past a trained length (factor s, trained length L), as in
+ * f_j = theta^(-2j / rot_dim), the turn of pair j per position in radians:
+ *   TAPS_ROPE_PLAIN   f_j
+ *   TAPS_ROPE_LINEAR  f_j / s: positions are interpolated
+ *   TAPS_ROPE_NTK     f_j with theta s^(rot_dim / (rot_dim - 2)): the slowest pair turns s times
+ *                     slower, the fastest as before (rot_dim at least 4)
+ *   TAPS_ROPE_YARN    by parts (YaRN, arXiv 2309.00071, alpha 1 and beta 32): with r = L f_j / (2
+ *                     pi) turns over the trained length and g = (r - 1) / 31 clamped to [0, 1],
+ *                     g f_j + (1 - g) f_j / s; cosines and sines are multiplied by 0.1 ln s + 1 */
+typedef enum {
+  TAPS_ROPE_PLAIN = 0,
+  TAPS_ROPE_LINEAR = 1,
+  TAPS_ROPE_NTK = 2,
+  TAPS_ROPE_YARN = 3
+} taps_rope_scaling;
+
+/* [host] The frequencies of rot_dim / 2 pairs (inv_freq, [host] memory) and the factor of cosines
+ * and sines.  rot_dim even, 2 .. 4096; theta finite and > 1; factor finite and >= 1; trained_len
+ * >= 1.  The plain kind reads neither factor nor trained_len, linear and NTK no trained_len. */
+taps_status taps_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor,
+                                  int64_t trained_len, double *inv_freq, float *mscale);
+
+/* [host] Norm and rotation of qk_rope_paged.
+ *   inv_freq        DEVICE [rot_dim / 2] fp64, 8-byte aligned: the pairs' turns per position
+ *   q_norm, k_norm  DEVICE [head_dim] RMSNorm weights in the call's dtype, 16-byte aligned, or
+ *                   NULL: no norm
+ *   norm_eps        finite and >= 0
+ *   mscale          factor of cosines and sines, finite (1 without stretching)
+ *   rot_dim         dims of a head that turn, from its first on: a multiple of 8, 8 .. head_dim
+ *   interleaved     0: pair j is (j, j + rot_dim / 2); 1: (2j, 2j + 1) */
+typedef struct {
+  const double *inv_freq;
+  const void *q_norm, *k_norm;
+  float norm_eps, mscale;
+  int32_t rot_dim, interleaved;
+} taps_rope;
+
+/* New tokens' queries, keys and values, as they leave their projection, made ready for attention
+ * over a paged cache: per query and key head RMSNorm over the whole head (x rsqrt(mean x^2 +
+ * eps) w), then pair j of it turned by positions[t] * inv_freq[j]: (a, b) -> mscale (a cos - b
+ * sin, b cos + a sin); dims from rot_dim on stay.  fp32 arithmetic (angles fp64), rounded once.
+ * Token t's key and value go to row slot_map[t] of the pools; slots outside [0, num_pages *
+ * page_rows), such as the -1 of kv_reserve_paged, leave them out (the query is written all the
+ * same).  No other row of the pools is written.
+ *   Q, K, V    [rows][Hq or Hkv][head_dim], consecutive rows q_stride, k_stride and v_stride
+ *              elements apart (at least a row, a multiple of 16 bytes): slices of a fused
+ *              projection's rows need no copy
+ *   positions  [rows] int32
+ *   slot_map   [rows] int64; a slot must not be named twice (its row would be a mix)
+ *   Q_out      [rows][Hq][head_dim]; it and the pools share no memory with Q, K, V or each other
+ *              (Q_out and the inputs are checked, and refused as TAPS_ERR_INVALID_ARG)
+ *   K_pages, V_pages, num_pages, page_rows  as for tree_verify_attn_paged
+ *   head_dim 64 or 128; dtype TAPS_BF16 or TAPS_FP32 for all of them; 16-byte aligned bases */
+taps_status qk_rope_paged(const void *Q, const void *K, const void *V, int64_t q_stride,
+                          int64_t k_stride, int64_t v_stride, const int32_t *positions,
+                          const int64_t *slot_map, int32_t rows, int32_t Hq, int32_t Hkv,
+                          int32_t head_dim, int32_t dtype, const taps_rope *rope, void *Q_out,
+                          void *K_pages, void *V_pages, int32_t num_pages, int32_t page_rows,
+                          hipStream_t stream);
+
+/* Host-only check of the sizes of chunk_attn_paged, no device access. */
+taps_status chunk_attn_paged_validate(int32_t batch, int32_t rows, int32_t Hq, int32_t Hkv,
+                                      int32_t head_dim, int32_t max_len, int32_t page_rows,
+                                      int32_t window, int32_t dtype, float scale);
+
+/* Bytes of scratch chunk_attn_paged needs (parts of tiles that are cut; 0 for short caches and
+ * for sizes that it rejects).  Calls that may overlap on the GPU need scratch of their own. */
+size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq, int32_t Hkv,
+                                        int32_t head_dim, int32_t max_len, int32_t page_rows,
+                                        int32_t dtype);
+
+/* Attention of chunks of new tokens over a paged KV cache: prompts, whole or in chunks, and
+ * single tokens among them.  Request b's n = q_start[b + 1] - q_start[b] new tokens are rows
+ * q_start[b] .. of Q and O, and the last n of its kv_len[b] cache rows are theirs (appended
+ * before the call).  Token i is at row p = kv_len[b] - n + i and sees the rows j <= p; with a
+ * window only p - window < j <= p.  O[i,h] = softmax_j(scale * Q[i,h] . K[j,g]) V[j,g], g = h /
+ * (Hq / Hkv); zeros for a token that sees no row (kv_len[b] < n).
+ *   Q            [rows][Hq][head_dim], consecutive rows q_stride elements apart (at least
+ *                Hq * head_dim, a multiple of 16 bytes)
+ *   K_pages, V_pages, num_pages, page_rows, block_table, max_pages  as for
+ *                tree_verify_attn_paged, in dtype; max_pages * page_rows at least max_len.  Block
+ *                table entries of pages that no token of the request sees (before the window, past
+ *                kv_len) may hold anything
+ *   q_start      [batch + 1] int32, not decreasing, within [0, rows] (clamped to it).  Rows of O
+ *                outside q_start[0] .. q_start[batch] - 1 are not written
+ *   kv_len       [batch] int32, clamped to [0, max_len].  Rows that no token of the call sees may
+ *                hold anything; rows that one sees and that are not finite leave undefined values
+ *                in any of the request's outputs
+ *   rows         [host] rows of Q and O, sizes the grid
+ *   head_dim     64 or 128; Hq a multiple of Hkv
+ *   max_len      [host] upper bound of kv_len, at most 2^30
+ *   window       0: none; else at least 1
+ *   dtype        TAPS_BF16 (fp32 accumulation, weights rounded to bf16 for the second product,
+ *                output rounded to nearest even) or TAPS_FP32
+ *   scale        softmax scale, finite and > 0
+ *   O            [rows][Hq][head_dim] in dtype, 16-byte aligned; not in Q's memory (checked)
+ *   ws           chunk_attn_paged_workspace_bytes(...) bytes, 16-byte aligned */
+taps_status chunk_attn_paged(const void *Q, int64_t q_stride, const void *K_pages,
+                             const void *V_pages, int32_t num_pages, int32_t page_rows,
+                             const int32_t *block_table, int32_t max_pages,
+                             const int32_t *q_start, const int32_t *kv_len, int32_t batch,
+                             int32_t rows, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                             int32_t max_len, int32_t window, int32_t dtype, float scale, void *O,
+                             void *ws, size_t ws_bytes, hipStream_t stream);
+
+#define TAPS_MAX_LOGPROB_TOP 64
+
+/* Host-only check of the sizes of taps_logprobs, no device access. */
+taps_status taps_logprobs_validate(int32_t batch, int32_t budget, int32_t vocab,
+                                   int64_t row_stride, int32_t dtype, int32_t top);
+
+/* Log probabilities of given tokens under each logits row (a prompt's next tokens, sampled or
+ * drafted ones), with their ranks, the row's entropy and its top alternatives.
+ *   logits       [batch][budget][vocab] as for taps_sample (row_stride, alignment, dtype)
+ *   n_nodes      [batch] int32 rows per request, or NULL (all): rows i >= n_nodes[b] get 0, rank
+ *                and index -1, their logits and tokens are not read
+ *   tokens       [batch][budget] int32.  Outside [0, vocab), such as the -1 of padding: log
+ *                probability -inf and rank -1 (entropy and alternatives are the row's)
+ *   top          alternatives per row, 0 .. min(vocab, TAPS_MAX_LOGPROB_TOP)
+ *   logprob      [batch][budget] float: ln p of the token
+ *   entropy      [batch][budget] float: -sum p ln p in nats
+ *   rank         [batch][budget] int32: tokens before it in the rank order (0: the largest)
+ *   top_idx      [batch][budget][top] int32, the first `top` tokens of the rank order
+ *   top_logprob  [batch][budget][top] float, theirs.  (Both may be NULL where top is 0)
+ * p_j = w_j / sum w, w_j = exp(x_j - x_0) for the largest value x_0: 1 where x_j equals x_0
+ * (infinite values too), 0 for NaN, as in taps_sample at T = 1.  The rank order is value
+ * descending, then index ascending; -0 equals +0; NaN is last.  A row of NaN alone has log
+ * probabilities -inf and entropy 0.  Sums are fp32 per thread, joined in fp64. */
+taps_status taps_logprobs(const void *logits, int64_t row_stride, int32_t batch, int32_t budget,
+                          int32_t vocab, int32_t dtype, const int32_t *n_nodes,
+                          const int32_t *tokens, int32_t top, float *logprob, float *entropy,
+                          int32_t *rank, int32_t *top_idx, float *top_logprob,
+                          hipStream_t stream);
 
 /* Human-readable name of a status code (static string). */
 const char *taps_status_string(int32_t status);

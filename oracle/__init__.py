@@ -18,6 +18,9 @@ Layout
   pages.py      pages from a free-page stack, slot maps, rows by slot
   decode.py     attention of one new token per request over a paged cache
   sample.py     token sampling with temperature, top-k, top-p and min-p
+  rope.py       per-head RMSNorm, rotary positions and the cache write of new rows
+  chunk.py      attention of chunks of new tokens over a paged cache
+  logprobs.py   log probabilities, ranks, entropy and top alternatives of logits rows
 
 Pins (what fixes each part without trusting this code) live in
 tests/test_oracle_*.py.  Parity of the oracle against the paper's own numbers
@@ -31,6 +34,9 @@ from .select import (  # noqa: F401
 from .attention import ancestor_sets, tree_attention, tree_attention_paged  # noqa: F401
 from .walk import accept_walk  # noqa: F401
 from .commit import committed_path, kv_commit, kv_commit_paged  # noqa: F401
+from .chunk import chunk_attention_paged  # noqa: F401
 from .decode import decode_attention_paged  # noqa: F401
+from .logprobs import logprobs_row  # noqa: F401
 from .pages import kv_append_paged, kv_reserve_paged  # noqa: F401
+from .rope import qk_rope_paged, rope_frequencies  # noqa: F401
 from .sample import sample, sample_row  # noqa: F401

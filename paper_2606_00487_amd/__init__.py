@@ -24,6 +24,16 @@ Around the round, over a paged cache:
     O = dec(Q, K_pages, V_pages, block_table, kv_len)                 # decode_attn_paged
     smp = TokenSampler(batch, budget, vocab)
     target_tokens, probs = smp(logits, u, tree.n_nodes, temperature=T, top_p=p)   # taps_sample
+
+A prompt, whole or in chunks, over the same cache:
+
+    freq, mscale = rope_frequencies(head_dim, 1e6)
+    rope = PagedQKRope(Hq, Hkv, head_dim, page_rows, freq, mscale=mscale)
+    Qr = rope(Q, K, V, positions, slots, K_pages, V_pages, q_norm, k_norm)    # qk_rope_paged
+    att = PagedChunkAttention(batch, max_rows, Hq, Hkv, head_dim, max_len, page_rows)
+    O = att(Qr, K_pages, V_pages, block_table, q_start, kv_len)               # chunk_attn_paged
+    sco = TokenLogProbs(batch, budget, vocab, top=5)
+    logprob, entropy, rank, top_idx, top_logprob = sco(logits, tokens)        # taps_logprobs
 """
 from __future__ import annotations
 
@@ -596,6 +606,20 @@ class PagedDecodeAttention:
         return O
 
 
+def _need_logits(dev: int, logits: torch.Tensor, batch, budget, vocab, dtype) -> int:
+    """[batch, budget, vocab], rows the same distance apart, which is returned in elements."""
+    if logits.shape != (batch, budget, vocab):
+        raise ValueError(f"logits: expected [{batch}, {budget}, {vocab}], "
+                         f"got {tuple(logits.shape)}")
+    if batch > 1 and budget > 1 and logits.stride(0) != budget * logits.stride(1):
+        raise ValueError("logits: all rows must be the same distance apart")
+    if logits.is_contiguous():
+        _need_on(dev, logits, "logits", dtype)
+        return vocab
+    rows = logits[0] if batch == 1 else logits[:, 0] if budget == 1 else logits.flatten(0, 1)
+    return _need_rows(dev, rows, "logits", dtype, (vocab,), (1,))
+
+
 class TokenSampler:
     """taps_sample: tokens from logits with temperature, top-k, top-p and min-p and given
     random numbers."""
@@ -615,18 +639,8 @@ class TokenSampler:
         others float32) or None.  Returns the tokens [batch, budget] int32 and their
         probabilities, float32."""
         batch, budget, vocab, dtype = self.shape
-        if logits.shape != (batch, budget, vocab):
-            raise ValueError(f"logits: expected [{batch}, {budget}, {vocab}], "
-                             f"got {tuple(logits.shape)}")
-        if batch > 1 and budget > 1 and logits.stride(0) != budget * logits.stride(1):
-            raise ValueError("logits: all rows must be the same distance apart")
-        dev, tdt = _current(), _TORCH_DT[dtype]
-        if logits.is_contiguous():
-            _need_on(dev, logits, "logits", tdt)
-            stride = vocab
-        else:
-            rows = logits[0] if batch == 1 else logits[:, 0] if budget == 1 else logits.flatten(0, 1)
-            stride = _need_rows(dev, rows, "logits", tdt, (vocab,), (1,))
+        dev = _current()
+        stride = _need_logits(dev, logits, batch, budget, vocab, _TORCH_DT[dtype])
         _need_on(dev, u, "u", torch.float32, (batch, budget))
         for t, name, dt in ((n_nodes, "n_nodes", torch.int32), (top_k, "top_k", torch.int32),
                             (temperature, "temperature", torch.float32),
@@ -639,3 +653,170 @@ class TokenSampler:
             _ptr(logits), stride, batch, budget, vocab, dtype, _ptr(n_nodes), ctypes.byref(st),
             _ptr(u), _ptr(tokens), _ptr(probs), None, 0, _stream()))
         return tokens, probs
+
+
+def rope_frequencies(rot_dim, theta=1e6, scaling="none", factor=1.0, trained_len=1,
+                     device="cuda"):
+    """taps_rope_frequencies: the turns per position of a head's rot_dim / 2 pairs in radians
+    (float64 tensor) and the factor of cosines and sines.  scaling: "none", "linear", "ntk" or
+    "yarn" (positions up to `factor` times the trained length; see include/taps.h)."""
+    if scaling not in _lib.ROPE_SCALINGS:
+        raise ValueError(f"scaling: expected one of {', '.join(_lib.ROPE_SCALINGS)}, got {scaling!r}")
+    lib = load()
+    freq, mscale = (ctypes.c_double * max(1, int(rot_dim) // 2))(), ctypes.c_float()
+    _lib.check(lib, "taps_rope_frequencies", lib.taps_rope_frequencies(
+        rot_dim, theta, _lib.ROPE_SCALINGS[scaling], factor, trained_len, freq,
+        ctypes.byref(mscale)))
+    return torch.tensor(list(freq), dtype=torch.float64, device=device), mscale.value
+
+
+class PagedQKRope:
+    """qk_rope_paged: per-head RMSNorm and rotary positions of new queries and keys, and the
+    keys and values into the page pools through a slot map."""
+
+    def __init__(self, Hq, Hkv, head_dim, page_rows, inv_freq, dtype=BF16, interleaved=False,
+                 mscale=1.0, eps=1e-6):
+        """inv_freq: float64 [rot_dim / 2] on the GPU (rope_frequencies); the first rot_dim dims
+        of each head turn, in pairs (j, j + rot_dim / 2), interleaved: (2j, 2j + 1)."""
+        self.lib = load()
+        _need(inv_freq, "inv_freq", torch.float64)
+        if inv_freq.dim() != 1:
+            raise ValueError(f"inv_freq: expected [rot_dim / 2], got {tuple(inv_freq.shape)}")
+        self.shape = (Hq, Hkv, head_dim, int(page_rows), dtype)
+        self.inv_freq = inv_freq
+        self.params = (float(eps), float(mscale), 2 * inv_freq.shape[0], int(bool(interleaved)))
+        self._page = (int(page_rows), Hkv, head_dim)
+        self._qrow, self._row, self._steps = (Hq, head_dim), (Hkv, head_dim), (head_dim, 1)
+
+    def __call__(self, Q, K, V, positions, slot_map, K_pages, V_pages, q_norm=None, k_norm=None,
+                 out=None):
+        """Q: [rows, Hq, head_dim], K, V: [rows, Hkv, head_dim], rows contiguous in themselves
+        (slices of a fused projection's rows are fine).  positions: int32, slot_map: int64, of
+        `rows` entries in any shape; q_norm, k_norm: [head_dim] weights or None.  Returns the
+        queries [rows, Hq, head_dim]."""
+        Hq, Hkv, hd, page_rows, dtype = self.shape
+        tdt = _TORCH_DT[dtype]
+        dev = _current()
+        qs = _need_rows(dev, Q, "Q", tdt, self._qrow, self._steps)
+        ks = _need_rows(dev, K, "K", tdt, self._row, self._steps)
+        vs = _need_rows(dev, V, "V", tdt, self._row, self._steps)
+        rows = Q.shape[0]
+        _need_on(dev, positions, "positions", torch.int32)
+        _need_on(dev, slot_map, "slot_map", torch.int64)
+        if not K.shape[0] == V.shape[0] == positions.numel() == slot_map.numel() == rows:
+            raise ValueError(f"Q has {rows} rows, K {K.shape[0]}, V {V.shape[0]}, positions "
+                             f"{positions.numel()} and slot_map {slot_map.numel()} entries")
+        _need_pools(dev, K_pages, V_pages, tdt, self._page)
+        _need_on(dev, self.inv_freq, "inv_freq", torch.float64)
+        if q_norm is not None:
+            _need_on(dev, q_norm, "q_norm", tdt, (hd,))
+        if k_norm is not None:
+            _need_on(dev, k_norm, "k_norm", tdt, (hd,))
+        if out is None:
+            out = K_pages.new_empty((rows, Hq, hd))
+        else:
+            _need_on(dev, out, "out", tdt, (rows, Hq, hd))
+        st = _lib.Rope(_ptr(self.inv_freq), _ptr(q_norm), _ptr(k_norm), *self.params)
+        _lib.check(self.lib, "qk_rope_paged", self.lib.qk_rope_paged(
+            _ptr(Q), _ptr(K), _ptr(V), qs, ks, vs, _ptr(positions), _ptr(slot_map), rows, Hq,
+            Hkv, hd, dtype, ctypes.byref(st), _ptr(out), _ptr(K_pages), _ptr(V_pages),
+            K_pages.shape[0], page_rows, _stream()))
+        return out
+
+
+class PagedChunkAttention:
+    """chunk_attn_paged: attention of chunks of new tokens, packed one request after the other,
+    over a paged KV cache."""
+
+    def __init__(self, batch, max_rows, Hq, Hkv, head_dim, max_len, page_rows, dtype=BF16,
+                 scale=None, window=0):
+        """max_rows: most rows (new tokens of all requests) of a call."""
+        self.lib = load()
+        self.scale = float(scale if scale is not None else head_dim ** -0.5)
+        self.batch, self.max_rows, self.max_len, self.window = batch, max_rows, max_len, window
+        self.shape = (Hq, Hkv, head_dim, int(page_rows), dtype)
+        _lib.check(self.lib, "chunk_attn_paged_validate", self.lib.chunk_attn_paged_validate(
+            batch, max_rows, Hq, Hkv, head_dim, max_len, int(page_rows), window, dtype,
+            self.scale))
+        self._page = (int(page_rows), Hkv, head_dim)
+        self._row, self._steps = (Hq, head_dim), (head_dim, 1)
+        self._ws = {}   # rows -> bytes of scratch
+
+    def _ws_bytes(self, rows):
+        n = self._ws.get(rows)
+        if n is None:
+            Hq, Hkv, hd, page_rows, dtype = self.shape
+            n = self._ws[rows] = self.lib.chunk_attn_paged_workspace_bytes(
+                self.batch, rows, Hq, Hkv, hd, self.max_len, page_rows, dtype)
+        return n
+
+    def __call__(self, Q, K_pages, V_pages, block_table, q_start, kv_len, out=None):
+        """Q: [rows, Hq, head_dim], rows may be apart; q_start: int32 [batch + 1], request b's
+        tokens are rows q_start[b] .. q_start[b + 1] - 1; kv_len: int32 [batch], theirs among
+        them.  Rows past the last request's are not written.  Each call has scratch of its own
+        (from torch's allocator, on the current stream), so calls may overlap."""
+        Hq, Hkv, hd, page_rows, dtype = self.shape
+        batch, tdt = self.batch, _TORCH_DT[dtype]
+        dev = _current()
+        qs = _need_rows(dev, Q, "Q", tdt, self._row, self._steps)
+        rows = Q.shape[0]
+        if rows > self.max_rows:
+            raise ValueError(f"Q: {rows} rows, at most {self.max_rows}")
+        _need_pools(dev, K_pages, V_pages, tdt, self._page)
+        _need_on(dev, block_table, "block_table", torch.int32)
+        if block_table.dim() != 2 or block_table.shape[0] != batch:
+            raise ValueError(f"block_table: expected [{batch}, max_pages], "
+                             f"got {tuple(block_table.shape)}")
+        _need_on(dev, q_start, "q_start", torch.int32, (batch + 1,))
+        _need_on(dev, kv_len, "kv_len", torch.int32, (batch,))
+        if out is None:
+            O = K_pages.new_empty((rows, Hq, hd))
+        else:
+            O = out
+            _need_on(dev, O, "O", tdt, (rows, Hq, hd))
+        nbytes = self._ws_bytes(rows)
+        ws = K_pages.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+        _lib.check(self.lib, "chunk_attn_paged", self.lib.chunk_attn_paged(
+            _ptr(Q), qs, _ptr(K_pages), _ptr(V_pages), K_pages.shape[0], page_rows,
+            _ptr(block_table), block_table.shape[1], _ptr(q_start), _ptr(kv_len), batch, rows, Hq,
+            Hkv, hd, self.max_len, self.window, dtype, self.scale, _ptr(O), _ptr(ws), nbytes,
+            _stream()))
+        return O
+
+
+class TokenLogProbs:
+    """taps_logprobs: log probabilities and ranks of given tokens, the rows' entropies and top
+    alternatives."""
+
+    def __init__(self, batch, budget, vocab, top=0, dtype=BF16):
+        """budget: rows per request (positions of a prompt, nodes of a tree; 1 in decoding)."""
+        self.lib = load()
+        self.shape = (batch, budget, vocab, top, dtype)
+        _lib.check(self.lib, "taps_logprobs_validate", self.lib.taps_logprobs_validate(
+            batch, budget, vocab, vocab, dtype, top))
+
+    def __call__(self, logits, tokens, n_nodes=None):
+        """logits: [batch, budget, vocab] as for TokenSampler; tokens: [batch, budget] int32;
+        n_nodes: [batch] int32 or None.  Returns the tokens' log probabilities (float32), the
+        rows' entropies (float32), the tokens' ranks (int32), each [batch, budget], and the top
+        alternatives' indices (int32) and log probabilities (float32), [batch, budget, top]."""
+        batch, budget, vocab, top, dtype = self.shape
+        dev = _current()
+        stride = _need_logits(dev, logits, batch, budget, vocab, _TORCH_DT[dtype])
+        _need_on(dev, tokens, "tokens", torch.int32, (batch, budget))
+        if n_nodes is not None:
+            _need_on(dev, n_nodes, "n_nodes", torch.int32, (batch,))
+        # one allocation for all five, 4 bytes a value
+        n = batch * budget
+        buf = tokens.new_empty((3 + 2 * top) * n)
+        rank, top_idx, fl = buf.split_with_sizes((n, top * n, (2 + top) * n))
+        fl = fl.view(torch.float32)
+        logprob, entropy, top_lp = fl.split_with_sizes((n, n, top * n))
+        at = buf.data_ptr()
+        _lib.check(self.lib, "taps_logprobs", self.lib.taps_logprobs(
+            _ptr(logits), stride, batch, budget, vocab, dtype, _ptr(n_nodes), _ptr(tokens), top,
+            at + 4 * (1 + top) * n, at + 4 * (2 + top) * n, at, at + 4 * n,
+            at + 4 * (3 + top) * n, _stream()))
+        return (logprob.view(batch, budget), entropy.view(batch, budget),
+                rank.view(batch, budget), top_idx.view(batch, budget, top),
+                top_lp.view(batch, budget, top))

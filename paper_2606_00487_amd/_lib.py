@@ -26,6 +26,7 @@ TAPS_SCORER_LEARNED = 2
 MAX_BLOCK = 32
 MAX_K = 16
 MAX_BUDGET = 512
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}   # taps_rope_scaling
 
 EXPORTED = [
     "taps_select_workspace_bytes", "taps_select_tables_bytes", "taps_select_validate", "taps_select",
@@ -36,7 +37,9 @@ EXPORTED = [
     "tree_verify_attn_paged_timed", "kv_commit_paged", "verify_layer_paged_workspace_bytes",
     "verify_layer_paged", "kv_reserve_paged", "kv_append_paged", "decode_attn_paged_validate",
     "decode_attn_paged_workspace_bytes", "decode_attn_paged", "taps_sample_validate",
-    "taps_sample_workspace_bytes", "taps_sample",
+    "taps_sample_workspace_bytes", "taps_sample", "taps_rope_frequencies", "qk_rope_paged",
+    "chunk_attn_paged_validate", "chunk_attn_paged_workspace_bytes", "chunk_attn_paged",
+    "taps_logprobs_validate", "taps_logprobs",
 ]
 SELECT_SCRATCH_BYTES = 8 << 20   # TAPS_SELECT_SCRATCH_BYTES
 
@@ -72,6 +75,13 @@ class Tree(ctypes.Structure):
 class Sampling(ctypes.Structure):
     _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
                 ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("q_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p), ("norm_eps", ctypes.c_float),
+                ("mscale", ctypes.c_float), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
 
 
 class TapsError(RuntimeError):
@@ -160,6 +170,22 @@ def load(path: str = LIB_PATH):
     lib.taps_sample.argtypes = [vp, i64, i32, i32, i32, i32, vp, P(Sampling), vp, vp, vp, vp, sz,
                                 vp]
     lib.taps_sample.restype = i32
+    lib.taps_rope_frequencies.argtypes = [i32, f64, i32, f64, i64, P(f64), P(f32)]
+    lib.taps_rope_frequencies.restype = i32
+    lib.qk_rope_paged.argtypes = [vp, vp, vp, i64, i64, i64, vp, vp, i32, i32, i32, i32, i32,
+                                  P(Rope), vp, vp, vp, i32, i32, vp]
+    lib.qk_rope_paged.restype = i32
+    lib.chunk_attn_paged_validate.argtypes = [i32] * 9 + [f32]
+    lib.chunk_attn_paged_validate.restype = i32
+    lib.chunk_attn_paged_workspace_bytes.argtypes = [i32] * 8
+    lib.chunk_attn_paged_workspace_bytes.restype = sz
+    lib.chunk_attn_paged.argtypes = [vp, i64, vp, vp, i32, i32, vp, i32, vp, vp, i32, i32, i32,
+                                     i32, i32, i32, i32, i32, f32, vp, vp, sz, vp]
+    lib.chunk_attn_paged.restype = i32
+    lib.taps_logprobs_validate.argtypes = [i32, i32, i32, i64, i32, i32]
+    lib.taps_logprobs_validate.restype = i32
+    lib.taps_logprobs.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.taps_logprobs.restype = i32
     lib.taps_status_string.argtypes = [i32]
     lib.taps_status_string.restype = ctypes.c_char_p
     lib.taps_spec_exp_host.argtypes = [f64]

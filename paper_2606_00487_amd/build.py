@@ -33,9 +33,11 @@ PER_FILE = {
     "attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "attn_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "chunk.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 SOURCES = ["topk.hip", "select.hip", "attn.hip", "attn_f32.hip", "walk.hip", "commit.hip", "layer.hip",
-           "pages.hip", "decode.hip", "sample.hip", "noalloc.hip", "api.cpp"]
+           "pages.hip", "decode.hip", "sample.hip", "rope.hip", "chunk.hip", "logprobs.hip",
+           "noalloc.hip", "api.cpp"]
 
 
 def hipcc() -> str:

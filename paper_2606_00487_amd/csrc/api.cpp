@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "common.h"
 
@@ -651,6 +652,198 @@ taps_status taps_sample(const void* logits, int64_t row_stride, int32_t batch, i
   if ((a4 & 3) != 0) return TAPS_ERR_INVALID_ARG;
   return launch_sample(logits, row_stride * es, batch, budget, vocab,
                        dtype, n_nodes, *s, u, tokens, probs, stream) == hipSuccess
+             ? TAPS_OK
+             : TAPS_ERR_HIP;
+}
+
+taps_status taps_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor,
+                                  int64_t trained_len, double* inv_freq, float* mscale) {
+  if (rot_dim < 2 || rot_dim > 4096 || (rot_dim & 1) != 0 || !inv_freq || !mscale)
+    return TAPS_ERR_INVALID_ARG;
+  if (!std::isfinite(theta) || !(theta > 1.0)) return TAPS_ERR_INVALID_ARG;
+  if (scaling < TAPS_ROPE_PLAIN || scaling > TAPS_ROPE_YARN) return TAPS_ERR_INVALID_ARG;
+  if (scaling != TAPS_ROPE_PLAIN && (!std::isfinite(factor) || !(factor >= 1.0)))
+    return TAPS_ERR_INVALID_ARG;
+  if (scaling == TAPS_ROPE_YARN && trained_len < 1) return TAPS_ERR_INVALID_ARG;
+  if (scaling == TAPS_ROPE_NTK) {
+    if (rot_dim < 4) return TAPS_ERR_INVALID_ARG;
+    theta *= std::pow(factor, rot_dim / (rot_dim - 2.0));
+    if (!std::isfinite(theta)) return TAPS_ERR_INVALID_ARG;
+  }
+  const double two_pi = 6.283185307179586;
+  for (int j = 0; j < rot_dim / 2; ++j) {
+    double f = std::pow(theta, -2.0 * j / rot_dim);
+    if (scaling == TAPS_ROPE_LINEAR) f /= factor;
+    if (scaling == TAPS_ROPE_YARN) {
+      const double g = std::min(1.0, std::max(0.0, ((double)trained_len * f / two_pi - 1.0) / 31.0));
+      f = g * f + (1.0 - g) * (f / factor);
+    }
+    inv_freq[j] = f;
+  }
+  *mscale = scaling == TAPS_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return TAPS_OK;
+}
+
+// whether [a, a + n) and [b, b + m) bytes meet
+static bool overlap(const void* a, int64_t n, const void* b, int64_t m) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + (uintptr_t)m && y < x + (uintptr_t)n;
+}
+// bytes from the first to the last of `rows` rows
+static int64_t span(int64_t rows, int64_t stride, int64_t row, int es) {
+  return ((rows - 1) * stride + row) * es;
+}
+
+taps_status qk_rope_paged(const void* Q, const void* K, const void* V, int64_t q_stride,
+                          int64_t k_stride, int64_t v_stride, const int32_t* positions,
+                          const int64_t* slot_map, int32_t rows, int32_t Hq, int32_t Hkv,
+                          int32_t head_dim, int32_t dtype, const taps_rope* rope, void* Q_out,
+                          void* K_pages, void* V_pages, int32_t num_pages, int32_t page_rows,
+                          hipStream_t stream) {
+  if (rows < 0 || Hq < 1 || Hkv < 1 || num_pages < 1 || page_shift_of(page_rows) < 0 || !rope)
+    return TAPS_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return TAPS_ERR_UNSUPPORTED;
+  if (dtype != TAPS_BF16 && dtype != TAPS_FP32) return TAPS_ERR_INVALID_ARG;
+  if (rope->rot_dim < 8 || rope->rot_dim > head_dim || rope->rot_dim % 8 != 0)
+    return TAPS_ERR_INVALID_ARG;
+  if (rope->interleaved != 0 && rope->interleaved != 1) return TAPS_ERR_INVALID_ARG;
+  if (!std::isfinite(rope->norm_eps) || rope->norm_eps < 0.f || !std::isfinite(rope->mscale))
+    return TAPS_ERR_INVALID_ARG;
+  if ((int64_t)Hkv * head_dim * 4 > ((int64_t)1 << 24) ||
+      (int64_t)Hq * head_dim * 4 > ((int64_t)1 << 24))
+    return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)num_pages * page_rows > (int64_t)UINT32_MAX) return TAPS_ERR_UNSUPPORTED;
+  const int es = dtype == TAPS_BF16 ? 2 : 4;
+  const int64_t qrow = (int64_t)Hq * head_dim, krow = (int64_t)Hkv * head_dim;
+  if (q_stride < qrow || k_stride < krow || v_stride < krow) return TAPS_ERR_INVALID_ARG;
+  const int64_t most = (int64_t)1 << 31;
+  if (q_stride > most || k_stride > most || v_stride > most) return TAPS_ERR_UNSUPPORTED;
+  if (((q_stride | k_stride | v_stride) * es & 15) != 0) return TAPS_ERR_INVALID_ARG;
+  if (rows == 0) return TAPS_OK;
+  if (!Q || !K || !V || !positions || !slot_map || !rope->inv_freq || !Q_out || !K_pages ||
+      !V_pages)
+    return TAPS_ERR_INVALID_ARG;
+  const uintptr_t a16 = (uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)Q_out |
+                        (uintptr_t)K_pages | (uintptr_t)V_pages | (uintptr_t)rope->q_norm |
+                        (uintptr_t)rope->k_norm;
+  if ((a16 & 15) != 0 || (((uintptr_t)slot_map | (uintptr_t)rope->inv_freq) & 7) != 0 ||
+      ((uintptr_t)positions & 3) != 0)
+    return TAPS_ERR_INVALID_ARG;
+  // a token's row of an output may be written while another wave still reads the inputs
+  const int64_t out = span(rows, qrow, qrow, es), pool = (int64_t)num_pages * page_rows * krow * es;
+  for (const void* o : {(const void*)Q_out, (const void*)K_pages, (const void*)V_pages}) {
+    const int64_t n = o == Q_out ? out : pool;
+    if (overlap(o, n, Q, span(rows, q_stride, qrow, es)) ||
+        overlap(o, n, K, span(rows, k_stride, krow, es)) ||
+        overlap(o, n, V, span(rows, v_stride, krow, es)))
+      return TAPS_ERR_INVALID_ARG;
+  }
+  if (overlap(Q_out, out, K_pages, pool) || overlap(Q_out, out, V_pages, pool) ||
+      overlap(K_pages, pool, V_pages, pool))
+    return TAPS_ERR_INVALID_ARG;
+  return launch_rope(Q, K, V, q_stride * es, k_stride * es, v_stride * es, positions, slot_map,
+                     rows, Hq, Hkv, head_dim, dtype, *rope, Q_out, K_pages, V_pages,
+                     (int64_t)num_pages * page_rows, stream) == hipSuccess
+             ? TAPS_OK
+             : TAPS_ERR_HIP;
+}
+
+taps_status chunk_attn_paged_validate(int32_t batch, int32_t rows, int32_t Hq, int32_t Hkv,
+                                      int32_t head_dim, int32_t max_len, int32_t page_rows,
+                                      int32_t window, int32_t dtype, float scale) {
+  if (batch < 0 || rows < 0 || Hq < 1 || Hkv < 1 || max_len < 0 || window < 0)
+    return TAPS_ERR_INVALID_ARG;
+  if (Hq % Hkv != 0) return TAPS_ERR_INVALID_ARG;
+  if (dtype != TAPS_BF16 && dtype != TAPS_FP32) return TAPS_ERR_INVALID_ARG;
+  if (page_shift_of(page_rows) < 0) return TAPS_ERR_INVALID_ARG;
+  if (!std::isfinite(scale) || !(scale > 0.f)) return TAPS_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return TAPS_ERR_UNSUPPORTED;
+  if (max_len > 1 << 30 || window > 1 << 30) return TAPS_ERR_UNSUPPORTED;
+  // a half tile's 32 rows are addressed with 32-bit offsets
+  if ((int64_t)Hkv * head_dim * 4 > ((int64_t)1 << 24)) return TAPS_ERR_UNSUPPORTED;
+  // query rows of a request and workgroups are counted in 32 bits
+  if (Hq > 65535 || batch > 1 << 20 || (int64_t)rows * Hq > (int64_t)1 << 30)
+    return TAPS_ERR_UNSUPPORTED;
+  if (plan_chunk(batch, rows, Hq, Hkv, max_len, dtype).items * Hkv > (int64_t)1 << 30)
+    return TAPS_ERR_UNSUPPORTED;
+  return TAPS_OK;
+}
+
+size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq, int32_t Hkv,
+                                        int32_t head_dim, int32_t max_len, int32_t page_rows,
+                                        int32_t dtype) {
+  if (chunk_attn_paged_validate(batch, rows, Hq, Hkv, head_dim, max_len, page_rows, 0, dtype,
+                                1.0f) != TAPS_OK ||
+      batch == 0 || rows == 0)
+    return 0;
+  return chunk_ws_bytes(plan_chunk(batch, rows, Hq, Hkv, max_len, dtype), head_dim, dtype);
+}
+
+taps_status chunk_attn_paged(const void* Q, int64_t q_stride, const void* K_pages,
+                             const void* V_pages, int32_t num_pages, int32_t page_rows,
+                             const int32_t* block_table, int32_t max_pages,
+                             const int32_t* q_start, const int32_t* kv_len, int32_t batch,
+                             int32_t rows, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                             int32_t max_len, int32_t window, int32_t dtype, float scale, void* O,
+                             void* ws, size_t ws_bytes, hipStream_t stream) {
+  const taps_status st = chunk_attn_paged_validate(batch, rows, Hq, Hkv, head_dim, max_len,
+                                                   page_rows, window, dtype, scale);
+  if (st != TAPS_OK) return st;
+  if (num_pages < 1 || max_pages < 1) return TAPS_ERR_INVALID_ARG;
+  if ((int64_t)num_pages * page_rows > (int64_t)UINT32_MAX) return TAPS_ERR_UNSUPPORTED;
+  if ((int64_t)max_pages * page_rows < max_len) return TAPS_ERR_INVALID_ARG;
+  const int es = dtype == TAPS_BF16 ? 2 : 4;
+  const int64_t row = (int64_t)Hq * head_dim;
+  if (q_stride < row || (q_stride * es & 15) != 0) return TAPS_ERR_INVALID_ARG;
+  if (q_stride > (int64_t)1 << 31) return TAPS_ERR_UNSUPPORTED;
+  if (batch == 0 || rows == 0) return TAPS_OK;
+  if (!Q || !K_pages || !V_pages || !block_table || !q_start || !kv_len || !O)
+    return TAPS_ERR_INVALID_ARG;
+  const uintptr_t a16 = (uintptr_t)Q | (uintptr_t)K_pages | (uintptr_t)V_pages | (uintptr_t)O;
+  if ((a16 & 15) != 0 ||
+      (((uintptr_t)block_table | (uintptr_t)q_start | (uintptr_t)kv_len) & 3) != 0)
+    return TAPS_ERR_INVALID_ARG;
+  if (overlap(O, span(rows, row, row, es), Q, span(rows, q_stride, row, es)))
+    return TAPS_ERR_INVALID_ARG;
+  const ChunkPlan p = plan_chunk(batch, rows, Hq, Hkv, max_len, dtype);
+  const size_t need = chunk_ws_bytes(p, head_dim, dtype);
+  if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return TAPS_ERR_WORKSPACE;
+  const PagedKV pk{block_table, max_pages, num_pages, page_shift_of(page_rows)};
+  return launch_chunk(Q, q_stride, K_pages, V_pages, pk, q_start, kv_len, batch, rows, Hq, Hkv,
+                      head_dim, max_len, window, dtype, scale, p, O, ws, stream) == hipSuccess
+             ? TAPS_OK
+             : TAPS_ERR_HIP;
+}
+
+taps_status taps_logprobs_validate(int32_t batch, int32_t budget, int32_t vocab,
+                                   int64_t row_stride, int32_t dtype, int32_t top) {
+  const taps_status st = taps_sample_validate(batch, budget, vocab, row_stride, dtype);
+  if (st != TAPS_OK) return st;
+  if (top < 0 || top > vocab) return TAPS_ERR_INVALID_ARG;
+  if (top > TAPS_MAX_LOGPROB_TOP) return TAPS_ERR_UNSUPPORTED;
+  return TAPS_OK;
+}
+
+taps_status taps_logprobs(const void* logits, int64_t row_stride, int32_t batch, int32_t budget,
+                          int32_t vocab, int32_t dtype, const int32_t* n_nodes,
+                          const int32_t* tokens, int32_t top, float* logprob, float* entropy,
+                          int32_t* rank, int32_t* top_idx, float* top_logprob,
+                          hipStream_t stream) {
+  const taps_status st = taps_logprobs_validate(batch, budget, vocab, row_stride, dtype, top);
+  if (st != TAPS_OK) return st;
+  if (batch == 0) return TAPS_OK;
+  if (!logits || !tokens || !logprob || !entropy || !rank) return TAPS_ERR_INVALID_ARG;
+  if (top > 0 && (!top_idx || !top_logprob)) return TAPS_ERR_INVALID_ARG;
+  // as taps_sample: rows of an odd vocabulary begin inside 16 bytes anyway
+  const int es = dtype == TAPS_BF16 ? 2 : 4;
+  const uintptr_t unaligned = ((int64_t)vocab * es & 15) == 0 ? 15 : es - 1;
+  if (((uintptr_t)logits & unaligned) != 0) return TAPS_ERR_INVALID_ARG;
+  const uintptr_t a4 = (uintptr_t)n_nodes | (uintptr_t)tokens | (uintptr_t)logprob |
+                       (uintptr_t)entropy | (uintptr_t)rank | (uintptr_t)top_idx |
+                       (uintptr_t)top_logprob;
+  if ((a4 & 3) != 0) return TAPS_ERR_INVALID_ARG;
+  return launch_logprobs(logits, row_stride * es, batch, budget, vocab, dtype, n_nodes, tokens,
+                         top, logprob, entropy, rank, top_idx, top_logprob, stream) == hipSuccess
              ? TAPS_OK
              : TAPS_ERR_HIP;
 }

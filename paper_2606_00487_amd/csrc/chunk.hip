@@ -1,0 +1,740 @@
+// Attention of chunks of new tokens over a paged KV cache (chunk_attn_paged).
+//
+// Request b brings n new tokens; its cache holds kv rows, theirs the last n.  Token i is at
+// position p = kv - n + i and sees the rows j <= p (within a window: p - window < j <= p):
+// O[i,h] = softmax_j(scale * q_ih . k_jg) v_jg.  The query rows of a KV head are the tokens x the
+// G query heads that share it, in tiles of kM rows; keys go by in tiles of 64.
+//
+// Pieces.  A workgroup takes the keys of one (KV head, query tile), or a part of them: no piece
+// has more than L key tiles, L = all tiles' keys / 256, so that a few long requests fill the chip
+// as well as many short ones.  The requests' lengths are device data: every workgroup forms L
+// and finds its piece from prefix sums over the batch.  Pieces of a tile that was cut leave
+// (O, max, sum) in fp32, which a second kernel adds.
+//
+// bf16 (v_mfma_f32_32x32x16_bf16): eight waves of 32 query rows each share the key tile.
+// S^T = K Q^T (A: keys from LDS, B: queries in registers) leaves a query's scores in two lanes;
+// they go, as P^T, straight into the B operand of O^T += V^T P^T, whose key order follows the
+// accumulators; the transposing LDS read takes V in that order.  K and V cycle through rings of
+// four tiles, filled by loads straight into LDS three tiles ahead; S of the next tile is issued
+// between this one's softmax and products.
+// fp32 (v_mfma_f32_16x16x4_f32): eight waves of 16 query rows, key tiles of 32 staged through
+// registers.
+#include <algorithm>
+
+#include "common.h"
+#include "ldsload.h"
+#include "scan.h"
+
+namespace taps {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 512;
+constexpr int kUnit = 64;      // keys per unit of a piece's length
+constexpr int kTarget = 256;   // pieces that the longest of them is cut for
+constexpr int kMinUnits = 4;   // shorter pieces would be mostly start and end
+
+struct ChunkArgs {
+  const unsigned char *Q, *K, *V;
+  int64_t q_stride;   // elements
+  PagedKV pk;
+  const int32_t *q_start, *kv_len;
+  int batch, rows, Hq, Hkv, max_len, window;
+  float scale_log2;
+  unsigned char* O;
+  float* wsO;     // [slots][kM][HD]; null: no piece is cut
+  float2* wsML;   // [slots][kM]
+  int slots;
+};
+
+// One request's share: n new tokens (rows q0 ..), kv rows, query tiles and the most key units
+// that one of its tiles sees
+struct Request {
+  int q0, n, kv, tiles, units;
+};
+template <int M>
+__device__ inline Request request_of(const ChunkArgs& A, int b, int G) {
+  Request r{0, 0, 0, 0, 0};
+  if (b >= A.batch) return r;
+  r.q0 = min(max(A.q_start[b], 0), A.rows);
+  r.n = max(min(A.q_start[b + 1], A.rows) - r.q0, 0);
+  r.kv = min(max(A.kv_len[b], 0), A.max_len);
+  r.tiles = (int)(((int64_t)r.n * G + M - 1) / M);
+  r.units = (r.kv + kUnit - 1) / kUnit;
+  // the keys of a tile's first to last token's window, wherever they begin in a unit
+  if (A.window > 0) {
+    const int64_t span = (int64_t)A.window + (M + G - 2) / G;
+    r.units = (int)min((int64_t)r.units, (span + kUnit - 2) / kUnit + 1);
+  }
+  return r;
+}
+
+__device__ inline int64_t wave_sum_i64(int64_t v) {
+  return (int64_t)lane_u64(wave_scan_u64((uint64_t)v), kWave - 1);
+}
+
+// Key units per piece at most.  Sum of tiles * units over the batch, times the KV heads, in
+// kTarget parts.
+template <int M>
+__device__ inline int piece_units(const ChunkArgs& A, int G, const Request& first) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int64_t total = wave_sum_i64((int64_t)first.tiles * first.units);
+  for (int b0 = kWave; b0 < A.batch; b0 += kWave) {
+    const Request r = request_of<M>(A, b0 + lane, G);
+    total += wave_sum_i64((int64_t)r.tiles * r.units);
+  }
+  const int64_t L = (total * A.Hkv + kTarget - 1) / kTarget;
+  return (int)max((int64_t)kMinUnits, min(L, (int64_t)1 << 30));
+}
+
+// Piece `item` of the batch (without the KV head), item counting the requests' tiles * splits
+// (cut_only: only those of requests that are cut).  The order within a request: splits, then its
+// tiles from the last one, which sees the most keys.
+struct Piece {
+  int b, q0, n, kv, tile, split, splits, L;
+  int slot;   // of a cut tile's first split; splits of a tile are `tiles` apart
+  int tiles;
+  bool found;
+};
+template <int M>
+__device__ inline Piece find_piece(const ChunkArgs& A, int G, int item, bool tiles_of_cut) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const Request first = request_of<M>(A, lane, G);
+  const bool whole = A.wsO == nullptr;
+  const int L = whole ? 1 << 30 : piece_units<M>(A, G, first);
+  Piece p{};
+  p.L = L;
+  p.found = false;
+  int64_t before = 0, cut_before = 0;
+  for (int b0 = 0; b0 < A.batch; b0 += kWave) {
+    const Request r = b0 == 0 ? first : request_of<M>(A, b0 + lane, G);
+    const int splits = whole ? 1 : max(1, (r.units + L - 1) / L);
+    const int64_t pieces = (int64_t)r.tiles * splits;
+    const int64_t cut = splits > 1 ? pieces : 0;
+    const int64_t count = tiles_of_cut ? (splits > 1 ? r.tiles : 0) : pieces;
+    const int64_t incl = (int64_t)wave_scan_u64((uint64_t)count);
+    const int64_t cut_incl = (int64_t)wave_scan_u64((uint64_t)cut);
+    const uint64_t hit = __ballot(before + incl > item);
+    if (hit) {
+      const int l = __ffsll((long long)hit) - 1;
+      const int64_t at = item - (before + (int64_t)lane_u64((uint64_t)(incl - count), l));
+      auto of = [&](int x) { return (int)__builtin_amdgcn_readlane(x, l); };
+      p.b = b0 + l;
+      p.q0 = of(r.q0), p.n = of(r.n), p.kv = of(r.kv), p.tiles = of(r.tiles);
+      p.splits = of(splits);
+      p.split = (int)(at / p.tiles);
+      p.tile = p.tiles - 1 - (int)(at - (int64_t)p.split * p.tiles);
+      p.slot = (int)(cut_before + (int64_t)lane_u64((uint64_t)(cut_incl - cut), l)) + p.tile;
+      p.found = true;
+      return p;
+    }
+    before += (int64_t)lane_u64((uint64_t)incl, kWave - 1);
+    cut_before += (int64_t)lane_u64((uint64_t)cut_incl, kWave - 1);
+  }
+  return p;
+}
+
+// Keys [lo, hi) that the tokens t0 .. t1 of a request see between them
+__device__ inline void key_range(const ChunkArgs& A, const Piece& p, int t0, int t1, int& lo,
+                                 int& hi) {
+  const int base = p.kv - p.n;
+  hi = max(base + t1 + 1, 0);
+  lo = A.window > 0 ? max(base + t0 - A.window + 1, 0) : 0;
+}
+
+// max and sum over a lane and the one 32 further
+__device__ inline float pair_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float pair_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// permutation of a row's 16-byte chunk index: the rows that an LDS read touches at once land
+// on distinct banks (rows of 16 chunks: all four bits of the row, of 8: three)
+template <int HD>
+__device__ inline int chunk_perm(int r) {
+  if constexpr (HD == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
+  else return ((r & 3) << 1) | ((r >> 2) & 1);
+}
+
+constexpr int kM = 256;   // bf16 query rows per workgroup
+template <int HD>
+__global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int KT = 64;              // keys per tile
+  constexpr int RING = 4;
+  constexpr int ROWB = HD * 2, CPR = ROWB / 16;   // bytes and 16-byte chunks of a row
+  constexpr int TILEB = KT * ROWB;
+  constexpr int NKK = HD / 16, NDB = HD / 32;
+  constexpr int BLKS = TILEB / 1024 / 8;          // 1 KB loads per wave and tile: 2 or 1
+  constexpr int BROWS = 1024 / ROWB;              // rows per load: 4 or 8
+  constexpr int LPG = 2 * BLKS;                   // loads per wave and step (V and K)
+  typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+  __shared__ __attribute__((aligned(1024))) unsigned char s_k[RING * TILEB], s_v[RING * TILEB];
+
+  const int G = A.Hq / A.Hkv;
+  const int kvh = blockIdx.x % A.Hkv;
+  const Piece p = find_piece<kM>(A, G, blockIdx.x / A.Hkv, false);
+  if (!p.found) return;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int last = p.n * G - 1;                   // last query row
+  const int row0 = p.tile * kM;
+  int lo, hi;
+  key_range(A, p, row0 / G, min(row0 + kM - 1, last) / G, lo, hi);
+  // this piece's key tiles [k0, k0 + nt * 64)
+  const int u0 = lo / kUnit, u1 = (hi + kUnit - 1) / kUnit;
+  const int ub = u0 + min((int64_t)p.split * p.L, (int64_t)(u1 - u0));
+  const int ue = (int)min((int64_t)ub + p.L, (int64_t)u1);
+  const bool cut = p.splits > 1;
+  if (cut && ub >= ue && p.split > 0) return;     // the tile has no such piece
+  const int nt = __builtin_amdgcn_readfirstlane(max(ue - ub, 0));
+  const int k0 = __builtin_amdgcn_readfirstlane(ub * kUnit);
+  const int k_end = __builtin_amdgcn_readfirstlane(min(hi, ue * kUnit));
+  const int k_lo = __builtin_amdgcn_readfirstlane(lo);
+
+  // this wave's query rows, tokens and positions
+  const int wrow0 = row0 + wave * 32;
+  const int qrow = min(wrow0 + l32, last);
+  const int tok = qrow / G, head = kvh * G + (qrow - tok * G);
+  const bool live = wrow0 + l32 <= last;
+  const int base = p.kv - p.n;
+  const int pos = live ? base + tok : -1;                          // sees keys <= pos
+  const int from = A.window > 0 ? pos - A.window + 1 : 0;          // and >= from
+  // (uniform) first and last position of the wave's rows; tiles outside are skipped
+  const int pos_lo = __builtin_amdgcn_readfirstlane(base + wrow0 / G);
+  const int pos_hi = __builtin_amdgcn_readfirstlane(
+      wrow0 <= last ? base + min(wrow0 + 31, last) / G : -1);
+  const int w_lo = A.window > 0 ? pos_lo - A.window + 1 : 0;
+  const int from_hi = A.window > 0 ? pos_hi - A.window + 1 : 0;
+  int tb = max(w_lo - k0, 0) / KT, te = pos_hi < k0 ? 0 : min((pos_hi - k0) / KT + 1, nt);
+  if (wrow0 > last) te = 0;
+  if (tb >= te) tb = te = 0;
+  tb = __builtin_amdgcn_readfirstlane(tb), te = __builtin_amdgcn_readfirstlane(te);
+
+  bf16x8 q[NKK];
+  {
+    const __bf16* const qp =
+        (const __bf16*)A.Q + (size_t)(p.q0 + tok) * A.q_stride + (size_t)head * HD;
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk) q[kk] = *(const bf16x8*)(qp + kk * 16 + hl * 8);
+  }
+
+  // ---- direct loads: block j of a tile (1 KB, BROWS rows) is wave j % 8's; a block lies in one
+  // half tile (32 keys), i.e. in one page.  Lane l of the wave holds the page of half tile l of
+  // the 64 from half tile pw on.
+  const uint32_t rsb = (uint32_t)A.Hkv * ROWB;
+  const int lr = lane / CPR;                      // row within the block
+  const int32_t* const bt = A.pk.btab + (size_t)p.b * A.pk.max_pages;
+  auto entries = [&](int h0) {
+    const int r = min((k0 >> 5) + h0 + lane, (k_end - 1) >> 5);   // half tiles of the piece only
+    const int e = (int)(((int64_t)max(r, 0) * 32) >> A.pk.page_shift);
+    return min(max(bt[min(e, A.pk.max_pages - 1)], 0), A.pk.num_pages - 1);
+  };
+  int pw = 0, pages = 0, pages_next = 0;
+  if (nt > 0) pages = entries(0), pages_next = entries(64);
+  const uint32_t ldk = __builtin_amdgcn_readfirstlane(lds_address(s_k));
+  const uint32_t ldv = __builtin_amdgcn_readfirstlane(lds_address(s_v));
+  const uint64_t kbase = (uint64_t)(A.K + (size_t)kvh * ROWB);
+  const uint64_t vbase = (uint64_t)(A.V + (size_t)kvh * ROWB);
+  // (past the piece nothing is read from memory; rows before the first visible key read 0 too)
+  auto issue = [&](uint64_t src, uint32_t dst, int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < BLKS; ++j) {
+      const int blk = wave + 8 * j, half = blk * BROWS / 32;
+      const int r0 = k0 + t * KT + half * 32;     // the half tile's first key
+      const int rows = min(max(k_end - r0, 0), 32);
+      const int pg = __builtin_amdgcn_readlane(pages, (2 * t + half - pw) & 63);
+      const uint64_t prow = ((uint64_t)(uint32_t)pg << A.pk.page_shift) |
+                            (uint32_t)(r0 & ((1 << A.pk.page_shift) - 1));
+      const int r = blk * BROWS % 32 + lr;        // row in the half tile
+      const int tr = blk * BROWS + lr;            // and in the tile
+      uint32_t off = (uint32_t)r * rsb + (uint32_t)(((lane % CPR) ^ chunk_perm<HD>(tr)) * 16);
+      off = r0 + r < k_lo ? 0x7FFFFF00u : off;
+      load_lds16_at(buffer_rsrc((const void*)(src + prow * rsb), (uint32_t)rows * rsb),
+                    dst + blk * 1024, off);
+    }
+  };
+  auto turn_pages = [&](int t) __attribute__((always_inline)) {   // tile t's pages are at hand
+    if (2 * t - pw >= 64) {
+      pw += 64;
+      pages = pages_next;
+      pages_next = entries(pw + 64);
+    }
+  };
+
+  // ---- LDS read offsets within a slot
+  const int fk = chunk_perm<HD>(l32);
+  uint32_t koff[NKK];
+#pragma unroll
+  for (int kk = 0; kk < NKK; ++kk) koff[kk] = l32 * ROWB + 16 * ((2 * kk + hl) ^ fk);
+  const int g16 = (lane >> 4) & 1, tq = (lane & 15) >> 2, qq = lane & 3;
+  uint32_t voff[2][NDB];
+#pragma unroll
+  for (int h8 = 0; h8 < 2; ++h8)
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      const int r = 8 * h8 + 4 * hl + tq;
+      voff[h8][db] =
+          r * ROWB + 8 * (qq & 1) + 16 * ((4 * db + 2 * g16 + (qq >> 1)) ^ chunk_perm<HD>(r));
+    }
+
+  f32x16 o[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
+  float m_ref = -INFINITY, l_run = 0.f, m_thr = -INFINITY, m_neg = 0.f;
+  const float thr8 = 8.f / A.scale_log2;
+
+  auto scores = [&](int slot, f32x16 (&s)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        const bf16x8 a = *(const bf16x8*)(s_k + slot * TILEB + kb * 32 * ROWB + koff[kk]);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[kk], s[kb], 0, 0, 0);
+      }
+    }
+  };
+  // P of the tile whose first key is `key`, from its scores
+  auto softmax = [&](f32x16 (&s)[2], int key, bf16x8 (&pr)[4]) __attribute__((always_inline)) {
+    if (key + KT - 1 > pos_lo || key < from_hi) {
+      const int a = pos - key, f = from - key;    // local keys f .. a
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int k = kb * 32 + 8 * (v >> 2) + 4 * hl + (v & 3);
+          s[kb][v] = k <= a && k >= f ? s[kb][v] : -INFINITY;
+        }
+    }
+    float mx = s[0][0], my = s[1][0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[0][v]), my = fmaxf(my, s[1][v]);
+    mx = pair_max(fmaxf(mx, my));
+    const bool upd = mx > m_thr;                  // move the reference by > 2^8 only
+    if (__ballot(upd)) {
+      const float nref = upd ? mx * A.scale_log2 : m_ref;
+      const float alpha = upd ? __builtin_amdgcn_exp2f(m_ref - nref) : 1.f;
+      m_thr = upd ? mx + thr8 : m_thr;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
+      m_ref = nref;
+      m_neg = m_ref == -INFINITY ? 0.f : -m_ref;
+    }
+#pragma unroll
+    for (int hf = 0; hf < 4; ++hf) {
+      float e[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        e[t] = __builtin_amdgcn_exp2f(fmaf(s[hf >> 1][(hf & 1) * 8 + t], A.scale_log2, m_neg));
+#pragma unroll
+      for (int t = 0; t < 8; ++t) pr[hf][t] = (__bf16)e[t];
+      l_run += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+    }
+  };
+  auto accumulate = [&](int slot, const bf16x8 (&pr)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int hf = 0; hf < 4; ++hf)
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        const unsigned char* const at = s_v + slot * TILEB + 16 * hf * ROWB;
+        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + voff[0][db]));
+        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + voff[1][db]));
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), pr[hf], o[db], 0, 0, 0);
+      }
+  };
+
+  if (nt > 0) {
+    issue(kbase, ldk, 0);
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      issue(vbase, ldv + t * TILEB, t);
+      issue(kbase, ldk + (t + 1) * TILEB, t + 1);
+    }
+    TAPS_WAIT_VMCNT(3 * LPG);                     // K(0): this wave's part
+    TAPS_LDS_BARRIER();                           // ... and every other wave's
+    f32x16 sc[2], sn[2];
+    if (tb == 0 && te > 0) scores(0, sc);
+    for (int t = 0; t < nt; ++t) {
+      // V(t) and K(t + 1) have landed: two steps' loads may be out.  The barrier also says that
+      // every wave has read K(t) and V(t - 1), whose slots are filled next.
+      TAPS_WAIT_VMCNT(2 * LPG);
+      TAPS_LDS_BARRIER();
+      turn_pages(t + 3);
+      issue(vbase, ldv + ((t + 3) & 3) * TILEB, t + 3);
+      turn_pages(t + 4);
+      issue(kbase, ldk + (t & 3) * TILEB, t + 4);
+      if (t + 1 >= tb && t + 1 < te) scores((t + 1) & 3, sn);
+      if (t >= tb && t < te) {
+        bf16x8 pr[4];
+        softmax(sc, k0 + t * KT, pr);
+        accumulate(t & 3, pr);
+      }
+      sc[0] = sn[0];
+      sc[1] = sn[1];
+    }
+    TAPS_WAIT_VMCNT(0);   // (empty) loads past the piece land before the LDS is released
+  }
+
+  const float l = pair_sum(l_run);
+  if (!live) return;
+  if (!cut) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;   // no key: zeros
+    __bf16* const out = (__bf16*)A.O + ((size_t)(p.q0 + tok) * A.Hq + head) * HD;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        bf16x4 x;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x[t] = (__bf16)(o[db][4 * r + t] * inv);
+        *(bf16x4*)(out + db * 32 + 8 * r + 4 * hl) = x;
+      }
+    return;
+  }
+  const int64_t slot = ((int64_t)p.slot + (int64_t)p.split * p.tiles) * A.Hkv + kvh;
+  if (slot >= A.slots) return;
+  const size_t at = (size_t)slot * kM + wave * 32 + l32;
+  float* const out = A.wsO + at * HD;
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      *(f32x4*)(out + db * 32 + 8 * r + 4 * hl) =
+          f32x4{o[db][4 * r], o[db][4 * r + 1], o[db][4 * r + 2], o[db][4 * r + 3]};
+  if (hl == 0) A.wsML[at] = make_float2(m_ref, l);   // (base 2, after the scale)
+#endif
+}
+
+// max and sum over the four lanes that share l % 16, in each of them
+__device__ inline float quad_max(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  return pair_max(x);
+}
+__device__ inline float quad_sum(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  return pair_sum(x);
+}
+
+// Lane (g = l / 16, c = l % 16).  S^T: the lane holds the dims 16 j + 4 g + 0..3 of key c and of
+// query c, four k-steps a load, and ends with the scores of query c for the keys 4 g + 0..3 of the
+// 16.  O^T += V^T P^T: k-step r takes the keys 4 g + r; row m of block t is dim m * HD / 16 + t, so
+// that a lane reads HD / 16 consecutive dims of a V row.
+constexpr int kMF = 128;   // fp32 query rows per workgroup
+template <int HD>
+__global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) {
+  constexpr int KT = 32;
+  constexpr int DPL = HD / 16, J = HD / 16;
+  constexpr int ROW = HD + 4;                     // LDS row stride: rows 4 banks apart
+  constexpr int CPR = HD / 4;                     // 16-byte chunks of a row
+  constexpr int LD = KT * CPR / kThreads;         // chunks per thread and tile: 2 or 1
+  __shared__ float s_k[2][KT][ROW], s_v[2][KT][ROW];
+
+  const int G = A.Hq / A.Hkv;
+  const int kvh = blockIdx.x % A.Hkv;
+  const Piece p = find_piece<kMF>(A, G, blockIdx.x / A.Hkv, false);
+  if (!p.found) return;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int last = p.n * G - 1;
+  const int row0 = p.tile * kMF;
+  int lo, hi;
+  key_range(A, p, row0 / G, min(row0 + kMF - 1, last) / G, lo, hi);
+  const int u0 = lo / kUnit, u1 = (hi + kUnit - 1) / kUnit;
+  const int ub = u0 + min((int64_t)p.split * p.L, (int64_t)(u1 - u0));
+  const int ue = (int)min((int64_t)ub + p.L, (int64_t)u1);
+  const bool cut = p.splits > 1;
+  if (cut && ub >= ue && p.split > 0) return;
+  const int k0 = ub * kUnit, k_end = min(hi, ue * kUnit);
+  const int nt = k_end > k0 ? (k_end - k0 + KT - 1) / KT : 0;
+
+  const int wrow0 = row0 + wave * 16;
+  const int qrow = min(wrow0 + c, last);
+  const int tok = qrow / G, head = kvh * G + (qrow - tok * G);
+  const bool live = wrow0 + c <= last;
+  const int base = p.kv - p.n;
+  const int pos = live ? base + tok : -1;
+  const int from = A.window > 0 ? pos - A.window + 1 : 0;
+  const int pos_lo = base + wrow0 / G;
+  const int pos_hi = wrow0 <= last ? base + min(wrow0 + 15, last) / G : -1;
+  const int w_lo = A.window > 0 ? pos_lo - A.window + 1 : 0;
+  const int from_hi = A.window > 0 ? pos_hi - A.window + 1 : 0;
+
+  f32x4 q[J];
+  {
+    const float* const qp =
+        (const float*)A.Q + (size_t)(p.q0 + tok) * A.q_stride + (size_t)head * HD;
+#pragma unroll
+    for (int j = 0; j < J; ++j) q[j] = *(const f32x4*)(qp + 16 * j + 4 * g);
+  }
+  const size_t rs = (size_t)A.Hkv * HD;
+  const float *const Kp = (const float*)A.K + (size_t)kvh * HD, *const Vp = (const float*)A.V + (size_t)kvh * HD;
+  const int32_t* const bt = A.pk.btab + (size_t)p.b * A.pk.max_pages;
+  f32x4 xk[LD], xv[LD];
+  auto load = [&](int t) {   // keys outside [lo, k_end) read as zeros
+    const int r0 = k0 + t * KT;
+    const int page = min(max(bt[min(r0 >> A.pk.page_shift, A.pk.max_pages - 1)], 0), A.pk.num_pages - 1);
+    const size_t prow = ((size_t)page << A.pk.page_shift) + (r0 & ((1 << A.pk.page_shift) - 1));
+#pragma unroll
+    for (int j = 0; j < LD; ++j) {
+      const int i = tid + j * kThreads, r = i / CPR, d = (i % CPR) * 4;
+      const bool in = r0 + r >= lo && r0 + r < k_end;
+      const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+      xk[j] = in ? *(const f32x4*)(Kp + (prow + r) * rs + d) : z;
+      xv[j] = in ? *(const f32x4*)(Vp + (prow + r) * rs + d) : z;
+    }
+  };
+  auto keep = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < LD; ++j) {
+      const int i = tid + j * kThreads, r = i / CPR, d = (i % CPR) * 4;
+      *(f32x4*)&s_k[buf][r][d] = xk[j];
+      *(f32x4*)&s_v[buf][r][d] = xv[j];
+    }
+  };
+
+  f32x4 o[DPL];
+#pragma unroll
+  for (int t = 0; t < DPL; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // the reference stays in score units: the exponent is (s - m) * scale, whose rounding error
+  // falls with the weight of the term
+  float m_ref = -INFINITY, l_run = 0.f;
+  if (nt > 0) {
+    load(0);
+    keep(0);
+  }
+  __syncthreads();
+  for (int t = 0; t < nt; ++t) {
+    const int key = k0 + t * KT, buf = t & 1;
+    if (t + 1 < nt) load(t + 1);
+    if (key <= pos_hi && key + KT > w_lo) {
+      f32x4 s[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        f32x4 sp[4];   // four partial sums per score: chains a quarter as long round less
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sp[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const f32x4 k = *(const f32x4*)&s_k[buf][16 * i + c][16 * j + 4 * g];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sp[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[j][e], sp[e], 0, 0, 0);
+        }
+        s[i] = (sp[0] + sp[1]) + (sp[2] + sp[3]);
+      }
+      if (key + KT - 1 > pos_lo || key < from_hi) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int k = key + 16 * i + 4 * g + r;
+            s[i][r] = k <= pos && k >= from ? s[i][r] : -INFINITY;
+          }
+      }
+      const float mx = quad_max(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                                      fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
+      const bool upd = (mx - m_ref) * A.scale_log2 > 8.f;
+      if (__ballot(upd)) {
+        const float nref = upd ? mx : m_ref;
+        const float alpha =
+            !upd ? 1.f
+                 : m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_ref - nref) * A.scale_log2);
+        l_run *= alpha;
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) o[d] *= alpha;
+        m_ref = nref;
+      }
+      const float mu = m_ref == -INFINITY ? 0.f : m_ref;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float e[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f((s[i][r] - mu) * A.scale_log2);
+        l_run += (e[0] + e[1]) + (e[2] + e[3]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float* const v = &s_v[buf][16 * i + 4 * g + r][DPL * c];
+#pragma unroll
+          for (int d = 0; d < DPL; d += 4) {
+            const f32x4 x = *(const f32x4*)(v + d);
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              o[d + w] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[w], e[r], o[d + w], 0, 0, 0);
+          }
+        }
+      }
+    }
+    if (t + 1 < nt) keep(buf ^ 1);   // read last before the barrier behind step t - 1
+    __syncthreads();
+  }
+
+  const float l = quad_sum(l_run);
+  if (!live) return;
+  // row r of block t is dim (4 g + r) * DPL + t of query c
+  float* out;
+  float inv = 1.f;
+  if (!cut) {
+    inv = l == 0.f ? 0.f : 1.f / l;
+    out = (float*)A.O + ((size_t)(p.q0 + tok) * A.Hq + head) * HD;
+  } else {
+    const int64_t slot = ((int64_t)p.slot + (int64_t)p.split * p.tiles) * A.Hkv + kvh;
+    if (slot >= A.slots) return;
+    const size_t at = (size_t)slot * kMF + wave * 16 + c;
+    out = A.wsO + at * HD;
+    // (base 2, after the scale)
+    if (g == 0) A.wsML[at] = make_float2(m_ref * A.scale_log2, l);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int d = 0; d < DPL; d += 4)
+      *(f32x4*)(out + (4 * g + r) * DPL + d) = f32x4{o[d][r], o[d + 1][r], o[d + 2][r], o[d + 3][r]} * inv;
+}
+
+// Adds the pieces of the tiles that were cut: a workgroup per (KV head, cut tile, 16 query rows),
+// a row per 16 threads.
+constexpr int kCombineThreads = 256, kCombineRows = 16;
+__device__ inline void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
+__device__ inline void store4(__bf16* p, const f32x4& x) {
+  bf16x4 r;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) r[t] = (__bf16)x[t];
+  *(bf16x4*)p = r;
+}
+template <typename T, int HD, int M>
+__global__ __launch_bounds__(kCombineThreads) void chunk_combine_kernel(const ChunkArgs A) {
+  constexpr int TPR = kCombineThreads / kCombineRows, W = HD / TPR;   // dims per thread: 8 or 4
+  const int G = A.Hq / A.Hkv, kvh = blockIdx.x % A.Hkv;
+  const Piece p = find_piece<M>(A, G, blockIdx.x / A.Hkv, true);
+  if (!p.found) return;
+  const int last = p.n * G - 1, row0 = p.tile * M;
+  const int r = blockIdx.y * kCombineRows + threadIdx.x / TPR, d = threadIdx.x % TPR * W;
+  if (row0 + r > last) return;
+  int lo, hi;
+  key_range(A, p, row0 / G, min(row0 + M - 1, last) / G, lo, hi);
+  const int units = (hi + kUnit - 1) / kUnit - lo / kUnit;
+  const int pieces = max(1, (int)(((int64_t)units + p.L - 1) / p.L));
+  auto at = [&](int s) {
+    return ((size_t)((int64_t)p.slot + (int64_t)s * p.tiles) * A.Hkv + kvh) * M + r;
+  };
+  if (((int64_t)p.slot + (int64_t)(pieces - 1) * p.tiles) * A.Hkv + kvh >= A.slots) return;
+  float Mx = -INFINITY, L = 0.f;
+  f32x4 acc[W / 4];
+#pragma unroll
+  for (int w = 0; w < W / 4; ++w) acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr int CH = 4;
+  for (int s0 = 0; s0 < pieces; s0 += CH) {
+    float2 ml[CH];
+    f32x4 x[CH][W / 4];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const size_t i = at(min(s0 + k, pieces - 1));
+      ml[k] = A.wsML[i];
+#pragma unroll
+      for (int w = 0; w < W / 4; ++w) x[k][w] = *(const f32x4*)(A.wsO + i * HD + d + 4 * w);
+    }
+    float Mc = Mx;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) Mc = fmaxf(Mc, ml[k].x);
+    const float a = Mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(Mx - Mc);
+    L *= a;
+#pragma unroll
+    for (int w = 0; w < W / 4; ++w) acc[w] *= a;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      if (s0 + k >= pieces) continue;
+      if (ml[k].x != -INFINITY) {
+        const float e = __builtin_amdgcn_exp2f(ml[k].x - Mc);
+        L += e * ml[k].y;
+#pragma unroll
+        for (int w = 0; w < W / 4; ++w) acc[w] += e * x[k][w];
+      }
+      if (ml[k].y != ml[k].y) L = ml[k].y;   // a NaN score moves no maximum
+    }
+    Mx = Mc;
+  }
+  const int tok = (row0 + r) / G, head = kvh * G + (row0 + r - tok * G);
+  T* const out = (T*)A.O + ((size_t)(p.q0 + tok) * A.Hq + head) * HD + d;
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+  for (int w = 0; w < W / 4; ++w) store4(out + 4 * w, acc[w] * inv);
+}
+
+template <typename T, int HD>
+hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
+  const unsigned grid = (unsigned)(p.items * A.Hkv);
+  constexpr int M = sizeof(T) == 2 ? kM : kMF;
+  if constexpr (sizeof(T) == 2) chunk_bf16_kernel<HD><<<grid, kThreads, 0, s>>>(A);
+  else chunk_f32_kernel<HD><<<grid, kThreads, 0, s>>>(A);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.slots == 0) return e;
+  chunk_combine_kernel<T, HD, M>
+      <<<dim3((unsigned)(p.cut_tiles * A.Hkv), M / kCombineRows), kCombineThreads, 0, s>>>(A);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Bounds of what the device finds.  Tiles: the requests' rows / M, and one more per request.
+// With L >= (sum of tiles * units) * Hkv / kTarget, the cut requests (units > L) have at most
+// kTarget / Hkv tiles between them, and at most twice as many pieces as their tiles * units / L.
+ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int max_len, int dtype) {
+  ChunkPlan p;
+  const int64_t M = dtype == TAPS_BF16 ? kM : kMF;
+  const int64_t tiles = std::min<int64_t>((int64_t)rows * (Hq / Hkv) / M + batch,
+                                          (int64_t)rows * (Hq / Hkv));
+  const bool may_cut = max_len > kMinUnits * kUnit;
+  const int64_t cut = std::min<int64_t>(tiles, std::max(1, kTarget / Hkv));
+  p.cut_tiles = may_cut ? cut : 0;
+  p.slots = may_cut ? (int64_t)Hkv * std::max(1, 2 * kTarget / Hkv) : 0;
+  p.items = tiles + p.slots / Hkv;
+  return p;
+}
+
+size_t chunk_ws_bytes(const ChunkPlan& p, int head_dim, int dtype) {
+  return (size_t)p.slots * (dtype == TAPS_BF16 ? kM : kMF) * (head_dim * sizeof(float) + sizeof(float2));
+}
+
+hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const void* V,
+                        const PagedKV& pk, const int32_t* q_start, const int32_t* kv_len,
+                        int batch, int rows, int Hq, int Hkv, int head_dim, int max_len,
+                        int window, int dtype, float scale, const ChunkPlan& p, void* O, void* ws,
+                        hipStream_t s) {
+  if (batch <= 0 || rows <= 0) return hipSuccess;
+  ChunkArgs A;
+  A.Q = (const unsigned char*)Q, A.K = (const unsigned char*)K, A.V = (const unsigned char*)V;
+  A.q_stride = q_stride, A.pk = pk, A.q_start = q_start, A.kv_len = kv_len;
+  A.batch = batch, A.rows = rows, A.Hq = Hq, A.Hkv = Hkv, A.max_len = max_len, A.window = window;
+  A.scale_log2 = scale * 1.4426950408889634f;
+  A.O = (unsigned char*)O;
+  A.slots = (int)p.slots;
+  A.wsO = p.slots ? (float*)ws : nullptr;
+  A.wsML = p.slots
+               ? (float2*)((float*)ws + (size_t)p.slots * (dtype == TAPS_BF16 ? kM : kMF) * head_dim)
+               : nullptr;
+  if (dtype == TAPS_BF16)
+    return head_dim == 128 ? launch_t<__bf16, 128>(A, p, s) : launch_t<__bf16, 64>(A, p, s);
+  return head_dim == 128 ? launch_t<float, 128>(A, p, s) : launch_t<float, 64>(A, p, s);
+}
+
+}  // namespace taps

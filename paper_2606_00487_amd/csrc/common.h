@@ -178,6 +178,33 @@ hipError_t launch_sample(const void* logits, int64_t row_bytes, int batch, int b
                          int dtype, const int32_t* n_nodes, const taps_sampling& s,
                          const float* u, int32_t* tokens, float* probs, hipStream_t stream);
 
+// Norm, rotation and cache write of new rows; strides in bytes
+hipError_t launch_rope(const void* Q, const void* K, const void* V, int64_t q_stride_bytes,
+                       int64_t k_stride_bytes, int64_t v_stride_bytes, const int32_t* pos,
+                       const int64_t* slots, int rows, int Hq, int Hkv, int head_dim, int dtype,
+                       const taps_rope& r, void* Qo, void* Kp, void* Vp, int64_t pool_rows,
+                       hipStream_t s);
+
+// Chunks of new tokens over a paged cache: query tiles, cut along the keys where few
+struct ChunkPlan {
+  int64_t items;       // most pieces per KV head
+  int64_t cut_tiles;   // most query tiles per KV head that are cut (0: none ever is)
+  int64_t slots;       // most pieces of cut tiles, all KV heads
+};
+ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int max_len, int dtype);
+size_t chunk_ws_bytes(const ChunkPlan& p, int head_dim, int dtype);
+// q_stride in elements
+hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const void* V,
+                        const PagedKV& pk, const int32_t* q_start, const int32_t* kv_len,
+                        int batch, int rows, int Hq, int Hkv, int head_dim, int max_len,
+                        int window, int dtype, float scale, const ChunkPlan& p, void* O, void* ws,
+                        hipStream_t s);
+
+hipError_t launch_logprobs(const void* logits, int64_t row_bytes, int batch, int budget,
+                           int vocab, int dtype, const int32_t* n_nodes, const int32_t* tokens,
+                           int top, float* logprob, float* entropy, int32_t* rank,
+                           int32_t* top_idx, float* top_logprob, hipStream_t s);
+
 double spec_exp_host(double t);
 
 }  // namespace taps
