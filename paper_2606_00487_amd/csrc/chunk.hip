@@ -15,7 +15,7 @@
 // S^T = K Q^T (A: keys from LDS, B: queries in registers) leaves a query's scores in two lanes;
 // they go, as P^T, straight into the B operand of O^T += V^T P^T, whose key order follows the
 // accumulators; the transposing LDS read takes V in that order.  K and V cycle through rings of
-// four tiles, filled by loads straight into LDS three tiles ahead; S of the next tile is issued
+// three tiles, filled by loads straight into LDS two tiles ahead; S of the next tile is issued
 // between this one's softmax and products.
 // fp32 (v_mfma_f32_16x16x4_f32): eight waves of 16 query rows, key tiles of 32 staged through
 // registers.
@@ -30,6 +30,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -167,17 +168,20 @@ __device__ inline int chunk_perm(int r) {
 }
 
 constexpr int kM = 256;   // bf16 query rows per workgroup
+template <int P>
+struct Slot {
+  static constexpr int value = P;
+};
 template <int HD>
 __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int KT = 64;              // keys per tile
-  constexpr int RING = 4;
+  constexpr int RING = 3;             // tiles of K and of V in LDS
   constexpr int ROWB = HD * 2, CPR = ROWB / 16;   // bytes and 16-byte chunks of a row
   constexpr int TILEB = KT * ROWB;
   constexpr int NKK = HD / 16, NDB = HD / 32;
-  constexpr int BLKS = TILEB / 1024 / 8;          // 1 KB loads per wave and tile: 2 or 1
+  constexpr int BPW = TILEB / 1024 / 4;           // 1 KB loads per wave and tile: 4 or 2
   constexpr int BROWS = 1024 / ROWB;              // rows per load: 4 or 8
-  constexpr int LPG = 2 * BLKS;                   // loads per wave and step (V and K)
   typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
   __shared__ __attribute__((aligned(1024))) unsigned char s_k[RING * TILEB], s_v[RING * TILEB];
 
@@ -208,18 +212,14 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
   const int tok = qrow / G, head = kvh * G + (qrow - tok * G);
   const bool live = wrow0 + l32 <= last;
   const int base = p.kv - p.n;
-  const int pos = live ? base + tok : -1;                          // sees keys <= pos
-  const int from = A.window > 0 ? pos - A.window + 1 : 0;          // and >= from
-  // (uniform) first and last position of the wave's rows; tiles outside are skipped
-  const int pos_lo = __builtin_amdgcn_readfirstlane(base + wrow0 / G);
+  const int place = live ? base + tok : -1;
+  const int pos = min(place, k_end - 1);                           // sees keys <= pos
+  const int from = A.window > 0 ? place - A.window + 1 : 0;        // and >= from
+  // (uniform) first and last position of the wave's rows
+  const int pos_lo = __builtin_amdgcn_readfirstlane(min(base + wrow0 / G, k_end - 1));
   const int pos_hi = __builtin_amdgcn_readfirstlane(
       wrow0 <= last ? base + min(wrow0 + 31, last) / G : -1);
-  const int w_lo = A.window > 0 ? pos_lo - A.window + 1 : 0;
   const int from_hi = A.window > 0 ? pos_hi - A.window + 1 : 0;
-  int tb = max(w_lo - k0, 0) / KT, te = pos_hi < k0 ? 0 : min((pos_hi - k0) / KT + 1, nt);
-  if (wrow0 > last) te = 0;
-  if (tb >= te) tb = te = 0;
-  tb = __builtin_amdgcn_readfirstlane(tb), te = __builtin_amdgcn_readfirstlane(te);
 
   bf16x8 q[NKK];
   {
@@ -229,54 +229,65 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
     for (int kk = 0; kk < NKK; ++kk) q[kk] = *(const bf16x8*)(qp + kk * 16 + hl * 8);
   }
 
-  // ---- direct loads: block j of a tile (1 KB, BROWS rows) is wave j % 8's; a block lies in one
-  // half tile (32 keys), i.e. in one page.  Lane l of the wave holds the page of half tile l of
-  // the 64 from half tile pw on.
+  // ---- direct loads.  Waves 0-3 load K, waves 4-7 V, of each tile one half (32 keys, in one page)
+  // per two waves, BPW blocks of 1 KB each.  Lane l holds the page of this wave's half of tile
+  // pw + l.
   const uint32_t rsb = (uint32_t)A.Hkv * ROWB;
-  const int lr = lane / CPR;                      // row within the block
+  const int half = (wave >> 1) & 1;
   const int32_t* const bt = A.pk.btab + (size_t)p.b * A.pk.max_pages;
-  auto entries = [&](int h0) {
-    const int r = min((k0 >> 5) + h0 + lane, (k_end - 1) >> 5);   // half tiles of the piece only
-    const int e = (int)(((int64_t)max(r, 0) * 32) >> A.pk.page_shift);
-    return min(max(bt[min(e, A.pk.max_pages - 1)], 0), A.pk.num_pages - 1);
+  auto entries = [&](int t0) {
+    const int r = min(k0 + (t0 + lane) * KT + half * 32, k_end - 1);   // rows of the piece only
+    const int e = min(max(r, 0) >> A.pk.page_shift, A.pk.max_pages - 1);
+    return min(max(bt[e], 0), A.pk.num_pages - 1);
   };
   int pw = 0, pages = 0, pages_next = 0;
   if (nt > 0) pages = entries(0), pages_next = entries(64);
-  const uint32_t ldk = __builtin_amdgcn_readfirstlane(lds_address(s_k));
-  const uint32_t ldv = __builtin_amdgcn_readfirstlane(lds_address(s_v));
-  const uint64_t kbase = (uint64_t)(A.K + (size_t)kvh * ROWB);
-  const uint64_t vbase = (uint64_t)(A.V + (size_t)kvh * ROWB);
-  // (past the piece nothing is read from memory; rows before the first visible key read 0 too)
-  auto issue = [&](uint64_t src, uint32_t dst, int t) __attribute__((always_inline)) {
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(wave < 4 ? s_k : s_v)) +
+                        (uint32_t)(half * 2 + (wave & 1)) * BPW * 1024;
+  const uint64_t src0 = (uint64_t)((wave < 4 ? A.K : A.V) + (size_t)kvh * ROWB);
+  uint32_t ld_off[BPW];
 #pragma unroll
-    for (int j = 0; j < BLKS; ++j) {
-      const int blk = wave + 8 * j, half = blk * BROWS / 32;
-      const int r0 = k0 + t * KT + half * 32;     // the half tile's first key
-      const int rows = min(max(k_end - r0, 0), 32);
-      const int pg = __builtin_amdgcn_readlane(pages, (2 * t + half - pw) & 63);
-      const uint64_t prow = ((uint64_t)(uint32_t)pg << A.pk.page_shift) |
-                            (uint32_t)(r0 & ((1 << A.pk.page_shift) - 1));
-      const int r = blk * BROWS % 32 + lr;        // row in the half tile
-      const int tr = blk * BROWS + lr;            // and in the tile
-      uint32_t off = (uint32_t)r * rsb + (uint32_t)(((lane % CPR) ^ chunk_perm<HD>(tr)) * 16);
-      off = r0 + r < k_lo ? 0x7FFFFF00u : off;
-      load_lds16_at(buffer_rsrc((const void*)(src + prow * rsb), (uint32_t)rows * rsb),
-                    dst + blk * 1024, off);
-    }
-  };
-  auto turn_pages = [&](int t) __attribute__((always_inline)) {   // tile t's pages are at hand
-    if (2 * t - pw >= 64) {
+  for (int j = 0; j < BPW; ++j) {
+    const int r = ((wave & 1) * BPW + j) * BROWS + lane / CPR;         // row in the half tile
+    ld_off[j] = (uint32_t)r * rsb + (uint32_t)(((lane % CPR) ^ chunk_perm<HD>(r)) * 16);
+  }
+  // (past the piece nothing is read from memory; rows before the first visible key read 0 too)
+  auto issue = [&](int slot, int t) __attribute__((always_inline)) {
+    if (t - pw >= 64) {
       pw += 64;
       pages = pages_next;
       pages_next = entries(pw + 64);
     }
+    const int r0 = k0 + t * KT + half * 32;       // the half tile's first key
+    const int rows = min(max(k_end - r0, 0), 32);
+    const int pg = __builtin_amdgcn_readlane(pages, (t - pw) & 63);
+    const uint64_t prow = ((uint64_t)(uint32_t)pg << A.pk.page_shift) |
+                          (uint32_t)(r0 & ((1 << A.pk.page_shift) - 1));
+    const i32x4 rs = buffer_rsrc((const void*)(src0 + prow * rsb), (uint32_t)rows * rsb);
+    if (r0 < k_lo) {
+      int ln = lane;
+      asm volatile("" : "+v"(ln));                // (rare: nothing of it is kept in registers)
+#pragma unroll
+      for (int j = 0; j < BPW; ++j) {
+        const int r = ((wave & 1) * BPW + j) * BROWS + ln / CPR;
+        load_lds16_at(rs, lds0 + slot * TILEB + j * 1024, r0 + r < k_lo ? 0x7FFFFF00u : ld_off[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < BPW; ++j) load_lds16_at(rs, lds0 + slot * TILEB + j * 1024, ld_off[j]);
+    }
   };
 
-  // ---- LDS read offsets within a slot
+  // ---- LDS read addresses in slot 0, opaque so that the slots are constant offsets
+  typedef __attribute__((address_space(3))) unsigned char lds_u8;
+  typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
   const int fk = chunk_perm<HD>(l32);
   uint32_t koff[NKK];
 #pragma unroll
-  for (int kk = 0; kk < NKK; ++kk) koff[kk] = l32 * ROWB + 16 * ((2 * kk + hl) ^ fk);
+  for (int kk = 0; kk < NKK; ++kk) {
+    koff[kk] = (uint32_t)(uintptr_t)(lds_u8*)s_k + l32 * ROWB + 16 * ((2 * kk + hl) ^ fk);
+    asm volatile("" : "+v"(koff[kk]));
+  }
   const int g16 = (lane >> 4) & 1, tq = (lane & 15) >> 2, qq = lane & 3;
   uint32_t voff[2][NDB];
 #pragma unroll
@@ -284,8 +295,9 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
 #pragma unroll
     for (int db = 0; db < NDB; ++db) {
       const int r = 8 * h8 + 4 * hl + tq;
-      voff[h8][db] =
-          r * ROWB + 8 * (qq & 1) + 16 * ((4 * db + 2 * g16 + (qq >> 1)) ^ chunk_perm<HD>(r));
+      voff[h8][db] = (uint32_t)(uintptr_t)(lds_u8*)s_v + r * ROWB + 8 * (qq & 1) +
+                     16 * ((4 * db + 2 * g16 + (qq >> 1)) ^ chunk_perm<HD>(r));
+      asm volatile("" : "+v"(voff[h8][db]));
     }
 
   f32x16 o[NDB];
@@ -293,38 +305,42 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
   for (int db = 0; db < NDB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
-  float m_ref = -INFINITY, l_run = 0.f, m_thr = -INFINITY, m_neg = 0.f;
+  float m_ref = -INFINITY, m_thr = -INFINITY, m_neg = 0.f;
+  float l_run = 0.f;
   const float thr8 = 8.f / A.scale_log2;
 
-  auto scores = [&](int slot, f32x16 (&s)[2]) __attribute__((always_inline)) {
+  // k-steps [a, b) of the scores of key block kb
+  auto scores = [&](int slot, int kb, int a, int b, f32x16& s) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kk = a; kk < b; ++kk) {
+      if (kk == 0) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+        for (int v = 0; v < 16; ++v) s[v] = 0.f;
+      }
+      const bf16x8 x = *(const lds_bf16x8*)(koff[kk] + (slot * TILEB + kb * 32 * ROWB));
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[kk], s, 0, 0, 0);
+    }
+  };
+  auto mask = [&](f32x16& s0, f32x16& s1, int key) __attribute__((always_inline)) {
+    if (key + KT - 1 > pos_lo || key < from_hi) {
+      const int a = pos - key - 4 * hl, f = from - key - 4 * hl;   // the lane's keys f .. a
 #pragma unroll
-      for (int kk = 0; kk < NKK; ++kk) {
-        const bf16x8 a = *(const bf16x8*)(s_k + slot * TILEB + kb * 32 * ROWB + koff[kk]);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[kk], s[kb], 0, 0, 0);
+      for (int v = 0; v < 16; ++v) {
+        const int k = 8 * (v >> 2) + (v & 3);
+        s0[v] = k <= a && k >= f ? s0[v] : -INFINITY;
+        s1[v] = k + 32 <= a && k + 32 >= f ? s1[v] : -INFINITY;
       }
     }
   };
-  // P of the tile whose first key is `key`, from its scores
-  auto softmax = [&](f32x16 (&s)[2], int key, bf16x8 (&pr)[4]) __attribute__((always_inline)) {
-    if (key + KT - 1 > pos_lo || key < from_hi) {
-      const int a = pos - key, f = from - key;    // local keys f .. a
+  auto tile_max = [&](const f32x16& s0, const f32x16& s1) __attribute__((always_inline)) {
+    float mx = s0[0], my = s1[0];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int k = kb * 32 + 8 * (v >> 2) + 4 * hl + (v & 3);
-          s[kb][v] = k <= a && k >= f ? s[kb][v] : -INFINITY;
-        }
-    }
-    float mx = s[0][0], my = s[1][0];
-#pragma unroll
-    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[0][v]), my = fmaxf(my, s[1][v]);
-    mx = pair_max(fmaxf(mx, my));
-    const bool upd = mx > m_thr;                  // move the reference by > 2^8 only
+    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s0[v]), my = fmaxf(my, s1[v]);
+    return pair_max(fmaxf(mx, my));
+  };
+  // the reference moves only when exceeded by > 2^8
+  auto rescale = [&](float mx) __attribute__((always_inline)) {
+    const bool upd = mx > m_thr;
     if (__ballot(upd)) {
       const float nref = upd ? mx * A.scale_log2 : m_ref;
       const float alpha = upd ? __builtin_amdgcn_exp2f(m_ref - nref) : 1.f;
@@ -337,58 +353,89 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
       m_ref = nref;
       m_neg = m_ref == -INFINITY ? 0.f : -m_ref;
     }
+  };
+  // the weights of 16 keys (8 in this lane), the first or second half of a key block.  Their sum
+  // takes the rounded ones, as the product does.
+  auto weights = [&](const f32x16& s, int hf) __attribute__((always_inline)) {
+    bf16x8 w;
 #pragma unroll
-    for (int hf = 0; hf < 4; ++hf) {
-      float e[8];
+    for (int t = 0; t < 8; ++t)
+      w[t] = (__bf16)__builtin_amdgcn_exp2f(
+          fmaf(s[hf * 8 + t], A.scale_log2, m_neg));
+    const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
-        e[t] = __builtin_amdgcn_exp2f(fmaf(s[hf >> 1][(hf & 1) * 8 + t], A.scale_log2, m_neg));
+    for (int t = 0; t < 8; t += 2)
+      l_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[t], w[t + 1]}, one, l_run, false);
+    return w;
+  };
+  auto product = [&](int slot, int hf, const bf16x8& w) __attribute__((always_inline)) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t) pr[hf][t] = (__bf16)e[t];
-      l_run += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+    for (int db = 0; db < NDB; ++db) {
+      const uint32_t at = slot * TILEB + 16 * hf * ROWB;
+      const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(voff[0][db] + at));
+      const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(voff[1][db] + at));
+      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), w, o[db], 0, 0, 0);
     }
   };
-  auto accumulate = [&](int slot, const bf16x8 (&pr)[4]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int hf = 0; hf < 4; ++hf)
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) {
-        const unsigned char* const at = s_v + slot * TILEB + 16 * hf * ROWB;
-        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + voff[0][db]));
-        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + voff[1][db]));
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), pr[hf], o[db], 0, 0, 0);
-      }
+
+  // Begin of step t (slot P = t mod 3): V(t) and K(t + 1) have landed (the wave's loads of one more
+  // tile may be out).  The barrier also says that every wave has read K(t) and V(t - 1), whose
+  // slots are filled next.
+  auto advance = [&](int P, int t) __attribute__((always_inline)) {
+    TAPS_WAIT_VMCNT(BPW);
+    TAPS_LDS_BARRIER();
+    issue(wave < 4 ? P : (P + 2) % 3, wave < 4 ? t + 3 : t + 2);
+  };
+  // Step t: the weights and products of tile t, from its scores (s0, s1), and the scores of tile t + 1
+  // (past the last one: of zeros) into n0 and, when they are used up, s0.
+  auto step = [&](auto pt, int t, f32x16& s0, f32x16& s1, f32x16& n0)
+                  __attribute__((always_inline)) {
+    constexpr int P = decltype(pt)::value, PN = (P + 1) % 3;
+    advance(P, t);
+    scores(PN, 0, 0, NKK / 2, n0);
+    mask(s0, s1, k0 + t * KT);
+    rescale(tile_max(s0, s1));
+    __builtin_amdgcn_sched_barrier(0);
+    const bf16x8 w0 = weights(s0, 0);
+    scores(PN, 0, NKK / 2, NKK, n0);
+    __builtin_amdgcn_sched_barrier(0);
+    product(P, 0, w0);
+    const bf16x8 w1 = weights(s0, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    scores(PN, 1, 0, NKK / 2, s0);
+    product(P, 1, w1);
+    const bf16x8 w2 = weights(s1, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    scores(PN, 1, NKK / 2, NKK, s0);
+    product(P, 2, w2);
+    const bf16x8 w3 = weights(s1, 1);
+    asm volatile("" : "+v"(l_run));               // (the sum is not put off to the next step)
+    __builtin_amdgcn_sched_barrier(0);
+    product(P, 3, w3);
   };
 
   if (nt > 0) {
-    issue(kbase, ldk, 0);
-#pragma unroll
-    for (int t = 0; t < 3; ++t) {
-      issue(vbase, ldv + t * TILEB, t);
-      issue(kbase, ldk + (t + 1) * TILEB, t + 1);
-    }
-    TAPS_WAIT_VMCNT(3 * LPG);                     // K(0): this wave's part
+    // In whole turns of the rings, so that the loop has one exit (with three, the accumulators
+    // moved between registers and did not all fit); keys past the piece are masked.
+    const int steps = (nt + 2) / 3 * 3;
+    // K(0) .. K(2), V(0), V(1)
+    issue(0, 0);
+    issue(1, 1);
+    if (wave < 4) issue(2, 2);
+    if (wave < 4) TAPS_WAIT_VMCNT(2 * BPW);       // K(0): this wave's part
     TAPS_LDS_BARRIER();                           // ... and every other wave's
-    f32x16 sc[2], sn[2];
-    if (tb == 0 && te > 0) scores(0, sc);
-    for (int t = 0; t < nt; ++t) {
-      // V(t) and K(t + 1) have landed: two steps' loads may be out.  The barrier also says that
-      // every wave has read K(t) and V(t - 1), whose slots are filled next.
-      TAPS_WAIT_VMCNT(2 * LPG);
-      TAPS_LDS_BARRIER();
-      turn_pages(t + 3);
-      issue(vbase, ldv + ((t + 3) & 3) * TILEB, t + 3);
-      turn_pages(t + 4);
-      issue(kbase, ldk + (t & 3) * TILEB, t + 4);
-      if (t + 1 >= tb && t + 1 < te) scores((t + 1) & 3, sn);
-      if (t >= tb && t < te) {
-        bf16x8 pr[4];
-        softmax(sc, k0 + t * KT, pr);
-        accumulate(t & 3, pr);
+    if (wrow0 > last) {                           // no rows: the wave only loads
+      for (int t = 0, P = 0; t < steps; ++t, P = P == 2 ? 0 : P + 1) advance(P, t);
+    } else {
+      f32x16 a, b, c;
+      scores(0, 0, 0, NKK, a);
+      scores(0, 1, 0, NKK, b);
+      for (int t = 0; t < steps; t += 3) {
+        step(Slot<0>(), t, a, b, c);
+        step(Slot<1>(), t + 1, c, a, b);
+        step(Slot<2>(), t + 2, b, c, a);
       }
-      sc[0] = sn[0];
-      sc[1] = sn[1];
     }
     TAPS_WAIT_VMCNT(0);   // (empty) loads past the piece land before the LDS is released
   }
