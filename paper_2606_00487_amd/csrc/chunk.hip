@@ -168,6 +168,18 @@ __device__ inline int chunk_perm(int r) {
 }
 
 constexpr int kM = 256;   // bf16 query rows per workgroup
+// the order of a region's instructions: N times a matrix product, DS LDS reads, V vector and T
+// transcendental instructions
+template <int N, int DS, int V, int T>
+__device__ __attribute__((always_inline)) inline void interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, DS, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+    __builtin_amdgcn_sched_group_barrier(0x400, T, 0);
+  }
+}
 template <int P>
 struct Slot {
   static constexpr int value = P;
@@ -251,30 +263,36 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
     const int r = ((wave & 1) * BPW + j) * BROWS + lane / CPR;         // row in the half tile
     ld_off[j] = (uint32_t)r * rsb + (uint32_t)(((lane % CPR) ^ chunk_perm<HD>(r)) * 16);
   }
-  // (past the piece nothing is read from memory; rows before the first visible key read 0 too)
-  auto issue = [&](int slot, int t) __attribute__((always_inline)) {
+  // `next` is the resource over the half tile that this wave loads next, `key` its first key: its
+  // address is formed among the matrix products, far from the barrier that the loads follow.
+  // Past the piece nothing is read from memory; rows before the first visible key read 0 too.
+  i32x4 next = {0, 0, 0, 0};
+  int key = 0;
+  auto prepare = [&](int t) __attribute__((always_inline)) {
     if (t - pw >= 64) {
       pw += 64;
       pages = pages_next;
       pages_next = entries(pw + 64);
     }
-    const int r0 = k0 + t * KT + half * 32;       // the half tile's first key
-    const int rows = min(max(k_end - r0, 0), 32);
+    key = k0 + t * KT + half * 32;
+    const int rows = min(max(k_end - key, 0), 32);
     const int pg = __builtin_amdgcn_readlane(pages, (t - pw) & 63);
     const uint64_t prow = ((uint64_t)(uint32_t)pg << A.pk.page_shift) |
-                          (uint32_t)(r0 & ((1 << A.pk.page_shift) - 1));
-    const i32x4 rs = buffer_rsrc((const void*)(src0 + prow * rsb), (uint32_t)rows * rsb);
-    if (r0 < k_lo) {
+                          (uint32_t)(key & ((1 << A.pk.page_shift) - 1));
+    next = buffer_rsrc((const void*)(src0 + prow * rsb), (uint32_t)rows * rsb);
+  };
+  auto issue = [&](int slot) __attribute__((always_inline)) {
+    if (key < k_lo) {
       int ln = lane;
       asm volatile("" : "+v"(ln));                // (rare: nothing of it is kept in registers)
 #pragma unroll
       for (int j = 0; j < BPW; ++j) {
         const int r = ((wave & 1) * BPW + j) * BROWS + ln / CPR;
-        load_lds16_at(rs, lds0 + slot * TILEB + j * 1024, r0 + r < k_lo ? 0x7FFFFF00u : ld_off[j]);
+        load_lds16_at(next, lds0 + slot * TILEB + j * 1024, key + r < k_lo ? 0x7FFFFF00u : ld_off[j]);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < BPW; ++j) load_lds16_at(rs, lds0 + slot * TILEB + j * 1024, ld_off[j]);
+      for (int j = 0; j < BPW; ++j) load_lds16_at(next, lds0 + slot * TILEB + j * 1024, ld_off[j]);
     }
   };
 
@@ -309,6 +327,18 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
   float l_run = 0.f;
   const float thr8 = 8.f / A.scale_log2;
 
+  // Operands wait in registers: each is replaced by the one four k-steps (V: 16 keys) on as soon as
+  // its product has been issued.
+  bf16x8 ka[4], va[NDB];
+  auto read_k = [&](int slot, int i) __attribute__((always_inline)) {   // i: key block, k-step
+    ka[i & 3] = *(const lds_bf16x8*)(koff[i % NKK] + (slot * TILEB + i / NKK * 32 * ROWB));
+  };
+  auto read_v = [&](int slot, int hf, int db) __attribute__((always_inline)) {
+    const uint32_t at = slot * TILEB + 16 * hf * ROWB;
+    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(voff[0][db] + at));
+    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(voff[1][db] + at));
+    va[db] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
   // k-steps [a, b) of the scores of key block kb
   auto scores = [&](int slot, int kb, int a, int b, f32x16& s) __attribute__((always_inline)) {
 #pragma unroll
@@ -317,11 +347,19 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
 #pragma unroll
         for (int v = 0; v < 16; ++v) s[v] = 0.f;
       }
-      const bf16x8 x = *(const lds_bf16x8*)(koff[kk] + (slot * TILEB + kb * 32 * ROWB));
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[kk], s, 0, 0, 0);
+      const int i = kb * NKK + kk;
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[i & 3], q[kk], s, 0, 0, 0);
+      if (i + 4 < 2 * NKK) read_k(slot, i + 4);
     }
   };
-  auto mask = [&](f32x16& s0, f32x16& s1, int key) __attribute__((always_inline)) {
+  auto largest = [&](const f32x16& s) __attribute__((always_inline)) {
+    float x = s[0], y = s[1];
+#pragma unroll
+    for (int v = 2; v < 16; v += 2) x = fmaxf(x, s[v]), y = fmaxf(y, s[v + 1]);
+    return fmaxf(x, y);
+  };
+  // the tile's largest score per query (m0: of the first key block)
+  auto tile_max = [&](f32x16& s0, f32x16& s1, int key, float m0) __attribute__((always_inline)) {
     if (key + KT - 1 > pos_lo || key < from_hi) {
       const int a = pos - key - 4 * hl, f = from - key - 4 * hl;   // the lane's keys f .. a
 #pragma unroll
@@ -330,13 +368,9 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
         s0[v] = k <= a && k >= f ? s0[v] : -INFINITY;
         s1[v] = k + 32 <= a && k + 32 >= f ? s1[v] : -INFINITY;
       }
+      m0 = largest(s0);
     }
-  };
-  auto tile_max = [&](const f32x16& s0, const f32x16& s1) __attribute__((always_inline)) {
-    float mx = s0[0], my = s1[0];
-#pragma unroll
-    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s0[v]), my = fmaxf(my, s1[v]);
-    return pair_max(fmaxf(mx, my));
+    return pair_max(fmaxf(m0, largest(s1)));
   };
   // the reference moves only when exceeded by > 2^8
   auto rescale = [&](float mx) __attribute__((always_inline)) {
@@ -371,48 +405,60 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
   auto product = [&](int slot, int hf, const bf16x8& w) __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < NDB; ++db) {
-      const uint32_t at = slot * TILEB + 16 * hf * ROWB;
-      const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(voff[0][db] + at));
-      const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(voff[1][db] + at));
-      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), w, o[db], 0, 0, 0);
+      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[db], w, o[db], 0, 0, 0);
+      if (hf < 3) read_v(slot, hf + 1, db);
     }
   };
 
   // Begin of step t (slot P = t mod 3): V(t) and K(t + 1) have landed (the wave's loads of one more
   // tile may be out).  The barrier also says that every wave has read K(t) and V(t - 1), whose
   // slots are filled next.
-  auto advance = [&](int P, int t) __attribute__((always_inline)) {
+  auto advance = [&]() __attribute__((always_inline)) {
     TAPS_WAIT_VMCNT(BPW);
     TAPS_LDS_BARRIER();
-    issue(wave < 4 ? P : (P + 2) % 3, wave < 4 ? t + 3 : t + 2);
   };
-  // Step t: the weights and products of tile t, from its scores (s0, s1), and the scores of tile t + 1
-  // (past the last one: of zeros) into n0 and, when they are used up, s0.
+  const int ahead = wave < 4 ? 3 : 2;             // tiles from a step's to the one it loads
+  auto fill = [&](int P) __attribute__((always_inline)) { issue(wave < 4 ? P : (P + 2) % 3); };
+  // Step t: the weights and products of tile t, from its scores (s0, s1; m0: the largest of s0),
+  // and the scores of tile t + 1 (past the last one: of zeros) into n0 and, when they are used
+  // up, s0.
+  float m0 = -INFINITY;
   auto step = [&](auto pt, int t, f32x16& s0, f32x16& s1, f32x16& n0)
                   __attribute__((always_inline)) {
     constexpr int P = decltype(pt)::value, PN = (P + 1) % 3;
-    advance(P, t);
-    scores(PN, 0, 0, NKK / 2, n0);
-    mask(s0, s1, k0 + t * KT);
-    rescale(tile_max(s0, s1));
+    advance();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) read_k(PN, i);
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) read_v(P, 0, db);
+    rescale(tile_max(s0, s1, k0 + t * KT, m0));
     __builtin_amdgcn_sched_barrier(0);
     const bf16x8 w0 = weights(s0, 0);
-    scores(PN, 0, NKK / 2, NKK, n0);
+    scores(PN, 0, 0, NKK, n0);
+    interleave<NKK, 1, 24 / NKK - 1, 1>();
+    __builtin_amdgcn_sched_barrier(0);
+    fill(P);
     __builtin_amdgcn_sched_barrier(0);
     product(P, 0, w0);
     const bf16x8 w1 = weights(s0, 1);
+    interleave<NDB, 2, 16 / NDB, 8 / NDB>();
     __builtin_amdgcn_sched_barrier(0);
-    scores(PN, 1, 0, NKK / 2, s0);
     product(P, 1, w1);
+    scores(PN, 1, 0, NKK / 2, s0);
     const bf16x8 w2 = weights(s1, 0);
+    interleave<NDB + NKK / 2, 2, 2, 1>();
     __builtin_amdgcn_sched_barrier(0);
-    scores(PN, 1, NKK / 2, NKK, s0);
+    prepare(t + 1 + ahead);
+    __builtin_amdgcn_sched_barrier(0);
     product(P, 2, w2);
+    scores(PN, 1, NKK / 2, NKK, s0);
     const bf16x8 w3 = weights(s1, 1);
     asm volatile("" : "+v"(l_run));               // (the sum is not put off to the next step)
+    interleave<NDB + NKK / 2, 2, 2, 1>();
     __builtin_amdgcn_sched_barrier(0);
     product(P, 3, w3);
+    m0 = largest(n0);
+    asm volatile("" : "+v"(m0));
   };
 
   if (nt > 0) {
@@ -420,17 +466,30 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
     // moved between registers and did not all fit); keys past the piece are masked.
     const int steps = (nt + 2) / 3 * 3;
     // K(0) .. K(2), V(0), V(1)
-    issue(0, 0);
-    issue(1, 1);
-    if (wave < 4) issue(2, 2);
-    if (wave < 4) TAPS_WAIT_VMCNT(2 * BPW);       // K(0): this wave's part
+    prepare(0);
+    issue(0);
+    prepare(1);
+    issue(1);
+    prepare(2);
+    if (wave < 4) {
+      issue(2);
+      prepare(3);
+      TAPS_WAIT_VMCNT(2 * BPW);                   // K(0): this wave's part
+    }
     TAPS_LDS_BARRIER();                           // ... and every other wave's
     if (wrow0 > last) {                           // no rows: the wave only loads
-      for (int t = 0, P = 0; t < steps; ++t, P = P == 2 ? 0 : P + 1) advance(P, t);
+      for (int t = 0, P = 0; t < steps; ++t, P = P == 2 ? 0 : P + 1) {
+        advance();
+        fill(P);
+        prepare(t + 1 + ahead);
+      }
     } else {
       f32x16 a, b, c;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) read_k(0, i);
       scores(0, 0, 0, NKK, a);
       scores(0, 1, 0, NKK, b);
+      m0 = largest(a);
       for (int t = 0; t < steps; t += 3) {
         step(Slot<0>(), t, a, b, c);
         step(Slot<1>(), t + 1, c, a, b);
