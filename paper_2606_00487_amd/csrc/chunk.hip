@@ -92,17 +92,18 @@ __device__ inline int piece_units(const ChunkArgs& A, int G, const Request& firs
   return (int)max((int64_t)kMinUnits, min(L, (int64_t)1 << 30));
 }
 
-// Piece `item` of the batch (without the KV head), item counting the requests' tiles * splits
-// (cut_only: only those of requests that are cut).  The order within a request: splits, then its
-// tiles from the last one, which sees the most keys.
+// Piece `item` of the batch (without the KV head), item counting the requests' tiles * splits.  The
+// order within a request: splits, then its tiles from the last one, which sees the most keys.
+// ROWS > 0: instead group `item` of ROWS query rows of the requests that are cut.
 struct Piece {
   int b, q0, n, kv, tile, split, splits, L;
-  int slot;   // of a cut tile's first split; splits of a tile are `tiles` apart
+  int slot;    // of the tile's first split; splits of a tile are `tiles` apart
   int tiles;
+  int group;   // ROWS > 0: the request's group of rows
   bool found;
 };
-template <int M>
-__device__ inline Piece find_piece(const ChunkArgs& A, int G, int item, bool tiles_of_cut) {
+template <int M, int ROWS>
+__device__ inline Piece find_piece(const ChunkArgs& A, int G, int item) {
   const int lane = threadIdx.x & (kWave - 1);
   const Request first = request_of<M>(A, lane, G);
   const bool whole = A.wsO == nullptr;
@@ -116,19 +117,26 @@ __device__ inline Piece find_piece(const ChunkArgs& A, int G, int item, bool til
     const int splits = whole ? 1 : max(1, (r.units + L - 1) / L);
     const int64_t pieces = (int64_t)r.tiles * splits;
     const int64_t cut = splits > 1 ? pieces : 0;
-    const int64_t count = tiles_of_cut ? (splits > 1 ? r.tiles : 0) : pieces;
+    int64_t count = pieces;
+    if constexpr (ROWS > 0) count = splits > 1 ? ((int64_t)r.n * G + ROWS - 1) / ROWS : 0;
     const int64_t incl = (int64_t)wave_scan_u64((uint64_t)count);
     const int64_t cut_incl = (int64_t)wave_scan_u64((uint64_t)cut);
     const uint64_t hit = __ballot(before + incl > item);
     if (hit) {
       const int l = __ffsll((long long)hit) - 1;
-      const int64_t at = item - (before + (int64_t)lane_u64((uint64_t)(incl - count), l));
+      // (at most item)
+      const int at = (int)(item - (before + (int64_t)lane_u64((uint64_t)(incl - count), l)));
       auto of = [&](int x) { return (int)__builtin_amdgcn_readlane(x, l); };
       p.b = b0 + l;
       p.q0 = of(r.q0), p.n = of(r.n), p.kv = of(r.kv), p.tiles = of(r.tiles);
       p.splits = of(splits);
-      p.split = (int)(at / p.tiles);
-      p.tile = p.tiles - 1 - (int)(at - (int64_t)p.split * p.tiles);
+      if constexpr (ROWS > 0) {
+        p.group = at;
+        p.tile = at / (M / ROWS);
+      } else {
+        p.split = p.splits == 1 ? 0 : at / p.tiles;
+        p.tile = p.tiles - 1 - (at - p.split * p.tiles);
+      }
       p.slot = (int)(cut_before + (int64_t)lane_u64((uint64_t)(cut_incl - cut), l)) + p.tile;
       p.found = true;
       return p;
@@ -199,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
 
   const int G = A.Hq / A.Hkv;
   const int kvh = blockIdx.x % A.Hkv;
-  const Piece p = find_piece<kM>(A, G, blockIdx.x / A.Hkv, false);
+  const Piece p = find_piece<kM, 0>(A, G, blockIdx.x / A.Hkv);
   if (!p.found) return;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -288,7 +296,8 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
 #pragma unroll
       for (int j = 0; j < BPW; ++j) {
         const int r = ((wave & 1) * BPW + j) * BROWS + ln / CPR;
-        load_lds16_at(next, lds0 + slot * TILEB + j * 1024, key + r < k_lo ? 0x7FFFFF00u : ld_off[j]);
+        const uint32_t off = key + r < k_lo ? 0x7FFFFF00u : ld_off[j];
+        load_lds16_at(next, lds0 + slot * TILEB + j * 1024, off);
       }
     } else {
 #pragma unroll
@@ -557,7 +566,7 @@ __global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) 
 
   const int G = A.Hq / A.Hkv;
   const int kvh = blockIdx.x % A.Hkv;
-  const Piece p = find_piece<kMF>(A, G, blockIdx.x / A.Hkv, false);
+  const Piece p = find_piece<kMF, 0>(A, G, blockIdx.x / A.Hkv);
   if (!p.found) return;
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -593,12 +602,14 @@ __global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) 
     for (int j = 0; j < J; ++j) q[j] = *(const f32x4*)(qp + 16 * j + 4 * g);
   }
   const size_t rs = (size_t)A.Hkv * HD;
-  const float *const Kp = (const float*)A.K + (size_t)kvh * HD, *const Vp = (const float*)A.V + (size_t)kvh * HD;
+  const float* const Kp = (const float*)A.K + (size_t)kvh * HD;
+  const float* const Vp = (const float*)A.V + (size_t)kvh * HD;
   const int32_t* const bt = A.pk.btab + (size_t)p.b * A.pk.max_pages;
   f32x4 xk[LD], xv[LD];
   auto load = [&](int t) {   // keys outside [lo, k_end) read as zeros
     const int r0 = k0 + t * KT;
-    const int page = min(max(bt[min(r0 >> A.pk.page_shift, A.pk.max_pages - 1)], 0), A.pk.num_pages - 1);
+    const int entry = bt[min(r0 >> A.pk.page_shift, A.pk.max_pages - 1)];
+    const int page = min(max(entry, 0), A.pk.num_pages - 1);
     const size_t prow = ((size_t)page << A.pk.page_shift) + (r0 & ((1 << A.pk.page_shift) - 1));
 #pragma unroll
     for (int j = 0; j < LD; ++j) {
@@ -714,12 +725,13 @@ __global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) 
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int d = 0; d < DPL; d += 4)
-      *(f32x4*)(out + (4 * g + r) * DPL + d) = f32x4{o[d][r], o[d + 1][r], o[d + 2][r], o[d + 3][r]} * inv;
+      *(f32x4*)(out + (4 * g + r) * DPL + d) =
+          f32x4{o[d][r], o[d + 1][r], o[d + 2][r], o[d + 3][r]} * inv;
 }
 
-// Adds the pieces of the tiles that were cut: a workgroup per (KV head, cut tile, 16 query rows),
-// a row per 16 threads.
-constexpr int kCombineThreads = 256, kCombineRows = 16;
+// Adds the pieces of the tiles that were cut: ROWS query rows of a (KV head, request that is cut) at a
+// time; 16 threads a row, and GROUPS of them share its pieces, kAhead of which load together.
+constexpr int kCombineThreads = 256, kAhead = 8;
 __device__ inline void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
 __device__ inline void store4(__bf16* p, const f32x4& x) {
   bf16x4 r;
@@ -727,63 +739,99 @@ __device__ inline void store4(__bf16* p, const f32x4& x) {
   for (int t = 0; t < 4; ++t) r[t] = (__bf16)x[t];
   *(bf16x4*)p = r;
 }
-template <typename T, int HD, int M>
+// weight of a part about the reference m (base 2) where the sum's is M
+__device__ inline float part_weight(float m, float M) {
+  return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+}
+template <typename T, int HD, int M, int ROWS, int GROUPS>
 __global__ __launch_bounds__(kCombineThreads) void chunk_combine_kernel(const ChunkArgs A) {
-  constexpr int TPR = kCombineThreads / kCombineRows, W = HD / TPR;   // dims per thread: 8 or 4
+  constexpr int W = HD / 64;   // 16-byte vectors per thread
+  static_assert(kCombineThreads == 16 * ROWS * GROUPS, "16 threads a row and group");
+  __shared__ f32x4 s_acc[GROUPS][ROWS][16][W];
+  __shared__ float2 s_ml[GROUPS][ROWS];
   const int G = A.Hq / A.Hkv, kvh = blockIdx.x % A.Hkv;
-  const Piece p = find_piece<M>(A, G, blockIdx.x / A.Hkv, true);
-  if (!p.found) return;
-  const int last = p.n * G - 1, row0 = p.tile * M;
-  const int r = blockIdx.y * kCombineRows + threadIdx.x / TPR, d = threadIdx.x % TPR * W;
-  if (row0 + r > last) return;
-  int lo, hi;
-  key_range(A, p, row0 / G, min(row0 + M - 1, last) / G, lo, hi);
-  const int units = (hi + kUnit - 1) / kUnit - lo / kUnit;
-  const int pieces = max(1, (int)(((int64_t)units + p.L - 1) / p.L));
-  auto at = [&](int s) {
-    return ((size_t)((int64_t)p.slot + (int64_t)s * p.tiles) * A.Hkv + kvh) * M + r;
-  };
-  if (((int64_t)p.slot + (int64_t)(pieces - 1) * p.tiles) * A.Hkv + kvh >= A.slots) return;
-  float Mx = -INFINITY, L = 0.f;
-  f32x4 acc[W / 4];
+  const int tr = threadIdx.x & 15, rr = (threadIdx.x >> 4) % ROWS;
+  const int grp = threadIdx.x / (16 * ROWS);
+  for (int item = blockIdx.x / A.Hkv;; item += gridDim.x / A.Hkv) {
+    const Piece p = find_piece<M, ROWS>(A, G, item);
+    if (!p.found) return;
+    const int last = p.n * G - 1, row0 = p.tile * M;
+    const int row = min(p.group * ROWS + rr, last);
+    int lo, hi;
+    key_range(A, p, row0 / G, min(row0 + M - 1, last) / G, lo, hi);
+    const int units = (hi + kUnit - 1) / kUnit - lo / kUnit;
+    const int pieces = max(1, (units + p.L - 1) / p.L);
+    // (never: the slots are bounded by the lengths themselves)
+    if (((int64_t)p.slot + (int64_t)(pieces - 1) * p.tiles) * A.Hkv + kvh >= A.slots) return;
+    float Mx = -INFINITY, L = 0.f;
+    f32x4 acc[W];
 #pragma unroll
-  for (int w = 0; w < W / 4; ++w) acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
-  constexpr int CH = 4;
-  for (int s0 = 0; s0 < pieces; s0 += CH) {
-    float2 ml[CH];
-    f32x4 x[CH][W / 4];
+    for (int w = 0; w < W; ++w) acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = grp; s0 < pieces; s0 += kAhead * GROUPS) {
+      float2 ml[kAhead];
+      f32x4 x[kAhead][W];
 #pragma unroll
-    for (int k = 0; k < CH; ++k) {
-      const size_t i = at(min(s0 + k, pieces - 1));
-      ml[k] = A.wsML[i];
+      for (int k = 0; k < kAhead; ++k) {
+        const int s = min(s0 + k * GROUPS, pieces - 1);
+        const size_t i =
+            ((size_t)((int64_t)p.slot + (int64_t)s * p.tiles) * A.Hkv + kvh) * M + (row - row0);
+        ml[k] = A.wsML[i];
 #pragma unroll
-      for (int w = 0; w < W / 4; ++w) x[k][w] = *(const f32x4*)(A.wsO + i * HD + d + 4 * w);
-    }
-    float Mc = Mx;
-#pragma unroll
-    for (int k = 0; k < CH; ++k) Mc = fmaxf(Mc, ml[k].x);
-    const float a = Mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(Mx - Mc);
-    L *= a;
-#pragma unroll
-    for (int w = 0; w < W / 4; ++w) acc[w] *= a;
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-      if (s0 + k >= pieces) continue;
-      if (ml[k].x != -INFINITY) {
-        const float e = __builtin_amdgcn_exp2f(ml[k].x - Mc);
-        L += e * ml[k].y;
-#pragma unroll
-        for (int w = 0; w < W / 4; ++w) acc[w] += e * x[k][w];
+        for (int w = 0; w < W; ++w) x[k][w] = *(const f32x4*)(A.wsO + i * HD + 64 * w + 4 * tr);
       }
-      if (ml[k].y != ml[k].y) L = ml[k].y;   // a NaN score moves no maximum
-    }
-    Mx = Mc;
-  }
-  const int tok = (row0 + r) / G, head = kvh * G + (row0 + r - tok * G);
-  T* const out = (T*)A.O + ((size_t)(p.q0 + tok) * A.Hq + head) * HD + d;
-  const float inv = L == 0.f ? 0.f : 1.f / L;
+      float Mc = Mx;
 #pragma unroll
-  for (int w = 0; w < W / 4; ++w) store4(out + 4 * w, acc[w] * inv);
+      for (int k = 0; k < kAhead; ++k) Mc = fmaxf(Mc, ml[k].x);
+      const float a = part_weight(Mx, Mc);
+      L *= a;
+#pragma unroll
+      for (int w = 0; w < W; ++w) acc[w] *= a;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (s0 + k * GROUPS >= pieces) continue;
+        if (ml[k].x != -INFINITY) {
+          const float e = part_weight(ml[k].x, Mc);
+          L += e * ml[k].y;
+#pragma unroll
+          for (int w = 0; w < W; ++w) acc[w] += e * x[k][w];
+        }
+        if (ml[k].y != ml[k].y) L = ml[k].y;   // a NaN score moves no maximum
+      }
+      Mx = Mc;
+    }
+    if (grp > 0) {
+#pragma unroll
+      for (int w = 0; w < W; ++w) s_acc[grp - 1][rr][tr][w] = acc[w];
+      if (tr == 0) s_ml[grp - 1][rr] = make_float2(Mx, L);
+    }
+    __syncthreads();
+    if (grp == 0 && p.group * ROWS + rr <= last) {
+      float Mc = Mx;
+#pragma unroll
+      for (int g = 0; g < GROUPS - 1; ++g) Mc = fmaxf(Mc, s_ml[g][rr].x);
+      const float a = part_weight(Mx, Mc);
+      L *= a;
+#pragma unroll
+      for (int w = 0; w < W; ++w) acc[w] *= a;
+#pragma unroll
+      for (int g = 0; g < GROUPS - 1; ++g) {
+        const float2 ml = s_ml[g][rr];
+        if (ml.x != -INFINITY) {
+          const float e = part_weight(ml.x, Mc);
+          L += e * ml.y;
+#pragma unroll
+          for (int w = 0; w < W; ++w) acc[w] += e * s_acc[g][rr][tr][w];
+        }
+        if (ml.y != ml.y) L = ml.y;
+      }
+      const int tok = row / G, head = kvh * G + (row - tok * G);
+      T* const out = (T*)A.O + ((size_t)(p.q0 + tok) * A.Hq + head) * HD + 4 * tr;
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+      for (int w = 0; w < W; ++w) store4(out + 64 * w, acc[w] * inv);
+    }
+    __syncthreads();   // the groups' parts are read before the next ones are written
+  }
 }
 
 template <typename T, int HD>
@@ -794,8 +842,9 @@ hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
   else chunk_f32_kernel<HD><<<grid, kThreads, 0, s>>>(A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 0) return e;
-  chunk_combine_kernel<T, HD, M>
-      <<<dim3((unsigned)(p.cut_tiles * A.Hkv), M / kCombineRows), kCombineThreads, 0, s>>>(A);
+  const unsigned cgrid = (unsigned)(p.cut_groups * A.Hkv);
+  if (p.cut_rows == 16) chunk_combine_kernel<T, HD, M, 16, 1><<<cgrid, kCombineThreads, 0, s>>>(A);
+  else chunk_combine_kernel<T, HD, M, 4, 4><<<cgrid, kCombineThreads, 0, s>>>(A);
   return hipGetLastError();
 }
 
@@ -811,14 +860,22 @@ ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int max_len, int dtyp
                                           (int64_t)rows * (Hq / Hkv));
   const bool may_cut = max_len > kMinUnits * kUnit;
   const int64_t cut = std::min<int64_t>(tiles, std::max(1, kTarget / Hkv));
-  p.cut_tiles = may_cut ? cut : 0;
+  // Their groups of rows in the second kernel, by their tiles and by all requests' rows; it takes
+  // more than about 1024 of them in turns.  Few rows have many pieces each, which four groups of
+  // threads share: us of 16 tokens (32/8 heads) over 32K, 31 pieces, with groups of 4 rows / 16
+  // 5.7 / 10.4; of 512 tokens over 8K, 4 pieces, 28 / 9.3.
+  p.cut_rows = (int64_t)rows * Hq <= 4096 ? 4 : 16;
+  const int64_t groups = std::min<int64_t>(cut * (M / p.cut_rows),
+                                           (int64_t)rows * (Hq / Hkv) / p.cut_rows + batch);
+  p.cut_groups = may_cut ? std::min<int64_t>(groups, std::max(1, 1024 / Hkv)) : 0;
   p.slots = may_cut ? (int64_t)Hkv * std::max(1, 2 * kTarget / Hkv) : 0;
   p.items = tiles + p.slots / Hkv;
   return p;
 }
 
 size_t chunk_ws_bytes(const ChunkPlan& p, int head_dim, int dtype) {
-  return (size_t)p.slots * (dtype == TAPS_BF16 ? kM : kMF) * (head_dim * sizeof(float) + sizeof(float2));
+  const size_t M = dtype == TAPS_BF16 ? kM : kMF;
+  return (size_t)p.slots * M * (head_dim * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const void* V,
@@ -835,9 +892,8 @@ hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const vo
   A.O = (unsigned char*)O;
   A.slots = (int)p.slots;
   A.wsO = p.slots ? (float*)ws : nullptr;
-  A.wsML = p.slots
-               ? (float2*)((float*)ws + (size_t)p.slots * (dtype == TAPS_BF16 ? kM : kMF) * head_dim)
-               : nullptr;
+  const size_t M = dtype == TAPS_BF16 ? kM : kMF;
+  A.wsML = p.slots ? (float2*)((float*)ws + (size_t)p.slots * M * head_dim) : nullptr;
   if (dtype == TAPS_BF16)
     return head_dim == 128 ? launch_t<__bf16, 128>(A, p, s) : launch_t<__bf16, 64>(A, p, s);
   return head_dim == 128 ? launch_t<float, 128>(A, p, s) : launch_t<float, 64>(A, p, s);

@@ -188,7 +188,8 @@ hipError_t launch_rope(const void* Q, const void* K, const void* V, int64_t q_st
 // Chunks of new tokens over a paged cache: query tiles, cut along the keys where few
 struct ChunkPlan {
   int64_t items;       // most pieces per KV head
-  int64_t cut_tiles;   // most query tiles per KV head that are cut (0: none ever is)
+  int64_t cut_groups;  // most groups of rows per KV head of requests that are cut (0: none ever is)
+  int cut_rows;        // rows of such a group: 16, or 4
   int64_t slots;       // most pieces of cut tiles, all KV heads
 };
 ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int max_len, int dtype);
