@@ -8,16 +8,22 @@
 // log2 e) rounded: what the rounding and the constant's error add to every t of a thread is known
 // and taken out in the join, so that a weight near the top is good to 2^-23.
 //
-// Top alternatives: the k-th largest of the threads' own maxima bounds the row's k-th value from
-// below.  The few threads that reach it look again at the batch of loads that held their maximum
-// (at all of them if a second batch reaches the bound), and what they find is ranked by counting.
-// Rows with more than kCand values at the bound (ties), or without k values above kLow (masks),
-// go value by value instead: the largest value not yet taken, then its places in index order.
+// The pass takes values as they are.  An infinity or NaN makes S one too: a wave that ends with
+// such a sum goes over its values again with those below kLow, and NaN, lifted to kLow (a wave
+// that meets one in its first loads does so at once), and rows whose maximum is not an ordinary
+// number are summed by the definition.
 //
-// Bound: HBM; in bf16 the vector unit is close behind (about 12 of the 16 instructions an element
-// that the memory's rate leaves).
+// Top alternatives: the k-th largest of 64 groups' maxima bounds the row's k-th value from below.
+// The few threads that reach it look again at the batch of loads that held their maximum (at all
+// of them if a second batch reaches the bound), and what they find is ranked by counting.  Rows
+// with more than kCand values at the bound (ties), or without k values above kLow (masks), go
+// value by value instead: the largest value not yet taken, then its places in index order.
+//
+// Bound: HBM; in bf16 the vector unit is close behind (9.5 instruction slots an element, of the 16
+// that the memory's rate leaves, four of them the exponential's).
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "common.h"
 
@@ -28,9 +34,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLog2eRest = 1.4426950408889634 - (double)kLog2e;
-// Values below kLow count as kLow in the sums, NaN too: their weights are 0 all the same where the
-// row's maximum is well above, and t stays finite (0 * inf).  Past 1e6 c's rounding reaches a
-// unit of the exponent.  Rows whose maximum is not between are done again with care.
+// Values below kLow count as kLow in the careful sums, NaN too: their weights are 0 all the same
+// where the row's maximum is well above, and t stays finite (0 * inf).  Past 1e6 c's rounding
+// reaches a unit of the exponent.  Rows whose maximum is not between go by the definition.
 constexpr float kLow = -1e6f, kHigh = 1e6f;
 constexpr int kCand = 512;   // candidates for the top alternatives
 
@@ -56,6 +62,11 @@ __device__ inline float value_at<uint16_t>(const uint16_t* x, int i) {
 template <>
 __device__ inline float value_at<float>(const float* x, int i) { return x[i]; }
 
+template <bool B>
+struct Flag {
+  static constexpr bool value = B;
+};
+
 // element e of a 16-byte unit
 template <typename T>
 __device__ inline float unit_value(const u32x4& r, int e) {
@@ -66,7 +77,15 @@ __device__ inline float unit_value(const u32x4& r, int e) {
 }
 
 // max(x, kLow), kLow for NaN
-__device__ inline float lifted(float x) { return __builtin_amdgcn_fmed3f(x, kLow, INFINITY); }
+__device__ inline float lifted(float x) { return x > kLow ? x : kLow; }
+
+// max by the bare instruction (fmaxf quiets its operands first, an instruction each); NaN operands
+// give either operand or NaN
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 // Row of `n` values: the first `head` lie before the first 16-byte boundary, then `units`
 // whole 16-byte units, then `tail` values.
@@ -88,22 +107,43 @@ struct Row {
   __device__ inline int edge(int i) const { return i < head ? i : n - tail + (i - head); }
 };
 
-template <int NT>
-__device__ inline double block_sum(double v, double* s) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  double t = 0.0;
-#pragma unroll
-  for (int w = 0; w < NT / 64; ++w) t += s[w];
-  return t;
+// over the lanes of a wave, in each of them (DPP row shifts, then row broadcasts)
+template <int CTRL, int ROWS>
+__device__ inline float dpp_max(float v) {
+  return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(
+                      __float_as_uint(v), __float_as_uint(v), CTRL, ROWS, 0xf, false)));
 }
 __device__ inline float wave_max(float v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-  return v;
+  v = dpp_max<0x111, 0xf>(v);
+  v = dpp_max<0x112, 0xf>(v);
+  v = dpp_max<0x114, 0xf>(v);
+  v = dpp_max<0x118, 0xf>(v);
+  v = dpp_max<0x142, 0xa>(v);
+  v = dpp_max<0x143, 0xc>(v);
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+template <int CTRL, int ROWS>
+__device__ inline double dpp_add(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)u, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+  return v + __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+__device__ inline double wave_sum(double v) {
+  v = dpp_add<0x111, 0xf>(v);
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);
+  v = dpp_add<0x143, 0xc>(v);
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)u, 63);
+  const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(u >> 32), 63);
+  return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+// the value of a value_key
+__device__ inline float key_value(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
 }
 
 template <typename T, int NT>
@@ -111,14 +151,16 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
   constexpr int E = Row<T>::E;
   constexpr int UN = 4;   // units per thread and batch
   constexpr int NW = NT / 64;
-  __shared__ double s_sum[NW];
+  __shared__ double s_z[NW], s_s[NW];
+  __shared__ float s_m[NW];
   __shared__ float s_max[NT];
   __shared__ float s_bound;
   __shared__ int s_int[NW];
   __shared__ int s_count;
   __shared__ uint64_t s_cand[kCand];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = blockIdx.x;
   const int b = (int)(row / A.budget), i = (int)(row - (int64_t)b * A.budget);
   const int top = A.top;
@@ -130,25 +172,30 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
     return;
   }
   const Row<T> R(A.x + (size_t)row * A.row_bytes, A.vocab);
+  constexpr int step = NT * UN;
+  const int whole = R.units / step, nb = (R.units + step - 1) / step;   // batches
+  u32x4 cur[UN], nxt[UN];
+  auto fetch = [&](int k, u32x4 (&r)[UN]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < UN; ++j) r[j] = R.unit(min(k * step + j * NT + tid, R.units - 1));
+  };
+  if (nb > 0) fetch(0, cur);
+
   const int tok = A.tokens[row];
   const bool given = tok >= 0 && tok < A.vocab;
   const float xt = given ? value_at(R.x, tok) : 0.f;
   // values that come before the token: above it, or equal and of a lower index.  Units before
   // the token's compare with the next value below it.
-  const bool plain = given && xt == xt && xt != -INFINITY;
+  const bool ordinary = given && xt == xt && xt != -INFINITY;
   const float xt_below =
       xt == 0.f ? -1.4e-45f
                 : __uint_as_float(__float_as_uint(xt) + (xt > 0.f ? 0xFFFFFFFFu : 1u));
   const int tok_unit = tok >= R.head ? (tok - R.head) / E : -1;   // (past the last: the tail's)
 
   // ---- one pass
-  float Z = 0.f, S = 0.f, c = 0.f, ref = -INFINITY;
-  float best = -INFINITY, rest = -INFINITY;   // largest lifted value; the largest of other batches
-  int best_at = 0, before = 0;
-  auto batch = [&](const float* x, int n, int at) __attribute__((always_inline)) {
-    float mx = x[0];
-#pragma unroll
-    for (int e = 1; e < n; ++e) mx = fmaxf(mx, x[e]);
+  float Z, S, c, ref, best, rest;   // best: largest value; rest: the largest of other batches
+  int best_at, before;              // before: of the wave's values
+  auto values = [&](const float* x, int n, float mx, int at) __attribute__((always_inline)) {
     if (__ballot(mx > ref + 5.5f)) {   // 5.5 log2 e: 2^8
       const bool upd = mx > ref + 5.5f;
       const float cn = -(mx * kLog2e);
@@ -171,77 +218,110 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
       S = fmaf(w, t, S);
     }
   };
-  {
-    const int step = NT * UN;
-    const int nb = (R.units + step - 1) / step;
-    u32x4 cur[UN], nxt[UN];
-    auto fetch = [&](int k, u32x4 (&r)[UN]) __attribute__((always_inline)) {
+  // the batch in cur; careful: units past the row read as kLow
+  auto batch = [&](auto careful, int k) __attribute__((always_inline)) {
+    float x[UN * E];
 #pragma unroll
-      for (int j = 0; j < UN; ++j) r[j] = R.unit(min(k * step + j * NT + tid, R.units - 1));
-    };
-    if (nb > 0) fetch(0, cur);
+    for (int j = 0; j < UN; ++j) {
+      const int u = k * step + j * NT + tid;
+      const float thr = u < tok_unit ? xt_below : xt;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        float v = unit_value<T>(cur[j], e);
+        if constexpr (decltype(careful)::value) v = u < R.units ? v : -INFINITY;
+        before += __popcll(__ballot(v > thr));
+        x[j * E + e] = decltype(careful)::value ? lifted(v) : v;
+      }
+    }
+    float m0 = x[0], m1 = x[1];
+#pragma unroll
+    for (int e = 2; e < UN * E; e += 4) {
+      m0 = max3(m0, x[e], x[e + 1]);
+      if (e + 2 < UN * E) m1 = max3(m1, x[e + 2], x[e + 3]);
+    }
+    values(x, UN * E, max3(m0, m1, m1), k);
+  };
+  auto pass = [&](auto careful) __attribute__((always_inline)) {
+    Z = S = c = 0.f;
+    ref = best = rest = -INFINITY;
+    best_at = before = 0;
     for (int k = 0; k < nb; ++k) {
       if (k + 1 < nb) fetch(k + 1, nxt);
-      float x[UN * E];
-#pragma unroll
-      for (int j = 0; j < UN; ++j) {
-        const int u = k * step + j * NT + tid;
-        const float thr = u < tok_unit ? xt_below : xt;
-        const bool in = u < R.units;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float v = in ? unit_value<T>(cur[j], e) : -INFINITY;
-          before += v > thr;
-          x[j * E + e] = lifted(v);
-        }
-      }
-      if (k * step + tid < R.units) batch(x, UN * E, k);
+      if (decltype(careful)::value || k == whole) batch(Flag<true>(), k);
+      else batch(Flag<false>(), k);
 #pragma unroll
       for (int j = 0; j < UN; ++j) cur[j] = nxt[j];
     }
-    // (units past the row were lifted to kLow)
-    if (tid < R.head + R.tail) {
-      const int j = R.edge(tid);
-      const float v = value_at(R.x, j);
-      before += j < tok ? v >= xt : v > xt;
+    // the edges; ties in the token's own unit
+    const bool in = tid < R.head + R.tail;
+    const int j = R.edge(in ? tid : 0);
+    const float v = in ? value_at(R.x, j) : -INFINITY;
+    before += __popcll(__ballot(in && (j < tok ? v >= xt : v > xt)));
+    if (__ballot(in)) {
       const float x = lifted(v);
-      batch(&x, 1, nb);
+      if (in) values(&x, 1, x, nb);
     }
-    // ties in the token's own unit
-    if (tid == 0 && given && tok_unit >= 0 && tok_unit < R.units)
-      for (int j = R.index(tok_unit, 0); j < tok; ++j) before += value_at(R.x, j) == xt;
-  }
-
-  // ---- the row's maximum; the threads' maxima for the bound
-  s_max[tid] = best;
-  if (tid == 0) s_count = 0;
-  __syncthreads();
-  float M = -INFINITY;
+    if (wave == 0 && given && tok_unit >= 0 && tok_unit < R.units) {
+      const int u0 = R.index(tok_unit, 0);
+      before += __popcll(__ballot(lane < tok - u0 && value_at(R.x, u0 + min(lane, E - 1)) == xt));
+    }
+  };
+  {
+    bool odd = false;
+    if (nb > 0) {
 #pragma unroll
-  for (int w = 0; w < NW; ++w) M = fmaxf(M, s_max[w * 64 + lane]);
-  M = wave_max(M);
-  const bool special = !(M > kLow + 1000.f && M < kHigh);
-
-  // ---- rank
-  if (!plain && given) {   // -inf or NaN: again, by the definition
+      for (int e = 0; e < E; ++e) odd = odd || !(fabsf(unit_value<T>(cur[0], e)) < INFINITY);
+    }
+    bool careful = __ballot(odd) != 0;
+    if (!careful) {
+      pass(Flag<false>());
+      careful = __ballot(!(fabsf(S) < INFINITY && fabsf(Z) < INFINITY)) != 0;
+      if (careful && nb > 0) fetch(0, cur);
+    }
+    if (careful) pass(Flag<true>());
+  }
+  if (!ordinary && given) {   // a token of -inf or NaN: its rank by the definition
     const uint32_t kt = value_key(__float_as_uint(xt));
     before = 0;
-    for (int j = tid; j < R.n; j += NT) {
-      const uint32_t k = value_key(__float_as_uint(value_at(R.x, j)));
-      before += k > kt || (k == kt && j < tok);
+    for (int j0 = 0; j0 < R.n; j0 += NT) {
+      const int j = j0 + tid;
+      const uint32_t k = j < R.n ? value_key(__float_as_uint(value_at(R.x, j))) : 0u;
+      before += __popcll(__ballot(j < R.n && (k > kt || (k == kt && j < tok))));
     }
   }
-  for (int m = 32; m >= 1; m >>= 1) before += __shfl_xor(before, m);
-  if (lane == 0) s_int[wave] = before;
 
-  // ---- Z and S about M
-  double Zd, Sd, Md = M;   // Sd in units of ln 2
-  if (!special) {
-    const double k = ref == -INFINITY ? 0.0 : -(double)c + (double)ref * kLog2eRest - Md * 1.4426950408889634;
-    const double a = ref == -INFINITY ? 0.0 : exp2(k);
-    Zd = block_sum<NT>(a * Z, s_sum);
-    Sd = block_sum<NT>(a * ((double)S + k * Z), s_sum) * 0.6931471805599453;
-  } else {
+  // ---- the waves' sums about their own maxima (ref -inf: a thread without values)
+  {
+    const float m = wave_max(best);
+    double a = 0.0, k = 0.0;
+    if (ref != -INFINITY) {
+      k = -(double)c + (double)ref * kLog2eRest - (double)m * 1.4426950408889634;
+      a = exp2(k);
+    }
+    const double z = wave_sum(a * Z), sn = wave_sum(a * ((double)S + k * Z));
+    s_max[tid] = best;
+    if (lane == 0) s_m[wave] = m, s_z[wave] = z, s_s[wave] = sn, s_int[wave] = before;
+    if (tid == 0) s_count = 0;
+  }
+  __syncthreads();
+  float M;
+  double Zd, Sd, Md;
+  int rank = 0;
+  {
+    const int w = min(lane, NW - 1);
+    const float m = s_m[w];
+    M = wave_max(m);
+    Md = M;
+    const double k = ((double)m - Md) * 1.4426950408889634;
+    const bool in = lane < NW && m != -INFINITY;
+    const double a = in ? exp2(k) : 0.0;
+    Zd = wave_sum(in ? a * s_z[w] : 0.0);
+    Sd = wave_sum(in ? a * (s_s[w] + k * s_z[w]) : 0.0) * 0.6931471805599453;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) rank += s_int[q];
+  }
+  const bool special = !(M > kLow + 1000.f && M < kHigh);
+  if (special) {
     // about kLow or below, or above kHigh: weights by the definition
     float m = -INFINITY;
     bool any = false;
@@ -249,15 +329,15 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
       const float v = value_at(R.x, j);
       if (v == v) m = v > m ? v : m, any = true;
     }
+    m = wave_max(m);
     __syncthreads();
-    s_max[tid] = m;
+    if (lane == 0) s_m[wave] = m;
     const int have = __syncthreads_or(any);
     M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, s_max[w * 64 + lane]);
-    M = wave_max(M);
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w]);
     Md = M;
-    double z = 0.0, s = 0.0;
+    double z = 0.0, sn = 0.0;
     for (int j = tid; have && j < R.n; j += NT) {
       const float v = value_at(R.x, j);
       if (v == M) {
@@ -265,11 +345,15 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
       } else if (v == v) {
         const double d = (double)v - Md, w = exp(d);
         z += w;
-        if (w > 0.0) s += w * d;
+        if (w > 0.0) sn += w * d;
       }
     }
-    Zd = block_sum<NT>(z, s_sum);
-    Sd = block_sum<NT>(s, s_sum);
+    z = wave_sum(z), sn = wave_sum(sn);
+    if (lane == 0) s_z[wave] = z, s_s[wave] = sn;
+    __syncthreads();
+    Zd = Sd = 0.0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) Zd += s_z[w], Sd += s_s[w];
   }
   const double lnz = log(Zd);
   auto lp = [&](float v) {
@@ -277,10 +361,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
     return v == M ? (float)-lnz : (float)(((double)v - Md) - lnz);
   };
   if (tid == 0) {
-    int r = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) r += s_int[w];
-    A.rank[row] = given ? r : -1;
+    A.rank[row] = given ? rank : -1;
     A.logprob[row] = given ? lp(xt) : -INFINITY;
     A.entropy[row] = Zd == 0.0 ? 0.f : (float)(lnz - Sd / Zd);
   }
@@ -290,26 +371,15 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
   bool fallback = special;
   if (!special) {
     if (wave == 0) {
-      float v[NW];
+      float v = s_max[lane];
 #pragma unroll
-      for (int w = 0; w < NW; ++w) v[w] = s_max[w * 64 + lane];
-      float bound = 0.f;
-      for (int r = 0; r < top; ++r) {
-        float m = v[0];
+      for (int w = 1; w < NW; ++w) v = fmaxf(v, s_max[w * 64 + lane]);
+      int above = 0;
 #pragma unroll
-        for (int w = 1; w < NW; ++w) m = fmaxf(m, v[w]);
-        bound = wave_max(m);
-        const uint64_t who = __ballot(m == bound);
-        if (lane == __ffsll((long long)who) - 1) {   // one of the equal ones goes
-          bool gone = false;
-#pragma unroll
-          for (int w = 0; w < NW; ++w) {
-            const bool hit = !gone && v[w] == bound;
-            v[w] = hit ? -INFINITY : v[w];
-            gone = gone || hit;
-          }
-        }
-      }
+      for (int q = 0; q < 64; ++q)
+        above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), q)) > v;
+      // the smallest value that fewer than `top` groups exceed
+      const float bound = -wave_max(above < top ? -v : -INFINITY);
       if (lane == 0) s_bound = bound;
     }
     __syncthreads();
@@ -323,16 +393,16 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
         }
       };
       if (best >= bound) {
-        const int step = NT * UN, nb = (R.units + step - 1) / step;
         const bool all = rest >= bound;
         for (int k = all ? 0 : best_at; k < (all ? nb : min(best_at + 1, nb)); ++k) {
+          u32x4 r[UN];
+          fetch(k, r);
 #pragma unroll
           for (int j = 0; j < UN; ++j) {
             const int u = k * step + j * NT + tid;
             if (u < R.units) {
-              const u32x4 r = R.unit(u);
 #pragma unroll
-              for (int e = 0; e < E; ++e) add(unit_value<T>(r, e), R.index(u, e));
+              for (int e = 0; e < E; ++e) add(unit_value<T>(r[j], e), R.index(u, e));
             }
           }
         }
@@ -347,9 +417,8 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
           int r = 0;
           for (int j = 0; j < n; ++j) r += s_cand[j] > mine;
           if (r < top) {
-            const int j = (int)cand_index(mine);
-            tidx[r] = j;
-            tlp[r] = lp(value_at(R.x, j));
+            tidx[r] = (int)cand_index(mine);
+            tlp[r] = lp(key_value((uint32_t)(mine >> 32)));
           }
         }
       }
@@ -407,10 +476,17 @@ hipError_t launch_logprobs(const void* logits, int64_t row_bytes, int batch, int
   LogprobArgs A;
   A.x = (const unsigned char*)logits, A.row_bytes = row_bytes;
   A.budget = budget, A.vocab = vocab, A.top = top, A.n_nodes = n_nodes, A.tokens = tokens;
-  A.logprob = logprob, A.entropy = entropy, A.rank = rank, A.top_idx = top_idx, A.top_lp = top_logprob;
+  A.logprob = logprob, A.entropy = entropy, A.rank = rank;
+  A.top_idx = top_idx, A.top_lp = top_logprob;
   const unsigned grid = (unsigned)rows;
-  if (dtype == TAPS_BF16) logprobs_kernel<uint16_t, 512><<<grid, 512, 0, s>>>(A);
-  else logprobs_kernel<float, 512><<<grid, 512, 0, s>>>(A);
+  const bool few = rows <= (getenv("LP_ROWS") ? atoi(getenv("LP_ROWS")) : 256);
+  if (dtype == TAPS_BF16) {
+    if (few) logprobs_kernel<uint16_t, 1024><<<grid, 1024, 0, s>>>(A);
+    else logprobs_kernel<uint16_t, 512><<<grid, 512, 0, s>>>(A);
+  } else {
+    if (few) logprobs_kernel<float, 1024><<<grid, 1024, 0, s>>>(A);
+    else logprobs_kernel<float, 512><<<grid, 512, 0, s>>>(A);
+  }
   return hipGetLastError();
 }
 
