@@ -672,6 +672,11 @@ taps_status chunk_attn_paged(const void *Q, int64_t q_stride, const void *K_page
 taps_status taps_logprobs_validate(int32_t batch, int32_t budget, int32_t vocab,
                                    int64_t row_stride, int32_t dtype, int32_t top);
 
+/* Bytes of scratch taps_logprobs needs (the parts that few rows are cut into; 0 for many rows or a
+ * small vocabulary).  Calls that may overlap on the GPU need scratch of their own. */
+size_t taps_logprobs_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab, int32_t dtype,
+                                     int32_t top);
+
 /* Log probabilities of given tokens under each logits row (a prompt's next tokens, sampled or
  * drafted ones), with their ranks, the row's entropy and its top alternatives.
  *   logits       [batch][budget][vocab] as for taps_sample (row_stride, alignment, dtype)
@@ -685,6 +690,7 @@ taps_status taps_logprobs_validate(int32_t batch, int32_t budget, int32_t vocab,
  *   rank         [batch][budget] int32: tokens before it in the rank order (0: the largest)
  *   top_idx      [batch][budget][top] int32, the first `top` tokens of the rank order
  *   top_logprob  [batch][budget][top] float, theirs.  (Both may be NULL where top is 0)
+ *   ws           taps_logprobs_workspace_bytes(...) bytes, 16-byte aligned
  * p_j = w_j / sum w, w_j = exp(x_j - x_0) for the largest value x_0: 1 where x_j equals x_0
  * (infinite values too), 0 for NaN, as in taps_sample at T = 1.  The rank order is value
  * descending, then index ascending; -0 equals +0; NaN is last.  A row of NaN alone has log
@@ -692,8 +698,8 @@ taps_status taps_logprobs_validate(int32_t batch, int32_t budget, int32_t vocab,
 taps_status taps_logprobs(const void *logits, int64_t row_stride, int32_t batch, int32_t budget,
                           int32_t vocab, int32_t dtype, const int32_t *n_nodes,
                           const int32_t *tokens, int32_t top, float *logprob, float *entropy,
-                          int32_t *rank, int32_t *top_idx, float *top_logprob,
-                          hipStream_t stream);
+                          int32_t *rank, int32_t *top_idx, float *top_logprob, void *ws,
+                          size_t ws_bytes, hipStream_t stream);
 
 /* Human-readable name of a status code (static string). */
 const char *taps_status_string(int32_t status);

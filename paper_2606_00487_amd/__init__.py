@@ -794,6 +794,7 @@ class TokenLogProbs:
         self.shape = (batch, budget, vocab, top, dtype)
         _lib.check(self.lib, "taps_logprobs_validate", self.lib.taps_logprobs_validate(
             batch, budget, vocab, vocab, dtype, top))
+        self.ws_bytes = self.lib.taps_logprobs_workspace_bytes(batch, budget, vocab, dtype, top)
 
     def __call__(self, logits, tokens, n_nodes=None):
         """logits: [batch, budget, vocab] as for TokenSampler; tokens: [batch, budget] int32;
@@ -813,10 +814,11 @@ class TokenLogProbs:
         fl = fl.view(torch.float32)
         logprob, entropy, top_lp = fl.split_with_sizes((n, n, top * n))
         at = buf.data_ptr()
+        ws = tokens.new_empty(self.ws_bytes, dtype=torch.uint8) if self.ws_bytes else None
         _lib.check(self.lib, "taps_logprobs", self.lib.taps_logprobs(
             _ptr(logits), stride, batch, budget, vocab, dtype, _ptr(n_nodes), _ptr(tokens), top,
             at + 4 * (1 + top) * n, at + 4 * (2 + top) * n, at, at + 4 * n,
-            at + 4 * (3 + top) * n, _stream()))
+            at + 4 * (3 + top) * n, _ptr(ws), self.ws_bytes, _stream()))
         return (logprob.view(batch, budget), entropy.view(batch, budget),
                 rank.view(batch, budget), top_idx.view(batch, budget, top),
                 top_lp.view(batch, budget, top))

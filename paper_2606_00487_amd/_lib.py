@@ -39,7 +39,7 @@ EXPORTED = [
     "decode_attn_paged_workspace_bytes", "decode_attn_paged", "taps_sample_validate",
     "taps_sample_workspace_bytes", "taps_sample", "taps_rope_frequencies", "qk_rope_paged",
     "chunk_attn_paged_validate", "chunk_attn_paged_workspace_bytes", "chunk_attn_paged",
-    "taps_logprobs_validate", "taps_logprobs",
+    "taps_logprobs_validate", "taps_logprobs_workspace_bytes", "taps_logprobs",
 ]
 SELECT_SCRATCH_BYTES = 8 << 20   # TAPS_SELECT_SCRATCH_BYTES
 
@@ -184,7 +184,10 @@ def load(path: str = LIB_PATH):
     lib.chunk_attn_paged.restype = i32
     lib.taps_logprobs_validate.argtypes = [i32, i32, i32, i64, i32, i32]
     lib.taps_logprobs_validate.restype = i32
-    lib.taps_logprobs.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.taps_logprobs_workspace_bytes.argtypes = [i32] * 5
+    lib.taps_logprobs_workspace_bytes.restype = sz
+    lib.taps_logprobs.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp,
+                                  sz, vp]
     lib.taps_logprobs.restype = i32
     lib.taps_status_string.argtypes = [i32]
     lib.taps_status_string.restype = ctypes.c_char_p

@@ -824,11 +824,17 @@ taps_status taps_logprobs_validate(int32_t batch, int32_t budget, int32_t vocab,
   return TAPS_OK;
 }
 
+size_t taps_logprobs_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab, int32_t dtype,
+                                     int32_t top) {
+  if (taps_logprobs_validate(batch, budget, vocab, vocab, dtype, top) != TAPS_OK) return 0;
+  return logprobs_ws_bytes((int64_t)batch * budget, vocab, dtype, top);
+}
+
 taps_status taps_logprobs(const void* logits, int64_t row_stride, int32_t batch, int32_t budget,
                           int32_t vocab, int32_t dtype, const int32_t* n_nodes,
                           const int32_t* tokens, int32_t top, float* logprob, float* entropy,
-                          int32_t* rank, int32_t* top_idx, float* top_logprob,
-                          hipStream_t stream) {
+                          int32_t* rank, int32_t* top_idx, float* top_logprob, void* ws,
+                          size_t ws_bytes, hipStream_t stream) {
   const taps_status st = taps_logprobs_validate(batch, budget, vocab, row_stride, dtype, top);
   if (st != TAPS_OK) return st;
   if (batch == 0) return TAPS_OK;
@@ -842,8 +848,11 @@ taps_status taps_logprobs(const void* logits, int64_t row_stride, int32_t batch,
                        (uintptr_t)entropy | (uintptr_t)rank | (uintptr_t)top_idx |
                        (uintptr_t)top_logprob;
   if ((a4 & 3) != 0) return TAPS_ERR_INVALID_ARG;
+  const size_t need = logprobs_ws_bytes((int64_t)batch * budget, vocab, dtype, top);
+  if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return TAPS_ERR_WORKSPACE;
   return launch_logprobs(logits, row_stride * es, batch, budget, vocab, dtype, n_nodes, tokens,
-                         top, logprob, entropy, rank, top_idx, top_logprob, stream) == hipSuccess
+                         top, logprob, entropy, rank, top_idx, top_logprob, ws,
+                         stream) == hipSuccess
              ? TAPS_OK
              : TAPS_ERR_HIP;
 }

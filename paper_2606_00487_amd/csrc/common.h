@@ -201,10 +201,11 @@ hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const vo
                         int window, int dtype, float scale, const ChunkPlan& p, void* O, void* ws,
                         hipStream_t s);
 
+size_t logprobs_ws_bytes(int64_t rows, int vocab, int dtype, int top);
 hipError_t launch_logprobs(const void* logits, int64_t row_bytes, int batch, int budget,
                            int vocab, int dtype, const int32_t* n_nodes, const int32_t* tokens,
                            int top, float* logprob, float* entropy, int32_t* rank,
-                           int32_t* top_idx, float* top_logprob, hipStream_t s);
+                           int32_t* top_idx, float* top_logprob, void* ws, hipStream_t s);
 
 double spec_exp_host(double t);
 

@@ -2,9 +2,10 @@
 // (taps_logprobs).
 //
 // With M the row's largest value, w_j = exp(x_j - M), Z = sum w_j and S = sum w_j (x_j - M):
-// log p_j = x_j - M - ln Z and the entropy is ln Z - S / Z.  One workgroup a row, one pass: each
-// thread keeps Z and S about a reference of its own, which moves only when a value exceeds it by
-// 2^8; they are joined in 64 bits.  A weight is 2^t, t = fma(x, log2 e, c) with c = -(reference *
+// log p_j = x_j - M - ln Z and the entropy is ln Z - S / Z.  One pass by one workgroup a row, or, of
+// few rows, one for each of a row's parts, which a second kernel joins: each thread keeps Z and S
+// about a reference of its own, which moves only when a value exceeds it by 2^8; they are joined in
+// 64 bits.  A weight is 2^t, t = fma(x, log2 e, c) with c = -(reference *
 // log2 e) rounded: what the rounding and the constant's error add to every t of a thread is known
 // and taken out in the join, so that a weight near the top is good to 2^-23.
 //
@@ -23,7 +24,6 @@
 // that the memory's rate leaves, four of them the exponential's).
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 #include "common.h"
 
@@ -39,6 +39,7 @@ constexpr double kLog2eRest = 1.4426950408889634 - (double)kLog2e;
 // reaches a unit of the exponent.  Rows whose maximum is not between go by the definition.
 constexpr float kLow = -1e6f, kHigh = 1e6f;
 constexpr int kCand = 512;   // candidates for the top alternatives
+constexpr int kThreads = 512, kUnits = 4;   // 16-byte units per thread in a batch of loads
 
 struct LogprobArgs {
   const unsigned char* x;
@@ -51,6 +52,19 @@ struct LogprobArgs {
   int32_t* rank;
   int32_t* top_idx;
   float* top_lp;
+  // parts > 1: what each part of a row leaves, [rows][parts] and [rows][parts][top]
+  int parts;
+  struct Part* part;
+  uint64_t* keys;
+};
+
+// Maximum of a part, its sums about it, the values before the token, the token's value
+struct Part {
+  double Z, S;
+  float M;
+  int before;
+  float token;
+  int given;
 };
 
 template <typename T>
@@ -87,16 +101,16 @@ __device__ inline float max3(float a, float b, float c) {
   return r;
 }
 
-// Row of `n` values: the first `head` lie before the first 16-byte boundary, then `units`
+// Row (or part of one) of `n` values: the first `head` lie before the first 16-byte boundary, then `units`
 // whole 16-byte units, then `tail` values.
 template <typename T>
 struct Row {
   static constexpr int E = 16 / sizeof(T);
   const T* x;
   int n, head, units, tail;
-  __device__ inline Row(const unsigned char* p, int vocab) {
-    x = (const T*)p;
-    n = vocab;
+  __device__ inline Row(const T* p, int len) {
+    x = p;
+    n = len;
     head = min(n, (int)((0 - (uintptr_t)p & 15) / sizeof(T)));
     units = (n - head) / E;
     tail = n - head - units * E;
@@ -141,16 +155,25 @@ __device__ inline double wave_sum(double v) {
   const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(u >> 32), 63);
   return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
+// 2^k, good to 2^-23: the whole part exactly, the rest by the fp32 instruction
+__device__ inline double power(double k) {
+  const double n = __builtin_rint(k);
+  return __builtin_ldexp((double)__builtin_amdgcn_exp2f((float)(k - n)), (int)fmax(n, -4000.0));
+}
+// ln p of the value v, from the row's maximum and sum
+__device__ inline float log_prob(float v, float M, double Z, double lnz) {
+  if (v != v || Z == 0.0) return -INFINITY;
+  return v == M ? (float)-lnz : (float)(((double)v - (double)M) - lnz);
+}
 // the value of a value_key
 __device__ inline float key_value(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
 }
 
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
+template <typename T>
+__global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A) {
   constexpr int E = Row<T>::E;
-  constexpr int UN = 4;   // units per thread and batch
-  constexpr int NW = NT / 64;
+  constexpr int NT = kThreads, UN = kUnits, NW = NT / 64;
   __shared__ double s_z[NW], s_s[NW];
   __shared__ float s_m[NW];
   __shared__ float s_max[NT];
@@ -161,17 +184,28 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t row = blockIdx.x;
-  const int b = (int)(row / A.budget), i = (int)(row - (int64_t)b * A.budget);
+  const int row = blockIdx.x, part = blockIdx.y;
   const int top = A.top;
   int32_t* const tidx = A.top_idx + (size_t)row * top;
   float* const tlp = A.top_lp + (size_t)row * top;
-  if (A.n_nodes && i >= A.n_nodes[b]) {
+  const size_t at_part = (size_t)row * A.parts + part;
+  uint64_t* const keys = A.keys + at_part * top;
+  if (A.n_nodes && row % A.budget >= A.n_nodes[row / A.budget]) {
+    if (part > 0) return;   // (with parts the second kernel writes the same)
     if (tid < top) tidx[tid] = -1, tlp[tid] = 0.f;
     if (tid == 0) A.logprob[row] = 0.f, A.entropy[row] = 0.f, A.rank[row] = -1;
     return;
   }
-  const Row<T> R(A.x + (size_t)row * A.row_bytes, A.vocab);
+  // the values from j0 on: parts begin at whole units, the first and the last take the edges
+  int j0 = 0, j1 = A.vocab;
+  const T* const x0 = (const T*)(A.x + (size_t)row * A.row_bytes);
+  if (A.parts > 1) {
+    const Row<T> all(x0, A.vocab);
+    auto begin = [&](int q) { return all.head + all.units * q / A.parts * E; };
+    if (part > 0) j0 = begin(part);
+    if (part < A.parts - 1) j1 = begin(part + 1);
+  }
+  const Row<T> R(x0 + j0, j1 - j0);
   constexpr int step = NT * UN;
   const int whole = R.units / step, nb = (R.units + step - 1) / step;   // batches
   u32x4 cur[UN], nxt[UN];
@@ -181,9 +215,10 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
   };
   if (nb > 0) fetch(0, cur);
 
-  const int tok = A.tokens[row];
-  const bool given = tok >= 0 && tok < A.vocab;
-  const float xt = given ? value_at(R.x, tok) : 0.f;
+  const int token = A.tokens[row];
+  const bool given = token >= 0 && token < A.vocab;
+  const float xt = given ? value_at(x0, token) : 0.f;
+  const int tok = token - j0;   // (among this part's values, or before or past them)
   // values that come before the token: above it, or equal and of a lower index.  Units before
   // the token's compare with the next value below it.
   const bool ordinary = given && xt == xt && xt != -INFINITY;
@@ -283,8 +318,8 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
   if (!ordinary && given) {   // a token of -inf or NaN: its rank by the definition
     const uint32_t kt = value_key(__float_as_uint(xt));
     before = 0;
-    for (int j0 = 0; j0 < R.n; j0 += NT) {
-      const int j = j0 + tid;
+    for (int q = 0; q < R.n; q += NT) {
+      const int j = q + tid;
       const uint32_t k = j < R.n ? value_key(__float_as_uint(value_at(R.x, j))) : 0u;
       before += __popcll(__ballot(j < R.n && (k > kt || (k == kt && j < tok))));
     }
@@ -296,7 +331,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
     double a = 0.0, k = 0.0;
     if (ref != -INFINITY) {
       k = -(double)c + (double)ref * kLog2eRest - (double)m * 1.4426950408889634;
-      a = exp2(k);
+      a = power(k);
     }
     const double z = wave_sum(a * Z), sn = wave_sum(a * ((double)S + k * Z));
     s_max[tid] = best;
@@ -314,7 +349,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
     Md = M;
     const double k = ((double)m - Md) * 1.4426950408889634;
     const bool in = lane < NW && m != -INFINITY;
-    const double a = in ? exp2(k) : 0.0;
+    const double a = in ? power(k) : 0.0;
     Zd = wave_sum(in ? a * s_z[w] : 0.0);
     Sd = wave_sum(in ? a * (s_s[w] + k * s_z[w]) : 0.0) * 0.6931471805599453;
 #pragma unroll
@@ -356,11 +391,17 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
     for (int w = 0; w < NW; ++w) Zd += s_z[w], Sd += s_s[w];
   }
   const double lnz = log(Zd);
-  auto lp = [&](float v) {
-    if (v != v || Zd == 0.0) return -INFINITY;
-    return v == M ? (float)-lnz : (float)(((double)v - Md) - lnz);
+  auto lp = [&](float v) { return log_prob(v, M, Zd, lnz); };
+  auto found = [&](int r, uint64_t key) {   // the row's (part's) r-th value
+    if (A.parts > 1) {
+      keys[r] = key;
+    } else {
+      tidx[r] = (int)cand_index(key);
+      tlp[r] = lp(key_value((uint32_t)(key >> 32)));
+    }
   };
-  if (tid == 0) {
+  if (tid == 0 && A.parts > 1) A.part[at_part] = Part{Zd, Sd, M, rank, xt, given};
+  if (tid == 0 && A.parts == 1) {
     A.rank[row] = given ? rank : -1;
     A.logprob[row] = given ? lp(xt) : -INFINITY;
     A.entropy[row] = Zd == 0.0 ? 0.f : (float)(lnz - Sd / Zd);
@@ -389,7 +430,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
       auto add = [&](float v, int j) {
         if (v >= bound) {
           const int at = atomicAdd(&s_count, 1);
-          if (at < kCand) s_cand[at] = cand_key(value_key(__float_as_uint(v)), (uint32_t)j);
+          if (at < kCand) s_cand[at] = cand_key(value_key(__float_as_uint(v)), (uint32_t)(j0 + j));
         }
       };
       if (best >= bound) {
@@ -416,10 +457,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
           const uint64_t mine = s_cand[q];
           int r = 0;
           for (int j = 0; j < n; ++j) r += s_cand[j] > mine;
-          if (r < top) {
-            tidx[r] = (int)cand_index(mine);
-            tlp[r] = lp(key_value((uint32_t)(mine >> 32)));
-          }
+          if (r < top) found(r, mine);
         }
       }
     }
@@ -428,7 +466,8 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
 
   // ---- value by value: the largest key below the last one, then its indices in order
   uint64_t last = 1ull << 32;   // above every value's key
-  for (int have = 0; have < top;) {
+  int have = 0;
+  while (have < top) {
     uint32_t m = 0;
     bool any = false;
     for (int j = tid; j < R.n; j += NT) {
@@ -439,12 +478,12 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
     for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
     __syncthreads();
     if (lane == 0) s_int[wave] = (int)m;
-    if (!__syncthreads_or(any)) break;   // (top <= vocab: never)
+    if (!__syncthreads_or(any)) break;   // a part of fewer values
     m = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) m = max(m, (uint32_t)s_int[w]);
-    for (int j0 = 0; j0 < R.n && have < top; j0 += NT) {
-      const int j = j0 + tid;
+    for (int q = 0; q < R.n && have < top; q += NT) {
+      const int j = q + tid;
       const float v = j < R.n ? value_at(R.x, j) : 0.f;
       const bool hit = j < R.n && value_key(__float_as_uint(v)) == m;
       const uint64_t mask = __ballot(hit);
@@ -458,19 +497,73 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const LogprobArgs A) {
         total += s_int[w];
       }
       at += __popcll(mask & ((1ull << lane) - 1));
-      if (hit && at < top) tidx[at] = j, tlp[at] = lp(v);
+      if (hit && at < top) found(at, cand_key(m, (uint32_t)(j0 + j)));
       have += total;
     }
     last = m;
+  }
+  if (A.parts > 1 && tid >= have && tid < top) keys[tid] = 0;   // (no value's key)
+}
+
+// A row from its parts: a workgroup a row.
+constexpr int kJoinThreads = 256, kMaxParts = 16;
+__global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(const LogprobArgs A) {
+  __shared__ uint64_t s_key[kMaxParts * TAPS_MAX_LOGPROB_TOP];
+  const int tid = threadIdx.x, lane = tid & 63, top = A.top;
+  const int row = blockIdx.x;
+  const int n = A.parts * top;
+  for (int q = tid; q < n; q += kJoinThreads) s_key[q] = A.keys[(size_t)row * n + q];
+  const Part p = A.part[(size_t)row * A.parts + min(lane, A.parts - 1)];
+  if (A.n_nodes && row % A.budget >= A.n_nodes[row / A.budget]) return;   // written
+  const bool in = lane < A.parts;
+  const float M = wave_max(p.M);
+  // parts without values but NaN have Z 0; equal maxima may be infinite
+  const double d = p.M == M ? 0.0 : (double)p.M - (double)M;
+  const double a = in && p.Z > 0.0 ? power(d * 1.4426950408889634) : 0.0;
+  const double Z = wave_sum(a * p.Z), S = wave_sum(a > 0.0 ? a * (p.S + d * p.Z) : 0.0);
+  const int rank = (int)wave_sum(in ? (double)p.before : 0.0);
+  const double lnz = log(Z);
+  if (tid == 0) {
+    A.rank[row] = p.given ? rank : -1;
+    A.logprob[row] = p.given ? log_prob(p.token, M, Z, lnz) : -INFINITY;
+    A.entropy[row] = Z == 0.0 ? 0.f : (float)(lnz - S / Z);
+  }
+  __syncthreads();
+  for (int q = tid; q < n; q += kJoinThreads) {
+    const uint64_t mine = s_key[q];
+    int r = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) r += s_key[j] > mine;
+    if (r >= top || mine == 0) continue;
+    A.top_idx[(size_t)row * top + r] = (int)cand_index(mine);
+    A.top_lp[(size_t)row * top + r] = log_prob(key_value((uint32_t)(mine >> 32)), M, Z, lnz);
   }
 }
 
 }  // namespace
 
+// Parts of a row: a workgroup for each CU where the rows are few, none with less than a whole batch of
+// values.  The vector unit of one CU bounds a row on its own (152K values in bf16: 10 us); the
+// join costs 4 us and more workgroups contend.  us a call (5 alternatives, from graphs) with 1 / 2
+// / 4 / 8 parts, bf16 rows of 151,936: one row 18.1 / 15.5 / 13.1 / 12.3, 64 rows 27.1 / 20.1 /
+// 15.3 / 16.9, 128 rows 27.0 / 21.4 / 21.5 / 26.2, 256 rows 29.7 / 28.5 / 31.3 / 43.0; fp32 rows of
+// 50,257: one 10.0 / 10.7 / 9.8 / 9.4, 64 rows 13.7 / 13.1 / 11.1 / 12.7, 256 rows 17.3 / 20.2 / 21.8 /
+// 28.7; bf16 rows of 32,000: one 9.0 / 10.6 / 10.5 / 10.3.
+int logprobs_parts(int64_t rows, int vocab, int dtype) {
+  if (rows <= 0) return 1;
+  const int64_t batch = kThreads * kUnits * (dtype == TAPS_BF16 ? 8 : 4);
+  const int64_t most = std::min<int64_t>(kMaxParts, vocab / batch);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, 256 / rows));
+}
+size_t logprobs_ws_bytes(int64_t rows, int vocab, int dtype, int top) {
+  const int parts = logprobs_parts(rows, vocab, dtype);
+  return parts > 1 ? (size_t)rows * parts * (sizeof(Part) + (size_t)top * sizeof(uint64_t)) : 0;
+}
+
 hipError_t launch_logprobs(const void* logits, int64_t row_bytes, int batch, int budget,
                            int vocab, int dtype, const int32_t* n_nodes, const int32_t* tokens,
                            int top, float* logprob, float* entropy, int32_t* rank,
-                           int32_t* top_idx, float* top_logprob, hipStream_t s) {
+                           int32_t* top_idx, float* top_logprob, void* ws, hipStream_t s) {
   const int64_t rows = (int64_t)batch * budget;
   if (rows <= 0) return hipSuccess;
   LogprobArgs A;
@@ -478,15 +571,15 @@ hipError_t launch_logprobs(const void* logits, int64_t row_bytes, int batch, int
   A.budget = budget, A.vocab = vocab, A.top = top, A.n_nodes = n_nodes, A.tokens = tokens;
   A.logprob = logprob, A.entropy = entropy, A.rank = rank;
   A.top_idx = top_idx, A.top_lp = top_logprob;
-  const unsigned grid = (unsigned)rows;
-  const bool few = rows <= (getenv("LP_ROWS") ? atoi(getenv("LP_ROWS")) : 256);
-  if (dtype == TAPS_BF16) {
-    if (few) logprobs_kernel<uint16_t, 1024><<<grid, 1024, 0, s>>>(A);
-    else logprobs_kernel<uint16_t, 512><<<grid, 512, 0, s>>>(A);
-  } else {
-    if (few) logprobs_kernel<float, 1024><<<grid, 1024, 0, s>>>(A);
-    else logprobs_kernel<float, 512><<<grid, 512, 0, s>>>(A);
-  }
+  A.parts = logprobs_parts(rows, vocab, dtype);
+  A.part = (Part*)ws;
+  A.keys = (uint64_t*)(A.part + rows * A.parts);
+  const dim3 grid((unsigned)rows, (unsigned)A.parts);
+  if (dtype == TAPS_BF16) logprobs_kernel<uint16_t><<<grid, kThreads, 0, s>>>(A);
+  else logprobs_kernel<float><<<grid, kThreads, 0, s>>>(A);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || A.parts == 1) return e;
+  logprobs_join_kernel<<<(unsigned)rows, kJoinThreads, 0, s>>>(A);
   return hipGetLastError();
 }
 

@@ -97,7 +97,7 @@ def test_chunk_workspace_is_bounded_and_none_for_short_caches(lib):
 
 def logprobs(lib, **kw):
     a = dict(x=F, stride=1024, batch=2, budget=3, vocab=1000, dtype=0, n=F, tok=F, top=5, lp=F,
-             ent=F, rank=F, idx=F, tlp=F)
+             ent=F, rank=F, idx=F, tlp=F, ws=F, ws_bytes=1 << 30)
     a.update(kw)
     return lib.taps_logprobs(*a.values(), None)
 
@@ -109,6 +109,14 @@ def logprobs(lib, **kw):
     (dict(top=-1), INV), (dict(top=65), UNS), (dict(vocab=4, top=5), INV),
     (dict(x=F + 2), INV), (dict(x=F + 1, vocab=1001), INV), (dict(tok=F + 2), INV),
     (dict(rank=F + 1), INV), (dict(n=F + 2), INV), (dict(idx=F + 2), INV),
+    (dict(vocab=100000, stride=100000, ws=None), WS), (dict(vocab=100000, stride=100000, ws=F + 8), WS),
+    (dict(vocab=100000, stride=100000, ws_bytes=99), WS),
 ] + [({k: None}, INV) for k in ("x", "tok", "lp", "ent", "rank", "idx", "tlp")])
 def test_logprobs_refuses(lib, kw, status):
     assert logprobs(lib, **kw) == status
+
+
+def test_logprobs_workspace_is_for_few_rows(lib):
+    ws = lib.taps_logprobs_workspace_bytes
+    assert ws(4, 512, 151936, 0, 5) == 0 and ws(1, 1, 1000, 0, 5) == 0 and ws(0, 1, 151936, 0, 5) == 0
+    assert 0 < ws(1, 1, 151936, 0, 64) <= 16 * (32 + 8 * 64) and ws(1, 1, 151936, 0, 65) == 0
