@@ -5,10 +5,11 @@
 // (a, b) -> m (a cos - b sin), m (b cos + a sin).  Pairs are (j, j + rot / 2) or (2j, 2j + 1); the
 // head's dims from rot on are not turned.  V is copied.
 //
-// A head is HD / 8 lanes of 8 values each, two runs of four: (half layout) the runs 4j.. and
-// rot / 2 + 4j.. of the four pairs 4j..4j+3, or eight neighbours, so that both values of a pair sit
-// in one lane and the lane's four angles are the same for every head.  A wave takes 64 / (HD / 8)
-// heads at a time, all heads (Q, K and V) of its row with one set of angles.
+// A lane holds 2 RUN values of a head in two runs: (half layout) RUN * j.. and rot / 2 + RUN * j.. of
+// the pairs RUN * j.., or neighbours, so that both values of a pair sit in one lane and the lane's
+// RUN angles are the same for every head.  A run is 16 bytes where the rotated part is whole runs
+// of them, else (bf16, rot_dim not a multiple of 16) 8.  A wave takes as many heads of one kind (Q,
+// K or V) at a time as fit, all heads of its row with one set of angles.
 //
 // Angles are formed in 64 bits, in turns: a position of 2^20 times a frequency leaves an fp32
 // product no better than 2^-4 of a radian.  The reduced angle (|x| <= pi / 4, off by 2^-25) goes
@@ -22,9 +23,7 @@
 namespace taps {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
@@ -42,28 +41,29 @@ struct RopeArgs {
   int rows, Hq, Hkv, rot;
 };
 
-// four values in memory: raw words
-template <typename T>
-struct Quad;
-template <>
-struct Quad<__bf16> {
-  typedef u32x2 raw;
+// a run in memory: raw words
+template <typename T, int RUN>
+struct Run;
+template <int RUN>
+struct Run<__bf16, RUN> {
+  typedef uint32_t raw __attribute__((ext_vector_type(RUN / 2)));
   static __device__ inline void widen(const raw& r, float* x) {
-    x[0] = __uint_as_float(r[0] << 16);
-    x[1] = __uint_as_float(r[0] & 0xFFFF0000u);
-    x[2] = __uint_as_float(r[1] << 16);
-    x[3] = __uint_as_float(r[1] & 0xFFFF0000u);
+#pragma unroll
+    for (int t = 0; t < RUN / 2; ++t) {
+      x[2 * t] = __uint_as_float(r[t] << 16);
+      x[2 * t + 1] = __uint_as_float(r[t] & 0xFFFF0000u);
+    }
   }
   static __device__ inline raw narrow(const float* x) {   // to nearest, ties to even
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    bf16x4 b;
+    typedef __bf16 bf16xn __attribute__((ext_vector_type(RUN)));
+    bf16xn b;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) b[t] = (__bf16)x[t];
+    for (int t = 0; t < RUN; ++t) b[t] = (__bf16)x[t];
     return __builtin_bit_cast(raw, b);
   }
 };
 template <>
-struct Quad<float> {
+struct Run<float, 4> {
   typedef u32x4 raw;
   static __device__ inline void widen(const raw& r, float* x) {
 #pragma unroll
@@ -80,12 +80,12 @@ __device__ inline float dpp_add(float x) {
   return x + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, 0xf, 0xf,
                                                          true));
 }
-// sum over the LPH (8 or 16) lanes of a head, in each of them
+// sum over the LPH (4, 8 or 16) lanes of a head, in each of them
 template <int LPH>
 __device__ inline float head_sum(float x) {
   x = dpp_add<0xB1>(x);    // lane ^ 1
   x = dpp_add<0x4E>(x);    // lane ^ 2
-  x = dpp_add<0x141>(x);   // the other four of eight
+  if constexpr (LPH >= 8) x = dpp_add<0x141>(x);    // the other four of eight
   if constexpr (LPH == 16) x = dpp_add<0x140>(x);   // the other eight of sixteen
   return x;
 }
@@ -114,118 +114,122 @@ __device__ inline void turn(double pos, double f, float m, float& c, float& s) {
   c = m * (((n + 1) & 2) ? -b : b);
 }
 
-template <typename T, int HD, bool INTERLEAVED>
+template <typename T, int HD, bool INTERLEAVED, int RUN>
 __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs A, int per_row) {
-  using Qd = Quad<T>;
-  typedef typename Qd::raw raw;
-  constexpr int LPH = HD / 8, HPW = kWave / LPH;
-  constexpr int CH = 4;   // heads of a lane whose loads are in flight together
+  using Rn = Run<T, RUN>;
+  typedef typename Rn::raw raw;
+  constexpr int EPL = 2 * RUN, LPH = HD / EPL, HPW = kWave / LPH;
+  constexpr int CH = 3;   // passes whose loads are in flight together
   const int lane = threadIdx.x & (kWave - 1), j = lane % LPH, hl = lane / LPH;
-  const int rq = A.rot / 4;
-  const bool turned = j < rq / 2;
+  const bool turned = j < A.rot / EPL;
   // first dims of the lane's two runs
-  const int d0 = INTERLEAVED ? 8 * j : turned ? 4 * j : A.rot + 8 * (j - rq / 2);
-  const int d1 = !INTERLEAVED && turned ? A.rot / 2 + 4 * j : d0 + 4;
-  const int heads = A.Hq + 2 * A.Hkv, passes = (heads + HPW - 1) / HPW;
+  const int d0 = INTERLEAVED ? EPL * j : turned ? RUN * j : A.rot + EPL * (j - A.rot / EPL);
+  const int d1 = !INTERLEAVED && turned ? A.rot / 2 + RUN * j : d0 + RUN;
+  // passes over the heads of Q, K and V
+  const int nq = (A.Hq + HPW - 1) / HPW, nk = (A.Hkv + HPW - 1) / HPW, passes = nq + 2 * nk;
 
-  double f[4];
+  double f[RUN];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-    f[t] = turned ? A.freq[4 * j + t] * 0.15915494309189535 : 0.0;   // 1 / (2 pi)
-  float qw[8], kw[8];
-  auto weights = [&](const void* w, float* x) {
-    if (!w) return;
-    Qd::widen(*(const raw*)((const T*)w + d0), x);
-    Qd::widen(*(const raw*)((const T*)w + d1), x + 4);
-  };
-  weights(A.qw, qw);
-  weights(A.kw, kw);
+  for (int t = 0; t < RUN; ++t)
+    f[t] = turned ? A.freq[RUN * j + t] * 0.15915494309189535 : 0.0;   // 1 / (2 pi)
+  raw w[2][2] = {};
+  if (A.qw) w[0][0] = *(const raw*)((const T*)A.qw + d0), w[0][1] = *(const raw*)((const T*)A.qw + d1);
+  if (A.kw) w[1][0] = *(const raw*)((const T*)A.kw + d0), w[1][1] = *(const raw*)((const T*)A.kw + d1);
 
   // a row's passes are dealt to per_row waves
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int64_t units = (int64_t)A.rows * per_row, step = (int64_t)gridDim.x * kWaves;
   for (int64_t u = (int64_t)blockIdx.x * kWaves + wave; u < units; u += step) {
-    const int row = (int)(u / per_row), part = (int)(u - (int64_t)row * per_row);
-    const int p0 = (int)((int64_t)passes * part / per_row);
-    const int p1 = (int)((int64_t)passes * (part + 1) / per_row);
+    int row = (int)u, p0 = 0, p1 = passes;
+    if (per_row > 1) {
+      row = (int)u / per_row;   // (few rows)
+      const int part = (int)u - row * per_row;
+      p0 = passes * part / per_row, p1 = passes * (part + 1) / per_row;
+    }
     const int64_t slot = A.slots[row];
     const bool keep = slot >= 0 && slot < A.pool_rows;
     const double pos = (double)A.pos[row];
-    const unsigned char* const q = A.Q + (size_t)row * A.qs;
-    const unsigned char* const k = A.K + (size_t)row * A.ks;
-    const unsigned char* const v = A.V + (size_t)row * A.vs;
-    float c[4], s[4];
+    float c[RUN], s[RUN];
     bool first = true;
     for (int p = p0; p < p1; p += CH) {
-      raw x0[CH] = {}, x1[CH] = {};
+      raw x0[CH], x1[CH];
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const int h = (p + i) * HPW + hl;
-        if (p + i < p1 && h < heads) {
-          const int kind = h < A.Hq ? 0 : h < A.Hq + A.Hkv ? 1 : 2;
-          const int hh = kind == 0 ? h : kind == 1 ? h - A.Hq : h - A.Hq - A.Hkv;
-          const T* const src = (const T*)(kind == 0 ? q : kind == 1 ? k : v) + (size_t)hh * HD;
-          x0[i] = *(const raw*)(src + d0);
-          x1[i] = *(const raw*)(src + d1);
-        }
+        const int q = min(p + i, p1 - 1);   // (past the last: the same again, not stored)
+        const int kind = q < nq ? 0 : q < nq + nk ? 1 : 2;
+        const unsigned char* const base = kind == 0   ? A.Q + (size_t)row * A.qs
+                                          : kind == 1 ? A.K + (size_t)row * A.ks
+                                                      : A.V + (size_t)row * A.vs;
+        const int h = (kind == 0 ? q : kind == 1 ? q - nq : q - nq - nk) * HPW + hl;
+        const uint32_t at = (uint32_t)min(h, (kind == 0 ? A.Hq : A.Hkv) - 1) * HD;
+        x0[i] = *(const raw*)((const T*)base + (at + d0));
+        x1[i] = *(const raw*)((const T*)base + (at + d1));
       }
       if (first) {   // under the first loads
         first = false;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) turn(pos, f[t], A.mscale, c[t], s[t]);
+        for (int t = 0; t < RUN; ++t) turn(pos, f[t], A.mscale, c[t], s[t]);
       }
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const int h = (p + i) * HPW + hl;
-        const bool in = p + i < p1 && h < heads;
-        const int kind = h < A.Hq ? 0 : h < A.Hq + A.Hkv ? 1 : 2;
-        const int hh = kind == 0 ? h : kind == 1 ? h - A.Hq : h - A.Hq - A.Hkv;
-        float x[8];
-        Qd::widen(x0[i], x);
-        Qd::widen(x1[i], x + 4);
-        float sq = 0.f;
+        if (p + i >= p1) break;
+        const int q = p + i, kind = q < nq ? 0 : q < nq + nk ? 1 : 2;
+        const int h = (kind == 0 ? q : kind == 1 ? q - nq : q - nq - nk) * HPW + hl;
+        const bool in = h < (kind == 0 ? A.Hq : A.Hkv) && (kind == 0 || keep);
+        if (kind != 2) {
+          float x[EPL];
+          Rn::widen(x0[i], x);
+          Rn::widen(x1[i], x + RUN);
+          if (kind == 0 ? A.qw != nullptr : A.kw != nullptr) {
+            float sq = 0.f;
 #pragma unroll
-        for (int t = 0; t < 8; ++t) sq = fmaf(x[t], x[t], sq);
-        const float ms = fmaf(head_sum<LPH>(sq), 1.f / HD, A.eps);
-        float rs = __builtin_amdgcn_rsqf(ms);
-        // one Newton step: the instruction alone is off by a unit in the last place
-        const float e = fmaf(-ms * rs, rs, 1.f);
-        rs = e == e && e < 1.f ? fmaf(0.5f * rs, e, rs) : rs;   // (not of 0 and infinity)
-        const bool norm = kind == 0 ? A.qw != nullptr : A.kw != nullptr;
-        if (norm) {
+            for (int t = 0; t < EPL; ++t) sq = fmaf(x[t], x[t], sq);
+            const float ms = fmaf(head_sum<LPH>(sq), 1.f / HD, A.eps);
+            float rs = __builtin_amdgcn_rsqf(ms);
+            // one Newton step: the instruction alone is off by a unit in the last place
+            const float e = fmaf(-ms * rs, rs, 1.f);
+            rs = e == e && e < 1.f ? fmaf(0.5f * rs, e, rs) : rs;   // (not of 0 and infinity)
+            float g[EPL];
+            Rn::widen(kind == 0 ? w[0][0] : w[1][0], g);
+            Rn::widen(kind == 0 ? w[0][1] : w[1][1], g + RUN);
 #pragma unroll
-          for (int t = 0; t < 8; ++t) x[t] = x[t] * rs * (kind == 0 ? qw[t] : kw[t]);
-        }
-        if (turned) {
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const int a = INTERLEAVED ? 2 * t : t, b = INTERLEAVED ? 2 * t + 1 : 4 + t;
-            const float xa = x[a], xb = x[b];
-            x[a] = fmaf(xa, c[t], -xb * s[t]);
-            x[b] = fmaf(xb, c[t], xa * s[t]);
+            for (int t = 0; t < EPL; ++t) x[t] = x[t] * rs * g[t];
           }
+          if (turned) {
+#pragma unroll
+            for (int t = 0; t < RUN; ++t) {
+              const int a = INTERLEAVED ? 2 * t : t, b = INTERLEAVED ? 2 * t + 1 : RUN + t;
+              const float xa = x[a], xb = x[b];
+              x[a] = fmaf(xa, c[t], -xb * s[t]);
+              x[b] = fmaf(xb, c[t], xa * s[t]);
+            }
+          }
+          x0[i] = Rn::narrow(x);
+          x1[i] = Rn::narrow(x + RUN);
         }
-        T* dst;
-        if (kind == 0) dst = (T*)A.Qo + ((size_t)row * A.Hq + hh) * HD;
-        else dst = (T*)(kind == 1 ? A.Kp : A.Vp) + ((size_t)slot * A.Hkv + hh) * HD;
-        if (in && (kind == 0 || keep)) {
-          *(raw*)(dst + d0) = kind == 2 ? x0[i] : Qd::narrow(x);
-          *(raw*)(dst + d1) = kind == 2 ? x1[i] : Qd::narrow(x + 4);
+        unsigned char* const base =
+            kind == 0 ? A.Qo + (size_t)row * A.Hq * (HD * sizeof(T))
+                      : (kind == 1 ? A.Kp : A.Vp) + (size_t)slot * A.Hkv * (HD * sizeof(T));
+        if (in) {
+          const uint32_t at = (uint32_t)h * HD;
+          *(raw*)((T*)base + (at + d0)) = x0[i];
+          *(raw*)((T*)base + (at + d1)) = x1[i];
         }
       }
     }
   }
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int RUN>
 hipError_t launch_t(const RopeArgs& A, int interleaved, hipStream_t s) {
-  const int passes = (A.Hq + 2 * A.Hkv + kWave / (HD / 8) - 1) / (kWave / (HD / 8));
-  // few rows: a row's heads over several waves
+  constexpr int HPW = kWave / (HD / (2 * RUN));
+  const int passes = (A.Hq + HPW - 1) / HPW + 2 * ((A.Hkv + HPW - 1) / HPW);
+  // few rows: a row's passes over several waves
   const int per_row = std::min(passes, std::max(1, 2048 / A.rows));
   const int64_t units = (int64_t)A.rows * per_row;
   const unsigned grid = (unsigned)std::min<int64_t>((units + kWaves - 1) / kWaves, 2048);
-  if (interleaved) rope_kernel<T, HD, true><<<grid, kThreads, 0, s>>>(A, per_row);
-  else rope_kernel<T, HD, false><<<grid, kThreads, 0, s>>>(A, per_row);
+  if (interleaved) rope_kernel<T, HD, true, RUN><<<grid, kThreads, 0, s>>>(A, per_row);
+  else rope_kernel<T, HD, false, RUN><<<grid, kThreads, 0, s>>>(A, per_row);
   return hipGetLastError();
 }
 
@@ -244,11 +248,12 @@ hipError_t launch_rope(const void* Q, const void* K, const void* V, int64_t q_st
   A.Qo = (unsigned char*)Qo, A.Kp = (unsigned char*)Kp, A.Vp = (unsigned char*)Vp;
   A.pool_rows = pool_rows, A.eps = r.norm_eps, A.mscale = r.mscale;
   A.rows = rows, A.Hq = Hq, A.Hkv = Hkv, A.rot = r.rot_dim;
-  if (dtype == TAPS_BF16)
-    return head_dim == 128 ? launch_t<__bf16, 128>(A, r.interleaved, s)
-                           : launch_t<__bf16, 64>(A, r.interleaved, s);
-  return head_dim == 128 ? launch_t<float, 128>(A, r.interleaved, s)
-                         : launch_t<float, 64>(A, r.interleaved, s);
+  const int il = r.interleaved;
+  if (dtype == TAPS_FP32)
+    return head_dim == 128 ? launch_t<float, 128, 4>(A, il, s) : launch_t<float, 64, 4>(A, il, s);
+  if (r.rot_dim % 16 == 0)
+    return head_dim == 128 ? launch_t<__bf16, 128, 8>(A, il, s) : launch_t<__bf16, 64, 8>(A, il, s);
+  return head_dim == 128 ? launch_t<__bf16, 128, 4>(A, il, s) : launch_t<__bf16, 64, 4>(A, il, s);
 }
 
 }  // namespace taps
