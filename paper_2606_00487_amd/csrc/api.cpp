@@ -764,7 +764,7 @@ taps_status chunk_attn_paged_validate(int32_t batch, int32_t rows, int32_t Hq, i
   // query rows of a request and workgroups are counted in 32 bits
   if (Hq > 65535 || batch > 1 << 20 || (int64_t)rows * Hq > (int64_t)1 << 30)
     return TAPS_ERR_UNSUPPORTED;
-  if (plan_chunk(batch, rows, Hq, Hkv, max_len, dtype).items * Hkv > (int64_t)1 << 30)
+  if (plan_chunk(batch, rows, Hq, Hkv, head_dim, max_len, dtype).items * Hkv > (int64_t)1 << 30)
     return TAPS_ERR_UNSUPPORTED;
   return TAPS_OK;
 }
@@ -776,7 +776,7 @@ size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq,
                                 1.0f) != TAPS_OK ||
       batch == 0 || rows == 0)
     return 0;
-  return chunk_ws_bytes(plan_chunk(batch, rows, Hq, Hkv, max_len, dtype), head_dim, dtype);
+  return chunk_ws_bytes(plan_chunk(batch, rows, Hq, Hkv, head_dim, max_len, dtype), head_dim);
 }
 
 taps_status chunk_attn_paged(const void* Q, int64_t q_stride, const void* K_pages,
@@ -805,8 +805,8 @@ taps_status chunk_attn_paged(const void* Q, int64_t q_stride, const void* K_page
     return TAPS_ERR_INVALID_ARG;
   if (overlap(O, span(rows, row, row, es), Q, span(rows, q_stride, row, es)))
     return TAPS_ERR_INVALID_ARG;
-  const ChunkPlan p = plan_chunk(batch, rows, Hq, Hkv, max_len, dtype);
-  const size_t need = chunk_ws_bytes(p, head_dim, dtype);
+  const ChunkPlan p = plan_chunk(batch, rows, Hq, Hkv, head_dim, max_len, dtype);
+  const size_t need = chunk_ws_bytes(p, head_dim);
   if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15) != 0)) return TAPS_ERR_WORKSPACE;
   const PagedKV pk{block_table, max_pages, num_pages, page_shift_of(page_rows)};
   return launch_chunk(Q, q_stride, K_pages, V_pages, pk, q_start, kv_len, batch, rows, Hq, Hkv,

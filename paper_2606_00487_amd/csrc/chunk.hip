@@ -3,7 +3,7 @@
 // Request b brings n new tokens; its cache holds kv rows, theirs the last n.  Token i is at
 // position p = kv - n + i and sees the rows j <= p (within a window: p - window < j <= p):
 // O[i,h] = softmax_j(scale * q_ih . k_jg) v_jg.  The query rows of a KV head are the tokens x the
-// G query heads that share it, in tiles of kM rows; keys go by in tiles of 64.
+// G query heads that share it, in tiles of M rows; keys go by in tiles of 64.
 //
 // Pieces.  A workgroup takes the keys of one (KV head, query tile), or a part of them: no piece
 // has more than L key tiles, L = all tiles' keys / 256, so that a few long requests fill the chip
@@ -38,6 +38,7 @@ constexpr int kThreads = 512;
 constexpr int kUnit = 64;      // keys per unit of a piece's length
 constexpr int kTarget = 256;   // pieces that the longest of them is cut for
 constexpr int kMinUnits = 4;   // shorter pieces would be mostly start and end
+constexpr int kCutGain = 6;    // units that a cut has to save: the second kernel costs as much
 
 struct ChunkArgs {
   const unsigned char *Q, *K, *V;
@@ -47,8 +48,8 @@ struct ChunkArgs {
   int batch, rows, Hq, Hkv, max_len, window;
   float scale_log2;
   unsigned char* O;
-  float* wsO;     // [slots][kM][HD]; null: no piece is cut
-  float2* wsML;   // [slots][kM]
+  float* wsO;     // [slots][M][HD]; null: no piece is cut
+  float2* wsML;   // [slots][M]
   int slots;
 };
 
@@ -78,8 +79,12 @@ __device__ inline int64_t wave_sum_i64(int64_t v) {
   return (int64_t)lane_u64(wave_scan_u64((uint64_t)v), kWave - 1);
 }
 
-// Key units per piece at most.  Sum of tiles * units over the batch, times the KV heads, in
-// kTarget parts.
+// Key units per piece at most: the sum of tiles * units over the batch, times the KV heads, in
+// kTarget parts
+__device__ inline int units_per_piece(int64_t total, int Hkv) {
+  const int64_t L = (total * Hkv + kTarget - 1) / kTarget;
+  return (int)max((int64_t)kMinUnits, min(L, (int64_t)1 << 30));
+}
 template <int M>
 __device__ inline int piece_units(const ChunkArgs& A, int G, const Request& first) {
   const int lane = threadIdx.x & (kWave - 1);
@@ -88,8 +93,7 @@ __device__ inline int piece_units(const ChunkArgs& A, int G, const Request& firs
     const Request r = request_of<M>(A, b0 + lane, G);
     total += wave_sum_i64((int64_t)r.tiles * r.units);
   }
-  const int64_t L = (total * A.Hkv + kTarget - 1) / kTarget;
-  return (int)max((int64_t)kMinUnits, min(L, (int64_t)1 << 30));
+  return units_per_piece(total, A.Hkv);
 }
 
 // Piece `item` of the batch (without the KV head), item counting the requests' tiles * splits.  The
@@ -105,16 +109,38 @@ struct Piece {
 template <int M, int ROWS>
 __device__ inline Piece find_piece(const ChunkArgs& A, int G, int item) {
   const int lane = threadIdx.x & (kWave - 1);
+  if (A.batch == 1) {   // no sums over the batch, all of it uniform
+    const Request r = request_of<M>(A, 0, G);
+    Piece p{};
+    p.q0 = r.q0, p.n = r.n, p.kv = r.kv, p.tiles = r.tiles;
+    p.L = 1 << 30;
+    p.splits = 1;
+    if (A.wsO != nullptr) {
+      p.L = units_per_piece((int64_t)r.tiles * r.units, A.Hkv);
+      if (r.units - kCutGain > p.L) p.splits = (r.units + p.L - 1) / p.L;
+      else p.L = 1 << 30;
+    }
+    if constexpr (ROWS > 0) {
+      p.found = p.splits > 1 && item < (r.n * G + ROWS - 1) / ROWS;
+      p.group = item;
+      p.tile = item / (M / ROWS);
+    } else {
+      p.found = item < r.tiles * p.splits;
+      p.split = r.tiles == 0 || p.splits == 1 ? 0 : item / r.tiles;
+      p.tile = r.tiles - 1 - (item - p.split * r.tiles);
+    }
+    p.slot = p.tile;
+    return p;
+  }
   const Request first = request_of<M>(A, lane, G);
   const bool whole = A.wsO == nullptr;
   const int L = whole ? 1 << 30 : piece_units<M>(A, G, first);
   Piece p{};
-  p.L = L;
   p.found = false;
   int64_t before = 0, cut_before = 0;
   for (int b0 = 0; b0 < A.batch; b0 += kWave) {
     const Request r = b0 == 0 ? first : request_of<M>(A, b0 + lane, G);
-    const int splits = whole ? 1 : max(1, (r.units + L - 1) / L);
+    const int splits = whole || r.units - kCutGain <= L ? 1 : (r.units + L - 1) / L;
     const int64_t pieces = (int64_t)r.tiles * splits;
     const int64_t cut = splits > 1 ? pieces : 0;
     int64_t count = pieces;
@@ -130,6 +156,7 @@ __device__ inline Piece find_piece(const ChunkArgs& A, int G, int item) {
       p.b = b0 + l;
       p.q0 = of(r.q0), p.n = of(r.n), p.kv = of(r.kv), p.tiles = of(r.tiles);
       p.splits = of(splits);
+      p.L = p.splits > 1 ? L : 1 << 30;
       if constexpr (ROWS > 0) {
         p.group = at;
         p.tile = at / (M / ROWS);
@@ -175,7 +202,6 @@ __device__ inline int chunk_perm(int r) {
   else return ((r & 3) << 1) | ((r >> 2) & 1);
 }
 
-constexpr int kM = 256;   // bf16 query rows per workgroup
 // the order of a region's instructions: N times a matrix product, DS LDS reads, V vector and T
 // transcendental instructions
 template <int N, int DS, int V, int T>
@@ -192,29 +218,32 @@ template <int P>
 struct Slot {
   static constexpr int value = P;
 };
-template <int HD>
-__global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A) {
+// W waves, 32 query rows each
+template <int HD, int W>
+__global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
 #if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int M = 32 * W;
   constexpr int KT = 64;              // keys per tile
   constexpr int RING = 3;             // tiles of K and of V in LDS
   constexpr int ROWB = HD * 2, CPR = ROWB / 16;   // bytes and 16-byte chunks of a row
   constexpr int TILEB = KT * ROWB;
   constexpr int NKK = HD / 16, NDB = HD / 32;
-  constexpr int BPW = TILEB / 1024 / 4;           // 1 KB loads per wave and tile: 4 or 2
+  constexpr int HW = W / 2;                       // waves that load K; the others load V
+  constexpr int BPW = TILEB / 1024 / HW;          // 1 KB loads per wave and tile
   constexpr int BROWS = 1024 / ROWB;              // rows per load: 4 or 8
   typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
   __shared__ __attribute__((aligned(1024))) unsigned char s_k[RING * TILEB], s_v[RING * TILEB];
 
   const int G = A.Hq / A.Hkv;
   const int kvh = blockIdx.x % A.Hkv;
-  const Piece p = find_piece<kM, 0>(A, G, blockIdx.x / A.Hkv);
+  const Piece p = find_piece<M, 0>(A, G, blockIdx.x / A.Hkv);
   if (!p.found) return;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hl = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int last = p.n * G - 1;                   // last query row
-  const int row0 = p.tile * kM;
+  const int row0 = p.tile * M;
   int lo, hi;
-  key_range(A, p, row0 / G, min(row0 + kM - 1, last) / G, lo, hi);
+  key_range(A, p, row0 / G, min(row0 + M - 1, last) / G, lo, hi);
   // this piece's key tiles [k0, k0 + nt * 64)
   const int u0 = lo / kUnit, u1 = (hi + kUnit - 1) / kUnit;
   const int ub = u0 + min((int64_t)p.split * p.L, (int64_t)(u1 - u0));
@@ -241,19 +270,14 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
       wrow0 <= last ? base + min(wrow0 + 31, last) / G : -1);
   const int from_hi = A.window > 0 ? pos_hi - A.window + 1 : 0;
 
-  bf16x8 q[NKK];
-  {
-    const __bf16* const qp =
-        (const __bf16*)A.Q + (size_t)(p.q0 + tok) * A.q_stride + (size_t)head * HD;
-#pragma unroll
-    for (int kk = 0; kk < NKK; ++kk) q[kk] = *(const bf16x8*)(qp + kk * 16 + hl * 8);
-  }
+  bf16x8 q[NKK];   // the lane's query: dims 16 kk + 8 hl ..
 
-  // ---- direct loads.  Waves 0-3 load K, waves 4-7 V, of each tile one half (32 keys, in one page)
-  // per two waves, BPW blocks of 1 KB each.  Lane l holds the page of this wave's half of tile
-  // pw + l.
+  // ---- direct loads.  The first half of the waves loads K, the second V; of each tile one half (32
+  // keys, in one page) per HW / 2 waves, BPW blocks of 1 KB each.  Lane l holds the page of this
+  // wave's half of tile pw + l.
   const uint32_t rsb = (uint32_t)A.Hkv * ROWB;
-  const int half = (wave >> 1) & 1;
+  const bool loads_k = wave < HW;
+  const int half = wave % HW / (HW / 2), block0 = wave % (HW / 2) * BPW;
   const int32_t* const bt = A.pk.btab + (size_t)p.b * A.pk.max_pages;
   auto entries = [&](int t0) {
     const int r = min(k0 + (t0 + lane) * KT + half * 32, k_end - 1);   // rows of the piece only
@@ -262,13 +286,13 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
   };
   int pw = 0, pages = 0, pages_next = 0;
   if (nt > 0) pages = entries(0), pages_next = entries(64);
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(wave < 4 ? s_k : s_v)) +
-                        (uint32_t)(half * 2 + (wave & 1)) * BPW * 1024;
-  const uint64_t src0 = (uint64_t)((wave < 4 ? A.K : A.V) + (size_t)kvh * ROWB);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(loads_k ? s_k : s_v)) +
+                        (uint32_t)(half * (TILEB / 2) + block0 * 1024);
+  const uint64_t src0 = (uint64_t)((loads_k ? A.K : A.V) + (size_t)kvh * ROWB);
   uint32_t ld_off[BPW];
 #pragma unroll
   for (int j = 0; j < BPW; ++j) {
-    const int r = ((wave & 1) * BPW + j) * BROWS + lane / CPR;         // row in the half tile
+    const int r = (block0 + j) * BROWS + lane / CPR;                   // row in the half tile
     ld_off[j] = (uint32_t)r * rsb + (uint32_t)(((lane % CPR) ^ chunk_perm<HD>(r)) * 16);
   }
   // `next` is the resource over the half tile that this wave loads next, `key` its first key: its
@@ -295,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
       asm volatile("" : "+v"(ln));                // (rare: nothing of it is kept in registers)
 #pragma unroll
       for (int j = 0; j < BPW; ++j) {
-        const int r = ((wave & 1) * BPW + j) * BROWS + ln / CPR;
+        const int r = (block0 + j) * BROWS + ln / CPR;
         const uint32_t off = key + r < k_lo ? 0x7FFFFF00u : ld_off[j];
         load_lds16_at(next, lds0 + slot * TILEB + j * 1024, off);
       }
@@ -426,8 +450,8 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
     TAPS_WAIT_VMCNT(BPW);
     TAPS_LDS_BARRIER();
   };
-  const int ahead = wave < 4 ? 3 : 2;             // tiles from a step's to the one it loads
-  auto fill = [&](int P) __attribute__((always_inline)) { issue(wave < 4 ? P : (P + 2) % 3); };
+  const int ahead = loads_k ? 3 : 2;             // tiles from a step's to the one it loads
+  auto fill = [&](int P) __attribute__((always_inline)) { issue(loads_k ? P : (P + 2) % 3); };
   // Step t: the weights and products of tile t, from its scores (s0, s1; m0: the largest of s0),
   // and the scores of tile t + 1 (past the last one: of zeros) into n0 and, when they are used
   // up, s0.
@@ -477,13 +501,19 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
     // K(0) .. K(2), V(0), V(1)
     prepare(0);
     issue(0);
+    {
+      const __bf16* const qp =
+          (const __bf16*)A.Q + (size_t)(p.q0 + tok) * A.q_stride + (size_t)head * HD;
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) q[kk] = *(const bf16x8*)(qp + kk * 16 + hl * 8);
+    }
     prepare(1);
     issue(1);
     prepare(2);
-    if (wave < 4) {
+    if (loads_k) {
       issue(2);
       prepare(3);
-      TAPS_WAIT_VMCNT(2 * BPW);                   // K(0): this wave's part
+      TAPS_WAIT_VMCNT(2 * BPW);                   // K(0), the queries: this wave's part
     }
     TAPS_LDS_BARRIER();                           // ... and every other wave's
     if (wrow0 > last) {                           // no rows: the wave only loads
@@ -526,7 +556,7 @@ __global__ __launch_bounds__(kThreads) void chunk_bf16_kernel(const ChunkArgs A)
   }
   const int64_t slot = ((int64_t)p.slot + (int64_t)p.split * p.tiles) * A.Hkv + kvh;
   if (slot >= A.slots) return;
-  const size_t at = (size_t)slot * kM + wave * 32 + l32;
+  const size_t at = (size_t)slot * M + wave * 32 + l32;
   float* const out = A.wsO + at * HD;
 #pragma unroll
   for (int db = 0; db < NDB; ++db)
@@ -834,31 +864,48 @@ __global__ __launch_bounds__(kCombineThreads) void chunk_combine_kernel(const Ch
   }
 }
 
+template <typename T, int HD, int M>
+hipError_t launch_combine(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
+  const unsigned grid = (unsigned)(p.cut_groups * A.Hkv);
+  if (p.cut_rows == 16) chunk_combine_kernel<T, HD, M, 16, 1><<<grid, kCombineThreads, 0, s>>>(A);
+  else chunk_combine_kernel<T, HD, M, 4, 4><<<grid, kCombineThreads, 0, s>>>(A);
+  return hipGetLastError();
+}
+
 template <typename T, int HD>
 hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
   const unsigned grid = (unsigned)(p.items * A.Hkv);
-  constexpr int M = sizeof(T) == 2 ? kM : kMF;
-  if constexpr (sizeof(T) == 2) chunk_bf16_kernel<HD><<<grid, kThreads, 0, s>>>(A);
-  else chunk_f32_kernel<HD><<<grid, kThreads, 0, s>>>(A);
+  if constexpr (sizeof(T) == 4) chunk_f32_kernel<HD><<<grid, kThreads, 0, s>>>(A);
+  else if (p.rows == 256) chunk_bf16_kernel<HD, 8><<<grid, 512, 0, s>>>(A);
+  else chunk_bf16_kernel<HD, 4><<<grid, 256, 0, s>>>(A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 0) return e;
-  const unsigned cgrid = (unsigned)(p.cut_groups * A.Hkv);
-  if (p.cut_rows == 16) chunk_combine_kernel<T, HD, M, 16, 1><<<cgrid, kCombineThreads, 0, s>>>(A);
-  else chunk_combine_kernel<T, HD, M, 4, 4><<<cgrid, kCombineThreads, 0, s>>>(A);
-  return hipGetLastError();
+  if constexpr (sizeof(T) == 2)
+    return p.rows == 256 ? launch_combine<T, HD, 256>(A, p, s) : launch_combine<T, HD, 128>(A, p, s);
+  else
+    return launch_combine<T, HD, kMF>(A, p, s);
 }
 
 }  // namespace
 
+// Tiles of 256 query rows use each key tile in LDS twice as often as those of 128; 128 spread a short
+// prompt over more CUs, and at head_dim 64, where the exponentials bound the kernel, three
+// workgroups of them share a CU.  us a call with 256 / 128 (32/8 heads): head_dim 128, prompts of 64,
+// 256, 1024, 2048 and 4096 tokens 15.9 / 12.5, 20.3 / 16.0, 42.9 / 34.6, 67 / 67, 158 / 211; 512
+// tokens over 8K 96 / 106; head_dim 64, prompts of 1024 and 8192 33 / 26, 377 / 319, 512 tokens over 8K
+// 65 / 76, 16 requests of 1 to 1024 tokens over 16K to 1 49 / 47.
 // Bounds of what the device finds.  Tiles: the requests' rows / M, and one more per request.
 // With L >= (sum of tiles * units) * Hkv / kTarget, the cut requests (units > L) have at most
 // kTarget / Hkv tiles between them, and at most twice as many pieces as their tiles * units / L.
-ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int max_len, int dtype) {
+ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int head_dim, int max_len,
+                     int dtype) {
   ChunkPlan p;
-  const int64_t M = dtype == TAPS_BF16 ? kM : kMF;
+  const bool few = (int64_t)rows * Hq <= 32768;   // at most 128 tiles of 256 rows
+  p.rows = dtype == TAPS_FP32 ? kMF : (few ? max_len <= 2048 : head_dim == 64) ? 128 : 256;
+  const int64_t M = p.rows;
   const int64_t tiles = std::min<int64_t>((int64_t)rows * (Hq / Hkv) / M + batch,
                                           (int64_t)rows * (Hq / Hkv));
-  const bool may_cut = max_len > kMinUnits * kUnit;
+  const bool may_cut = max_len > (kMinUnits + kCutGain) * kUnit;
   const int64_t cut = std::min<int64_t>(tiles, std::max(1, kTarget / Hkv));
   // Their groups of rows in the second kernel, by their tiles and by all requests' rows; it takes
   // more than about 1024 of them in turns.  Few rows have many pieces each, which four groups of
@@ -873,9 +920,8 @@ ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int max_len, int dtyp
   return p;
 }
 
-size_t chunk_ws_bytes(const ChunkPlan& p, int head_dim, int dtype) {
-  const size_t M = dtype == TAPS_BF16 ? kM : kMF;
-  return (size_t)p.slots * M * (head_dim * sizeof(float) + sizeof(float2));
+size_t chunk_ws_bytes(const ChunkPlan& p, int head_dim) {
+  return (size_t)p.slots * p.rows * (head_dim * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const void* V,
@@ -892,8 +938,7 @@ hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const vo
   A.O = (unsigned char*)O;
   A.slots = (int)p.slots;
   A.wsO = p.slots ? (float*)ws : nullptr;
-  const size_t M = dtype == TAPS_BF16 ? kM : kMF;
-  A.wsML = p.slots ? (float2*)((float*)ws + (size_t)p.slots * M * head_dim) : nullptr;
+  A.wsML = p.slots ? (float2*)((float*)ws + (size_t)p.slots * p.rows * head_dim) : nullptr;
   if (dtype == TAPS_BF16)
     return head_dim == 128 ? launch_t<__bf16, 128>(A, p, s) : launch_t<__bf16, 64>(A, p, s);
   return head_dim == 128 ? launch_t<float, 128>(A, p, s) : launch_t<float, 64>(A, p, s);

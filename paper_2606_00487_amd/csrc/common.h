@@ -187,13 +187,15 @@ hipError_t launch_rope(const void* Q, const void* K, const void* V, int64_t q_st
 
 // Chunks of new tokens over a paged cache: query tiles, cut along the keys where few
 struct ChunkPlan {
+  int rows;            // query rows of a tile
   int64_t items;       // most pieces per KV head
   int64_t cut_groups;  // most groups of rows per KV head of requests that are cut (0: none ever is)
   int cut_rows;        // rows of such a group: 16, or 4
   int64_t slots;       // most pieces of cut tiles, all KV heads
 };
-ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int max_len, int dtype);
-size_t chunk_ws_bytes(const ChunkPlan& p, int head_dim, int dtype);
+ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int head_dim, int max_len,
+                     int dtype);
+size_t chunk_ws_bytes(const ChunkPlan& p, int head_dim);
 // q_stride in elements
 hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const void* V,
                         const PagedKV& pk, const int32_t* q_start, const int32_t* kv_len,

@@ -88,7 +88,7 @@ def test_chunk_refuses(lib, kw, status):
 
 def test_chunk_workspace_is_bounded_and_none_for_short_caches(lib):
     ws = lib.chunk_attn_paged_workspace_bytes
-    assert ws(4, 100, 32, 8, 128, 256, 64, 0) == 0         # 256 rows are never cut
+    assert ws(4, 100, 32, 8, 128, 640, 64, 0) == 0         # 640 rows are never cut
     n = ws(4, 100, 32, 8, 128, 8192, 64, 0)
     assert 0 < n <= 512 * 256 * (128 * 4 + 8)
     assert ws(4, 1 << 20, 32, 8, 128, 1 << 20, 64, 0) == n  # by the pieces, not by the rows
