@@ -6,7 +6,7 @@
 // G query heads that share it, in tiles of M rows; keys go by in tiles of 64.
 //
 // Pieces.  A workgroup takes the keys of one (KV head, query tile), or a part of them: no piece
-// has more than L key tiles, L = all tiles' keys / 256, so that a few long requests fill the chip
+// has more than L key tiles, L = all tiles' keys / 256 (fp32: 512), so that a few long requests fill the chip
 // as well as many short ones.  The requests' lengths are device data: every workgroup forms L
 // and finds its piece from prefix sums over the batch.  Pieces of a tile that was cut leave
 // (O, max, sum) in fp32, which a second kernel adds.
@@ -17,7 +17,7 @@
 // accumulators; the transposing LDS read takes V in that order.  K and V cycle through rings of
 // three tiles, filled by loads straight into LDS two tiles ahead; S of the next tile is issued
 // between this one's softmax and products.
-// fp32 (v_mfma_f32_16x16x4_f32): eight waves of 16 query rows, key tiles of 32 staged through
+// fp32 (v_mfma_f32_16x16x4_f32): four waves of 16 query rows, key tiles of 32 staged through
 // registers.
 #include <algorithm>
 
@@ -34,11 +34,19 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 512;
 constexpr int kUnit = 64;      // keys per unit of a piece's length
-constexpr int kTarget = 256;   // pieces that the longest of them is cut for
-constexpr int kMinUnits = 4;   // shorter pieces would be mostly start and end
-constexpr int kCutGain = 6;    // units that a cut has to save: the second kernel costs as much
+
+// Query rows of a tile: 128 or 256 in bf16, 64 in fp32.  A cut: into pieces of 1 / target of all
+// tiles' units, none shorter than min_units (mostly start and end), and only where it saves more
+// than `gain` units of a tile's time (the second kernel costs as much).  An fp32 unit takes as long
+// as four in bf16.
+constexpr int kMF = 64;
+struct Cut {
+  int target, min_units, gain;
+};
+__host__ __device__ constexpr Cut cut_of(int M) {
+  return M == kMF ? Cut{512, 2, 1} : Cut{256, 4, 6};
+}
 
 struct ChunkArgs {
   const unsigned char *Q, *K, *V;
@@ -63,7 +71,7 @@ __device__ inline Request request_of(const ChunkArgs& A, int b, int G) {
   Request r{0, 0, 0, 0, 0};
   if (b >= A.batch) return r;
   r.q0 = min(max(A.q_start[b], 0), A.rows);
-  r.n = max(min(A.q_start[b + 1], A.rows) - r.q0, 0);
+  r.n = max(min(max(A.q_start[b + 1], 0), A.rows) - r.q0, 0);
   r.kv = min(max(A.kv_len[b], 0), A.max_len);
   r.tiles = (int)(((int64_t)r.n * G + M - 1) / M);
   r.units = (r.kv + kUnit - 1) / kUnit;
@@ -80,10 +88,17 @@ __device__ inline int64_t wave_sum_i64(int64_t v) {
 }
 
 // Key units per piece at most: the sum of tiles * units over the batch, times the KV heads, in
-// kTarget parts
+// `target` parts
+template <int M>
 __device__ inline int units_per_piece(int64_t total, int Hkv) {
-  const int64_t L = (total * Hkv + kTarget - 1) / kTarget;
-  return (int)max((int64_t)kMinUnits, min(L, (int64_t)1 << 30));
+  constexpr Cut C = cut_of(M);
+  const int64_t L = (total * Hkv + C.target - 1) / C.target;
+  return (int)max((int64_t)C.min_units, min(L, (int64_t)1 << 30));
+}
+// ... and the pieces of a tile of the request
+template <int M>
+__device__ inline int splits_of(int units, int L) {
+  return units - cut_of(M).gain > L ? (units + L - 1) / L : 1;
 }
 template <int M>
 __device__ inline int piece_units(const ChunkArgs& A, int G, const Request& first) {
@@ -93,7 +108,7 @@ __device__ inline int piece_units(const ChunkArgs& A, int G, const Request& firs
     const Request r = request_of<M>(A, b0 + lane, G);
     total += wave_sum_i64((int64_t)r.tiles * r.units);
   }
-  return units_per_piece(total, A.Hkv);
+  return units_per_piece<M>(total, A.Hkv);
 }
 
 // Piece `item` of the batch (without the KV head), item counting the requests' tiles * splits.  The
@@ -116,9 +131,9 @@ __device__ inline Piece find_piece(const ChunkArgs& A, int G, int item) {
     p.L = 1 << 30;
     p.splits = 1;
     if (A.wsO != nullptr) {
-      p.L = units_per_piece((int64_t)r.tiles * r.units, A.Hkv);
-      if (r.units - kCutGain > p.L) p.splits = (r.units + p.L - 1) / p.L;
-      else p.L = 1 << 30;
+      p.L = units_per_piece<M>((int64_t)r.tiles * r.units, A.Hkv);
+      p.splits = splits_of<M>(r.units, p.L);
+      if (p.splits == 1) p.L = 1 << 30;
     }
     if constexpr (ROWS > 0) {
       p.found = p.splits > 1 && item < (r.n * G + ROWS - 1) / ROWS;
@@ -140,7 +155,7 @@ __device__ inline Piece find_piece(const ChunkArgs& A, int G, int item) {
   int64_t before = 0, cut_before = 0;
   for (int b0 = 0; b0 < A.batch; b0 += kWave) {
     const Request r = b0 == 0 ? first : request_of<M>(A, b0 + lane, G);
-    const int splits = whole || r.units - kCutGain <= L ? 1 : (r.units + L - 1) / L;
+    const int splits = whole ? 1 : splits_of<M>(r.units, L);
     const int64_t pieces = (int64_t)r.tiles * splits;
     const int64_t cut = splits > 1 ? pieces : 0;
     int64_t count = pieces;
@@ -584,14 +599,14 @@ __device__ inline float quad_sum(float x) {
 // query c, four k-steps a load, and ends with the scores of query c for the keys 4 g + 0..3 of the
 // 16.  O^T += V^T P^T: k-step r takes the keys 4 g + r; row m of block t is dim m * HD / 16 + t, so
 // that a lane reads HD / 16 consecutive dims of a V row.
-constexpr int kMF = 128;   // fp32 query rows per workgroup
+constexpr int kThreads = 256;
 template <int HD>
 __global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) {
   constexpr int KT = 32;
   constexpr int DPL = HD / 16, J = HD / 16;
   constexpr int ROW = HD + 4;                     // LDS row stride: rows 4 banks apart
   constexpr int CPR = HD / 4;                     // 16-byte chunks of a row
-  constexpr int LD = KT * CPR / kThreads;         // chunks per thread and tile: 2 or 1
+  constexpr int LD = KT * CPR / kThreads;         // chunks per thread and tile: 4 or 2
   __shared__ float s_k[2][KT][ROW], s_v[2][KT][ROW];
 
   const int G = A.Hq / A.Hkv;
@@ -895,18 +910,19 @@ hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
 // tokens over 8K 96 / 106; head_dim 64, prompts of 1024 and 8192 33 / 26, 377 / 319, 512 tokens over 8K
 // 65 / 76, 16 requests of 1 to 1024 tokens over 16K to 1 49 / 47.
 // Bounds of what the device finds.  Tiles: the requests' rows / M, and one more per request.
-// With L >= (sum of tiles * units) * Hkv / kTarget, the cut requests (units > L) have at most
-// kTarget / Hkv tiles between them, and at most twice as many pieces as their tiles * units / L.
+// With L >= (sum of tiles * units) * Hkv / target, the cut requests (units > L) have at most
+// target / Hkv tiles between them, and at most twice as many pieces as their tiles * units / L.
 ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int head_dim, int max_len,
                      int dtype) {
   ChunkPlan p;
+  const Cut C = cut_of(dtype == TAPS_FP32 ? kMF : 256);
   const bool few = (int64_t)rows * Hq <= 32768;   // at most 128 tiles of 256 rows
   p.rows = dtype == TAPS_FP32 ? kMF : (few ? max_len <= 2048 : head_dim == 64) ? 128 : 256;
   const int64_t M = p.rows;
   const int64_t tiles = std::min<int64_t>((int64_t)rows * (Hq / Hkv) / M + batch,
                                           (int64_t)rows * (Hq / Hkv));
-  const bool may_cut = max_len > (kMinUnits + kCutGain) * kUnit;
-  const int64_t cut = std::min<int64_t>(tiles, std::max(1, kTarget / Hkv));
+  const bool may_cut = max_len > (C.min_units + C.gain) * kUnit;
+  const int64_t cut = std::min<int64_t>(tiles, std::max(1, C.target / Hkv));
   // Their groups of rows in the second kernel, by their tiles and by all requests' rows; it takes
   // more than about 1024 of them in turns.  Few rows have many pieces each, which four groups of
   // threads share: us of 16 tokens (32/8 heads) over 32K, 31 pieces, with groups of 4 rows / 16
@@ -915,7 +931,7 @@ ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int head_dim, int max
   const int64_t groups = std::min<int64_t>(cut * (M / p.cut_rows),
                                            (int64_t)rows * (Hq / Hkv) / p.cut_rows + batch);
   p.cut_groups = may_cut ? std::min<int64_t>(groups, std::max(1, 1024 / Hkv)) : 0;
-  p.slots = may_cut ? (int64_t)Hkv * std::max(1, 2 * kTarget / Hkv) : 0;
+  p.slots = may_cut ? (int64_t)Hkv * std::max(1, 2 * C.target / Hkv) : 0;
   p.items = tiles + p.slots / Hkv;
   return p;
 }

@@ -156,9 +156,11 @@ __device__ inline double wave_sum(double v) {
   return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 // 2^k, good to 2^-23: the whole part exactly, the rest by the fp32 instruction
+// (0 for -inf)
 __device__ inline double power(double k) {
+  k = fmax(k, -4000.0);
   const double n = __builtin_rint(k);
-  return __builtin_ldexp((double)__builtin_amdgcn_exp2f((float)(k - n)), (int)fmax(n, -4000.0));
+  return __builtin_ldexp((double)__builtin_amdgcn_exp2f((float)(k - n)), (int)n);
 }
 // ln p of the value v, from the row's maximum and sum
 __device__ inline float log_prob(float v, float M, double Z, double lnz) {

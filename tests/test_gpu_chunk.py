@@ -235,3 +235,49 @@ def test_same_bits_on_streams_and_in_graphs(dtype):
         torch.cuda.synchronize()
         for _, o in graphs:
             assert torch.equal(o, eager)
+
+
+@pytest.mark.parametrize("hd,Hq,Hkv,n", [(128, 20, 4, 1700), (64, 16, 2, 2100)])
+def test_whole_prompts(hd, Hq, Hkv, n):
+    """The tiles of long prompts, their keys not cut."""
+    check(case(16, [(n, n)], Hq, Hkv, hd, 128, BF))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_starts_outside_the_rows_are_clamped(dtype):
+    Q, K, V, table, start, kv, max_len = case(17, [(20, 90), (43, 100)], 4, 2, 128, 32, dtype)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    _, want = call(Q, K, V, table, i32([0, 20, 63]), kv, max_len)
+    _, got = call(Q, K, V, table, i32([-7, 20, 2 ** 31 - 1]), kv, max_len)
+    assert torch.equal(got, want)
+    out = torch.full_like(Q, 7.0)
+    call(Q, K, V, table, i32([2 ** 31 - 1, 5, -(2 ** 31)]), kv, max_len, out=out)
+    assert (out == 7).all()                              # decreasing: no request has a row
+
+
+def test_lengths_past_the_bound_and_pages_outside_the_pool():
+    """kv_len past max_len counts as max_len; page ids are clamped: any values, but no fault."""
+    Q, K, V, table, start, kv, max_len = case(18, [(20, 200), (64, 64)], 4, 2, 128, 32, BF)
+    kv2 = kv.clone()
+    kv2[0] = 2 ** 31 - 1
+    assert torch.equal(call(Q, K, V, table, start, kv2, 200)[1], call(Q, K, V, table, start, kv, 200)[1])
+    wild = torch.where(torch.arange(table.shape[1], device="cuda") % 2 == 0, table, -(2 ** 31))
+    call(Q, K, V, wild.int(), start, kv, max_len)
+    call(Q, K, V, torch.full_like(table, 2 ** 31 - 1), start, kv, max_len)
+    torch.cuda.synchronize()
+
+
+def test_arguments_are_checked():
+    Q, K, V, table, start, kv, max_len = case(19, [(8, 8)], 4, 2, 128, 32, BF)
+    op = taps.PagedChunkAttention(1, 8, 4, 2, 128, max_len, 32)
+    for bad in ((Q.float(), K, V, table, start, kv), (Q.cpu(), K, V, table, start, kv),
+                (Q, K, V, table, start.long(), kv), (Q, K.float(), V, table, start, kv)):
+        with pytest.raises(TypeError):
+            op(*bad)
+    for bad in ((Q[:, :3], K, V, table, start, kv), (Q, K, V[1:], table, start, kv),
+                (Q, K, V, table[0], start, kv), (Q, K, V, table, start[:1], kv),
+                (Q, K, V, table, start, start), (Q.transpose(0, 1), K, V, table, start, kv),
+                (Q, K.transpose(0, 1), V, table, start, kv)):
+        with pytest.raises(ValueError):
+            op(*bad)
+    assert op(Q[:0], K, V, table, start * 0, kv).shape == (0, 4, 128)

@@ -160,3 +160,36 @@ def test_no_requests():
     out = taps.TokenLogProbs(0, 3, 100, top=2)(torch.empty(0, 3, 100, dtype=BF, device="cuda"),
                                               torch.empty(0, 3, dtype=torch.int32, device="cuda"))
     assert [tuple(t.shape) for t in out] == [(0, 3)] * 3 + [(0, 3, 2)] * 2
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_special_values_of_rows_in_parts(dtype):
+    """Few rows of a large vocabulary are cut into parts: parts without values, with infinities, with
+    fewer than `top` values, the token in each of them."""
+    V = 70001
+    x, tok = peaked(31, 13, 1, V, dtype=dtype)
+    x[0, 0, :] = -INF
+    x[1, 0, :] = NAN
+    x[2, 0, 40000] = INF
+    x[3, 0, [5, 69999]] = INF
+    x[4, 0, 100:] = -INF
+    x[5, 0, :-7] = -INF
+    x[6, 0, :35000] = NAN
+    x[7, 0, 30000:] = torch.finfo(dtype).min
+    x[8, 0, :] = NAN
+    x[8, 0, 50000] = -2.0
+    x[9, 0, :] = -3.25                                   # all equal: the first ones
+    x[10, 0, :35000], x[10, 0, 35000:] = -0.0, 0.0
+    x[11, 0, 35000:] = -INF
+    x[11, 0, :35000] = NAN
+    for t in (0, 20000, 40000, 70000, -1):
+        tok.fill_(t)
+        check(x, tok, 20)
+    n = torch.tensor([i % 2 for i in range(13)], dtype=torch.int32, device="cuda")
+    check(x, tok, 3, n)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 31, 64, 65, 128, 129, 257])
+def test_numbers_of_rows_around_the_cut(rows):
+    x, tok = peaked(rows, rows, 1, 50021)
+    check(x, tok, 2)

@@ -178,3 +178,28 @@ def test_streams_and_graph_replays():
         assert torch.equal(out, eager) and torch.equal(again_K, Kp)
         if i == 0:
             assert torch.equal(out, want) and torch.equal(again_K[again_K != 0], wK[again_K != 0])
+
+
+def test_arguments_are_checked():
+    freq, _ = taps.rope_frequencies(128)
+    Q, K, V, pos, slots, Kp, Vp, qw, kw = inputs(3, 8, 4, 2, 128, 32, BF)
+    op = taps.PagedQKRope(4, 2, 128, 32, freq)
+    for bad in ((Q.float(), K, V, pos, slots, Kp, Vp), (Q, K, V, pos.long(), slots, Kp, Vp),
+                (Q, K, V, pos, slots.int(), Kp, Vp), (Q, K, V.cpu(), pos, slots, Kp, Vp)):
+        with pytest.raises(TypeError):
+            op(*bad)
+    for bad in ((Q[:, :3], K, V, pos, slots, Kp, Vp), (Q, K[:7], V, pos, slots, Kp, Vp),
+                (Q, K, V, pos[:7], slots, Kp, Vp), (Q, K, V, pos, slots[1:], Kp, Vp),
+                (Q, K, V, pos, slots, Kp[:, :16], Vp)):
+        with pytest.raises(ValueError):
+            op(*bad)
+    with pytest.raises(ValueError):
+        op(Q, K, V, pos, slots, Kp, Vp, q_norm=qw[:64])
+    with pytest.raises(TypeError):
+        taps.PagedQKRope(4, 2, 128, 32, freq.float())
+    with pytest.raises(taps.TapsError):
+        taps.PagedQKRope(4, 2, 128, 32, freq[:6])(Q, K, V, pos, slots, Kp, Vp)   # 12 dims
+    with pytest.raises(ValueError):
+        taps.rope_frequencies(64, scaling="cubic")
+    with pytest.raises(taps.TapsError):
+        taps.rope_frequencies(63)
