@@ -716,10 +716,11 @@ class PagedQKRope:
             out = K_pages.new_empty((rows, Hq, hd))
         else:
             _need_on(dev, out, "out", tdt, (rows, Hq, hd))
-        st = _lib.Rope(_ptr(self.inv_freq), _ptr(q_norm), _ptr(k_norm), *self.params)
+        st = _lib.Rope(self.inv_freq.data_ptr(), _ptr(q_norm), _ptr(k_norm), *self.params)
         _lib.check(self.lib, "qk_rope_paged", self.lib.qk_rope_paged(
-            _ptr(Q), _ptr(K), _ptr(V), qs, ks, vs, _ptr(positions), _ptr(slot_map), rows, Hq,
-            Hkv, hd, dtype, ctypes.byref(st), _ptr(out), _ptr(K_pages), _ptr(V_pages),
+            Q.data_ptr(), K.data_ptr(), V.data_ptr(), qs, ks, vs, positions.data_ptr(),
+            slot_map.data_ptr(), rows, Hq, Hkv, hd, dtype, ctypes.byref(st), out.data_ptr(),
+            K_pages.data_ptr(), V_pages.data_ptr(),
             K_pages.shape[0], page_rows, _stream()))
         return out
 
@@ -777,9 +778,9 @@ class PagedChunkAttention:
         nbytes = self._ws_bytes(rows)
         ws = K_pages.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
         _lib.check(self.lib, "chunk_attn_paged", self.lib.chunk_attn_paged(
-            _ptr(Q), qs, _ptr(K_pages), _ptr(V_pages), K_pages.shape[0], page_rows,
-            _ptr(block_table), block_table.shape[1], _ptr(q_start), _ptr(kv_len), batch, rows, Hq,
-            Hkv, hd, self.max_len, self.window, dtype, self.scale, _ptr(O), _ptr(ws), nbytes,
+            Q.data_ptr(), qs, K_pages.data_ptr(), V_pages.data_ptr(), K_pages.shape[0], page_rows,
+            block_table.data_ptr(), block_table.shape[1], q_start.data_ptr(), kv_len.data_ptr(),
+            batch, rows, Hq, Hkv, hd, self.max_len, self.window, dtype, self.scale, O.data_ptr(), _ptr(ws), nbytes,
             _stream()))
         return O
 
@@ -807,18 +808,13 @@ class TokenLogProbs:
         _need_on(dev, tokens, "tokens", torch.int32, (batch, budget))
         if n_nodes is not None:
             _need_on(dev, n_nodes, "n_nodes", torch.int32, (batch,))
-        # one allocation for all five, 4 bytes a value
-        n = batch * budget
-        buf = tokens.new_empty((3 + 2 * top) * n)
-        rank, top_idx, fl = buf.split_with_sizes((n, top * n, (2 + top) * n))
-        fl = fl.view(torch.float32)
-        logprob, entropy, top_lp = fl.split_with_sizes((n, n, top * n))
-        at = buf.data_ptr()
+        logprob = torch.empty_like(tokens, dtype=torch.float32)
+        entropy, rank = torch.empty_like(logprob), torch.empty_like(tokens)
+        top_idx = tokens.new_empty((batch, budget, top))
+        top_logprob = logprob.new_empty((batch, budget, top))
         ws = tokens.new_empty(self.ws_bytes, dtype=torch.uint8) if self.ws_bytes else None
         _lib.check(self.lib, "taps_logprobs", self.lib.taps_logprobs(
-            _ptr(logits), stride, batch, budget, vocab, dtype, _ptr(n_nodes), _ptr(tokens), top,
-            at + 4 * (1 + top) * n, at + 4 * (2 + top) * n, at, at + 4 * n,
-            at + 4 * (3 + top) * n, _ptr(ws), self.ws_bytes, _stream()))
-        return (logprob.view(batch, budget), entropy.view(batch, budget),
-                rank.view(batch, budget), top_idx.view(batch, budget, top),
-                top_lp.view(batch, budget, top))
+            logits.data_ptr(), stride, batch, budget, vocab, dtype, _ptr(n_nodes),
+            tokens.data_ptr(), top, logprob.data_ptr(), entropy.data_ptr(), rank.data_ptr(),
+            top_idx.data_ptr(), top_logprob.data_ptr(), _ptr(ws), self.ws_bytes, _stream()))
+        return logprob, entropy, rank, top_idx, top_logprob
