@@ -510,9 +510,6 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
   };
 
   if (nt > 0) {
-    // In whole turns of the rings, so that the loop has one exit (with three, the accumulators
-    // moved between registers and did not all fit); keys past the piece are masked.
-    const int steps = (nt + 2) / 3 * 3;
     // K(0) .. K(2), V(0), V(1)
     prepare(0);
     issue(0);
@@ -532,7 +529,7 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
     }
     TAPS_LDS_BARRIER();                           // ... and every other wave's
     if (wrow0 > last) {                           // no rows: the wave only loads
-      for (int t = 0, P = 0; t < steps; ++t, P = P == 2 ? 0 : P + 1) {
+      for (int t = 0, P = 0; t < nt; ++t, P = P == 2 ? 0 : P + 1) {
         advance();
         fill(P);
         prepare(t + 1 + ahead);
@@ -544,10 +541,10 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
       scores(0, 0, 0, NKK, a);
       scores(0, 1, 0, NKK, b);
       m0 = largest(a);
-      for (int t = 0; t < steps; t += 3) {
+      for (int t = 0; t < nt; t += 3) {   // (one exit: with three the accumulators moved about)
         step(Slot<0>(), t, a, b, c);
-        step(Slot<1>(), t + 1, c, a, b);
-        step(Slot<2>(), t + 2, b, c, a);
+        if (t + 1 < nt) step(Slot<1>(), t + 1, c, a, b);
+        if (t + 2 < nt) step(Slot<2>(), t + 2, b, c, a);
       }
     }
     TAPS_WAIT_VMCNT(0);   // (empty) loads past the piece land before the LDS is released
