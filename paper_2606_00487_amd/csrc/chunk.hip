@@ -5,20 +5,31 @@
 // O[i,h] = softmax_j(scale * q_ih . k_jg) v_jg.  The query rows of a KV head are the tokens x the
 // G query heads that share it, in tiles of M rows; keys go by in tiles of 64.
 //
-// Pieces.  A workgroup takes the keys of one (KV head, query tile), or a part of them: no piece
-// has more than L key tiles, L = all tiles' keys / 256 (fp32: 512), so that a few long requests fill the chip
-// as well as many short ones.  The requests' lengths are device data: every workgroup forms L
-// and finds its piece from prefix sums over the batch.  Pieces of a tile that was cut leave
-// (O, max, sum) in fp32, which a second kernel adds.
+// Pieces.  A workgroup takes the keys of one (KV head, query tile), or a part of them: no piece of
+// a tile that is cut has more than L units of 64 keys, L = all tiles' units / 256 (or 512), so that
+// a few long requests fill the chip as well as many short ones.  The requests' lengths are device
+// data: every workgroup forms L and finds its piece from prefix sums over the batch.  Pieces of a
+// tile that was cut leave (O, max, sum) in fp32, which a second kernel adds.
 //
-// bf16 (v_mfma_f32_32x32x16_bf16): eight waves of 32 query rows each share the key tile.
-// S^T = K Q^T (A: keys from LDS, B: queries in registers) leaves a query's scores in two lanes;
-// they go, as P^T, straight into the B operand of O^T += V^T P^T, whose key order follows the
-// accumulators; the transposing LDS read takes V in that order.  K and V cycle through rings of
-// three tiles, filled by loads straight into LDS two tiles ahead; S of the next tile is issued
-// between this one's softmax and products.
+// bf16 (v_mfma_f32_32x32x16_bf16): eight waves (short prompts and head_dim 64: four) of 32 query
+// rows each share the key tile.  S^T = K Q^T (A: keys from LDS, B: queries in registers) leaves a
+// query's scores in two lanes; they go, as P^T, straight into the B operand of O^T += V^T P^T,
+// whose key order follows the accumulators; the transposing LDS read takes V in that order.  K and
+// V cycle through rings of three tiles, filled by loads straight into LDS two tiles ahead; S of the
+// next tile is issued between this one's softmax and products, each matrix instruction among the
+// vector and LDS instructions of the other part.
+// Bound: the matrix instructions (4 head_dim flops a visible pair and head) and, for few rows over
+// a long cache, HBM.  head_dim 128, 32/8 heads: a prompt of 16,384 tokens takes 1.88 ms, 1167
+// TFLOP/s (a library product of 8192^3: 1219).  A step of 64 keys takes 3500 cycles of which the
+// SIMD's matrix instructions fill 2048, at the clock of 1.86 GHz that the card holds under it; the
+// library's product keeps them busier at 1.5 GHz, to the same product of the two.  16 tokens over
+// 32,768 keys: 33 us, 4.1 TB/s with the join.  A piece costs 5.4 us besides its steps (finding it
+// 1.0, its pages 1.4, the first tile 1.3, the first scores 0.4, its end 1.1), which bounds ragged
+// batches; at head_dim 64 the exponentials take longer than the products.
 // fp32 (v_mfma_f32_16x16x4_f32): four waves of 16 query rows, key tiles of 32 staged through
-// registers.
+// registers, bound by the fp32 matrix instructions: a prompt of 2048 tokens, 32/8 heads of 128, 380
+// us, 90 TFLOP/s (a library product: 145).  128 rows a tile take 352 us there, and 41 for 47 us for
+// 16 tokens over 8K, but 254 for 225 us for 8 ragged requests.
 #include <algorithm>
 
 #include "common.h"
@@ -36,17 +47,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kUnit = 64;      // keys per unit of a piece's length
 
-// Query rows of a tile: 128 or 256 in bf16, 64 in fp32.  A cut: into pieces of 1 / target of all
-// tiles' units, none shorter than min_units (mostly start and end), and only where it saves more
-// than `gain` units of a tile's time (the second kernel costs as much).  An fp32 unit takes as long
-// as four in bf16.
-constexpr int kMF = 64;
-struct Cut {
-  int target, min_units, gain;
-};
-__host__ __device__ constexpr Cut cut_of(int M) {
-  return M == kMF ? Cut{512, 2, 1} : Cut{256, 4, 6};
-}
+constexpr int kMF = 64;        // query rows of an fp32 tile; 128 or 256 in bf16
 
 struct ChunkArgs {
   const unsigned char *Q, *K, *V;
@@ -55,6 +56,7 @@ struct ChunkArgs {
   const int32_t *q_start, *kv_len;
   int batch, rows, Hq, Hkv, max_len, window;
   float scale_log2;
+  ChunkCut cut;
   unsigned char* O;
   float* wsO;     // [slots][M][HD]; null: no piece is cut
   float2* wsML;   // [slots][M]
@@ -89,16 +91,13 @@ __device__ inline int64_t wave_sum_i64(int64_t v) {
 
 // Key units per piece at most: the sum of tiles * units over the batch, times the KV heads, in
 // `target` parts
-template <int M>
-__device__ inline int units_per_piece(int64_t total, int Hkv) {
-  constexpr Cut C = cut_of(M);
-  const int64_t L = (total * Hkv + C.target - 1) / C.target;
-  return (int)max((int64_t)C.min_units, min(L, (int64_t)1 << 30));
+__device__ inline int units_per_piece(const ChunkArgs& A, int64_t total) {
+  const int64_t L = (total * A.Hkv + (1 << A.cut.target_log2) - 1) >> A.cut.target_log2;
+  return (int)max((int64_t)A.cut.min_units, min(L, (int64_t)1 << 30));
 }
 // ... and the pieces of a tile of the request
-template <int M>
-__device__ inline int splits_of(int units, int L) {
-  return units - cut_of(M).gain > L ? (units + L - 1) / L : 1;
+__device__ inline int splits_of(const ChunkArgs& A, int units, int L) {
+  return units - A.cut.gain > L ? (units + L - 1) / L : 1;
 }
 template <int M>
 __device__ inline int piece_units(const ChunkArgs& A, int G, const Request& first) {
@@ -108,7 +107,7 @@ __device__ inline int piece_units(const ChunkArgs& A, int G, const Request& firs
     const Request r = request_of<M>(A, b0 + lane, G);
     total += wave_sum_i64((int64_t)r.tiles * r.units);
   }
-  return units_per_piece<M>(total, A.Hkv);
+  return units_per_piece(A, total);
 }
 
 // Piece `item` of the batch (without the KV head), item counting the requests' tiles * splits.  The
@@ -131,8 +130,8 @@ __device__ inline Piece find_piece(const ChunkArgs& A, int G, int item) {
     p.L = 1 << 30;
     p.splits = 1;
     if (A.wsO != nullptr) {
-      p.L = units_per_piece<M>((int64_t)r.tiles * r.units, A.Hkv);
-      p.splits = splits_of<M>(r.units, p.L);
+      p.L = units_per_piece(A, (int64_t)r.tiles * r.units);
+      p.splits = splits_of(A, r.units, p.L);
       if (p.splits == 1) p.L = 1 << 30;
     }
     if constexpr (ROWS > 0) {
@@ -155,7 +154,7 @@ __device__ inline Piece find_piece(const ChunkArgs& A, int G, int item) {
   int64_t before = 0, cut_before = 0;
   for (int b0 = 0; b0 < A.batch; b0 += kWave) {
     const Request r = b0 == 0 ? first : request_of<M>(A, b0 + lane, G);
-    const int splits = whole ? 1 : splits_of<M>(r.units, L);
+    const int splits = whole ? 1 : splits_of(A, r.units, L);
     const int64_t pieces = (int64_t)r.tiles * splits;
     const int64_t cut = splits > 1 ? pieces : 0;
     int64_t count = pieces;
@@ -287,9 +286,9 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
 
   bf16x8 q[NKK];   // the lane's query: dims 16 kk + 8 hl ..
 
-  // ---- direct loads.  The first half of the waves loads K, the second V; of each tile one half (32
-  // keys, in one page) per HW / 2 waves, BPW blocks of 1 KB each.  Lane l holds the page of this
-  // wave's half of tile pw + l.
+  // ---- direct loads.  The first half of the waves loads K, the second V; of each tile one half
+  // (32 keys, in one page) per HW / 2 waves, BPW blocks of 1 KB each.  Lane l holds the page of
+  // this wave's half of tile pw + l.
   const uint32_t rsb = (uint32_t)A.Hkv * ROWB;
   const bool loads_k = wave < HW;
   const int half = wave % HW / (HW / 2), block0 = wave % (HW / 2) * BPW;
@@ -771,8 +770,10 @@ __global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) 
           f32x4{o[d][r], o[d + 1][r], o[d + 2][r], o[d + 3][r]} * inv;
 }
 
-// Adds the pieces of the tiles that were cut: ROWS query rows of a (KV head, request that is cut) at a
-// time; 16 threads a row, and GROUPS of them share its pieces, kAhead of which load together.
+// Adds the pieces of the tiles that were cut: ROWS query rows of a (KV head, request that is cut)
+// at a time; 16 threads a row, and GROUPS of them share its pieces, kAhead of which load together.
+// Bound: the pieces' bytes (512 tokens over 8K, 32/8 heads of 128: 33 MB in 9 us) or, for few rows,
+// latency (5 us).
 constexpr int kCombineThreads = 256, kAhead = 8;
 __device__ inline void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
 __device__ inline void store4(__bf16* p, const f32x4& x) {
@@ -893,42 +894,54 @@ hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 0) return e;
   if constexpr (sizeof(T) == 2)
-    return p.rows == 256 ? launch_combine<T, HD, 256>(A, p, s) : launch_combine<T, HD, 128>(A, p, s);
+    return p.rows == 256 ? launch_combine<T, HD, 256>(A, p, s)
+                         : launch_combine<T, HD, 128>(A, p, s);
   else
     return launch_combine<T, HD, kMF>(A, p, s);
 }
 
 }  // namespace
 
-// Tiles of 256 query rows use each key tile in LDS twice as often as those of 128; 128 spread a short
-// prompt over more CUs, and at head_dim 64, where the exponentials bound the kernel, three
-// workgroups of them share a CU.  us a call with 256 / 128 (32/8 heads): head_dim 128, prompts of 64,
-// 256, 1024, 2048 and 4096 tokens 15.9 / 12.5, 20.3 / 16.0, 42.9 / 34.6, 67 / 67, 158 / 211; 512
-// tokens over 8K 96 / 106; head_dim 64, prompts of 1024 and 8192 33 / 26, 377 / 319, 512 tokens over 8K
-// 65 / 76, 16 requests of 1 to 1024 tokens over 16K to 1 49 / 47.
+// Tiles of 256 query rows use each key tile in LDS twice as often as those of 128; 128 spread a
+// short prompt over more CUs, and at head_dim 64, where the exponentials bound the kernel, three
+// workgroups of them share a CU.  us a call with 256 / 128 rows (32/8 heads): head_dim 128, prompts
+// of 600, 1024, 1536, 2048, 2560 and 4096 tokens 24 / 19, 40 / 27, 52 / 41, 67 / 61, 80 / 90 and
+// 145 / 182; 512 tokens over 8K 92 / 105, 8 prompts of 100 to 1000 47 / 50; head_dim 64, prompts of
+// 1024 and 2048 29 / 20 and 47 / 39, 16 requests of 1 to 1024 tokens over 16K to 1 47 / 39, 512
+// over 8K 60 / 63.
+// Cuts.  Pieces: one per CU (three share one at head_dim 64: 16 requests of 1 to 1024 tokens take
+// 39 us with 512 for 44 with 256; fp32: 512).  min_units: mostly a piece's start and end.  gain:
+// what the second kernel costs; an fp32 unit takes as long as four in bf16.  Where 64 tiles or more
+// take part the pieces may be longer, and where max_len then lets none be cut the second kernel is
+// not launched: a prompt of 1024 takes 27 us with 8 and 30 with 4, 16 tokens over 900 keys 21 and
+// 15.
 // Bounds of what the device finds.  Tiles: the requests' rows / M, and one more per request.
 // With L >= (sum of tiles * units) * Hkv / target, the cut requests (units > L) have at most
 // target / Hkv tiles between them, and at most twice as many pieces as their tiles * units / L.
 ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int head_dim, int max_len,
                      int dtype) {
   ChunkPlan p;
-  const Cut C = cut_of(dtype == TAPS_FP32 ? kMF : 256);
-  const bool few = (int64_t)rows * Hq <= 32768;   // at most 128 tiles of 256 rows
-  p.rows = dtype == TAPS_FP32 ? kMF : (few ? max_len <= 2048 : head_dim == 64) ? 128 : 256;
-  const int64_t M = p.rows;
+  const int64_t heads = (int64_t)rows * Hq;       // query rows of all heads
+  p.rows = dtype == TAPS_FP32 ? kMF
+           : head_dim == 64 || (heads <= 65536 && max_len <= 2048) ? 128 : 256;
+  p.cut = p.rows == kMF ? ChunkCut{9, 2, 1}
+          : p.rows == 256
+              ? ChunkCut{8, 4, 6}
+              : ChunkCut{head_dim == 64 ? 9 : 8, heads > 8192 ? 8 : 4, 8};
+  const int64_t M = p.rows, target = (int64_t)1 << p.cut.target_log2;
   const int64_t tiles = std::min<int64_t>((int64_t)rows * (Hq / Hkv) / M + batch,
                                           (int64_t)rows * (Hq / Hkv));
-  const bool may_cut = max_len > (C.min_units + C.gain) * kUnit;
-  const int64_t cut = std::min<int64_t>(tiles, std::max(1, C.target / Hkv));
+  const bool may_cut = max_len > (p.cut.min_units + p.cut.gain) * kUnit;
+  const int64_t cut = std::min<int64_t>(tiles, std::max<int64_t>(1, target / Hkv));
   // Their groups of rows in the second kernel, by their tiles and by all requests' rows; it takes
   // more than about 1024 of them in turns.  Few rows have many pieces each, which four groups of
   // threads share: us of 16 tokens (32/8 heads) over 32K, 31 pieces, with groups of 4 rows / 16
   // 5.7 / 10.4; of 512 tokens over 8K, 4 pieces, 28 / 9.3.
-  p.cut_rows = (int64_t)rows * Hq <= 4096 ? 4 : 16;
+  p.cut_rows = heads <= 4096 ? 4 : 16;
   const int64_t groups = std::min<int64_t>(cut * (M / p.cut_rows),
                                            (int64_t)rows * (Hq / Hkv) / p.cut_rows + batch);
   p.cut_groups = may_cut ? std::min<int64_t>(groups, std::max(1, 1024 / Hkv)) : 0;
-  p.slots = may_cut ? (int64_t)Hkv * std::max(1, 2 * C.target / Hkv) : 0;
+  p.slots = may_cut ? (int64_t)Hkv * std::max<int64_t>(1, 2 * target / Hkv) : 0;
   p.items = tiles + p.slots / Hkv;
   return p;
 }
@@ -948,6 +961,7 @@ hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const vo
   A.q_stride = q_stride, A.pk = pk, A.q_start = q_start, A.kv_len = kv_len;
   A.batch = batch, A.rows = rows, A.Hq = Hq, A.Hkv = Hkv, A.max_len = max_len, A.window = window;
   A.scale_log2 = scale * 1.4426950408889634f;
+  A.cut = p.cut;
   A.O = (unsigned char*)O;
   A.slots = (int)p.slots;
   A.wsO = p.slots ? (float*)ws : nullptr;

@@ -185,11 +185,17 @@ hipError_t launch_rope(const void* Q, const void* K, const void* V, int64_t q_st
                        const taps_rope& r, void* Qo, void* Kp, void* Vp, int64_t pool_rows,
                        hipStream_t s);
 
-// Chunks of new tokens over a paged cache: query tiles, cut along the keys where few
+// Chunks of new tokens over a paged cache: query tiles, cut along the keys where few.  A cut: into
+// pieces of 1 / 2^target_log2 of all tiles' key units, none shorter than min_units, and only where
+// it saves more than `gain` units of a tile's time.
+struct ChunkCut {
+  int target_log2, min_units, gain;
+};
 struct ChunkPlan {
   int rows;            // query rows of a tile
+  ChunkCut cut;
   int64_t items;       // most pieces per KV head
-  int64_t cut_groups;  // most groups of rows per KV head of requests that are cut (0: none ever is)
+  int64_t cut_groups;  // groups of rows per KV head of requests that are cut (0: none ever is)
   int cut_rows;        // rows of such a group: 16, or 4
   int64_t slots;       // most pieces of cut tiles, all KV heads
 };

