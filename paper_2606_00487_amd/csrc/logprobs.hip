@@ -394,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
 #pragma unroll
     for (int w = 0; w < NW; ++w) Zd += s_z[w], Sd += s_s[w];
   }
-  const double lnz = log(Zd);
+  const double lnz = A.parts == 1 ? log(Zd) : 0.0;   // (parts: the second kernel takes it)
   auto lp = [&](float v) { return log_prob(v, M, Zd, lnz); };
   auto found = [&](int r, uint64_t key) {   // the row's (part's) r-th value
     if (A.parts > 1) {
