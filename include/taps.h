@@ -606,8 +606,8 @@ typedef struct {
  * page_rows), such as the -1 of kv_reserve_paged, leave them out (the query is written all the
  * same).  No other row of the pools is written.
  *   Q, K, V    [rows][Hq or Hkv][head_dim], consecutive rows q_stride, k_stride and v_stride
- *              elements apart (at least a row, a multiple of 16 bytes): slices of a fused
- *              projection's rows need no copy
+ *              elements apart (at least a row, at most 2^30, a multiple of 16 bytes): slices of a
+ *              fused projection's rows need no copy
  *   positions  [rows] int32
  *   slot_map   [rows] int64; a slot must not be named twice (its row would be a mix)
  *   Q_out      [rows][Hq][head_dim]; it and the pools share no memory with Q, K, V or each other
@@ -639,9 +639,10 @@ size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq,
  * window only p - window < j <= p.  O[i,h] = softmax_j(scale * Q[i,h] . K[j,g]) V[j,g], g = h /
  * (Hq / Hkv); zeros for a token that sees no row (kv_len[b] < n).
  *   Q            [rows][Hq][head_dim], consecutive rows q_stride elements apart (at least
- *                Hq * head_dim, a multiple of 16 bytes)
+ *                Hq * head_dim, at most 2^30, a multiple of 16 bytes)
  *   K_pages, V_pages, num_pages, page_rows, block_table, max_pages  as for
- *                tree_verify_attn_paged, in dtype; max_pages * page_rows at least max_len.  Block
+ *                tree_verify_attn_paged, in dtype; max_pages * page_rows at least max_len.  Pages
+ *                may be in several requests' tables (a common beginning).  Block
  *                table entries of pages that no token of the request sees (before the window, past
  *                kv_len) may hold anything
  *   q_start      [batch + 1] int32, not decreasing, within [0, rows] (clamped to it).  Rows of O
@@ -656,7 +657,8 @@ size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq,
  *   dtype        TAPS_BF16 (fp32 accumulation, weights rounded to bf16 for the second product,
  *                output rounded to nearest even) or TAPS_FP32
  *   scale        softmax scale, finite and > 0
- *   O            [rows][Hq][head_dim] in dtype, 16-byte aligned; not in Q's memory (checked)
+ *   O            [rows][Hq][head_dim] in dtype, 16-byte aligned; not in the memory of Q or of the
+ *                pools (checked)
  *   ws           chunk_attn_paged_workspace_bytes(...) bytes, 16-byte aligned */
 taps_status chunk_attn_paged(const void *Q, int64_t q_stride, const void *K_pages,
                              const void *V_pages, int32_t num_pages, int32_t page_rows,
@@ -679,7 +681,8 @@ size_t taps_logprobs_workspace_bytes(int32_t batch, int32_t budget, int32_t voca
 
 /* Log probabilities of given tokens under each logits row (a prompt's next tokens, sampled or
  * drafted ones), with their ranks, the row's entropy and its top alternatives.
- *   logits       [batch][budget][vocab] as for taps_sample (row_stride, alignment, dtype)
+ *   logits       [batch][budget][vocab] as for taps_sample (row_stride, alignment, dtype, limits of
+ *                the sizes: a prompt of more than TAPS_MAX_BUDGET positions is several requests)
  *   n_nodes      [batch] int32 rows per request, or NULL (all): rows i >= n_nodes[b] get 0, rank
  *                and index -1, their logits and tokens are not read
  *   tokens       [batch][budget] int32.  Outside [0, vocab), such as the -1 of padding: log
@@ -691,6 +694,7 @@ size_t taps_logprobs_workspace_bytes(int32_t batch, int32_t budget, int32_t voca
  *   top_idx      [batch][budget][top] int32, the first `top` tokens of the rank order
  *   top_logprob  [batch][budget][top] float, theirs.  (Both may be NULL where top is 0)
  *   ws           taps_logprobs_workspace_bytes(...) bytes, 16-byte aligned
+ * The outputs share no memory with the inputs or each other.
  * p_j = w_j / sum w, w_j = exp(x_j - x_0) for the largest value x_0: 1 where x_j equals x_0
  * (infinite values too), 0 for NaN, as in taps_sample at T = 1.  The rank order is value
  * descending, then index ascending; -0 equals +0; NaN is last.  A row of NaN alone has log

@@ -661,7 +661,8 @@ def rope_frequencies(rot_dim, theta=1e6, scaling="none", factor=1.0, trained_len
     (float64 tensor) and the factor of cosines and sines.  scaling: "none", "linear", "ntk" or
     "yarn" (positions up to `factor` times the trained length; see include/taps.h)."""
     if scaling not in _lib.ROPE_SCALINGS:
-        raise ValueError(f"scaling: expected one of {', '.join(_lib.ROPE_SCALINGS)}, got {scaling!r}")
+        raise ValueError(
+            f"scaling: expected one of {', '.join(_lib.ROPE_SCALINGS)}, got {scaling!r}")
     lib = load()
     freq, mscale = (ctypes.c_double * max(1, int(rot_dim) // 2))(), ctypes.c_float()
     _lib.check(lib, "taps_rope_frequencies", lib.taps_rope_frequencies(
@@ -780,8 +781,8 @@ class PagedChunkAttention:
         _lib.check(self.lib, "chunk_attn_paged", self.lib.chunk_attn_paged(
             Q.data_ptr(), qs, K_pages.data_ptr(), V_pages.data_ptr(), K_pages.shape[0], page_rows,
             block_table.data_ptr(), block_table.shape[1], q_start.data_ptr(), kv_len.data_ptr(),
-            batch, rows, Hq, Hkv, hd, self.max_len, self.window, dtype, self.scale, O.data_ptr(), _ptr(ws), nbytes,
-            _stream()))
+            batch, rows, Hq, Hkv, hd, self.max_len, self.window, dtype, self.scale, O.data_ptr(),
+            _ptr(ws), nbytes, _stream()))
         return O
 
 
@@ -790,7 +791,8 @@ class TokenLogProbs:
     alternatives."""
 
     def __init__(self, batch, budget, vocab, top=0, dtype=BF16):
-        """budget: rows per request (positions of a prompt, nodes of a tree; 1 in decoding)."""
+        """budget: rows per request (positions of a prompt, up to 512, nodes of a tree; 1 in
+        decoding or for rows that are each their own request)."""
         self.lib = load()
         self.shape = (batch, budget, vocab, top, dtype)
         _lib.check(self.lib, "taps_logprobs_validate", self.lib.taps_logprobs_validate(

@@ -675,7 +675,8 @@ taps_status taps_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling
     double f = std::pow(theta, -2.0 * j / rot_dim);
     if (scaling == TAPS_ROPE_LINEAR) f /= factor;
     if (scaling == TAPS_ROPE_YARN) {
-      const double g = std::min(1.0, std::max(0.0, ((double)trained_len * f / two_pi - 1.0) / 31.0));
+      const double turns = (double)trained_len * f / two_pi;
+      const double g = std::min(1.0, std::max(0.0, (turns - 1.0) / 31.0));
       f = g * f + (1.0 - g) * (f / factor);
     }
     inv_freq[j] = f;
@@ -716,7 +717,7 @@ taps_status qk_rope_paged(const void* Q, const void* K, const void* V, int64_t q
   const int es = dtype == TAPS_BF16 ? 2 : 4;
   const int64_t qrow = (int64_t)Hq * head_dim, krow = (int64_t)Hkv * head_dim;
   if (q_stride < qrow || k_stride < krow || v_stride < krow) return TAPS_ERR_INVALID_ARG;
-  const int64_t most = (int64_t)1 << 31;
+  const int64_t most = (int64_t)1 << 30;   // (byte spans stay below 2^63)
   if (q_stride > most || k_stride > most || v_stride > most) return TAPS_ERR_UNSUPPORTED;
   if (((q_stride | k_stride | v_stride) * es & 15) != 0) return TAPS_ERR_INVALID_ARG;
   if (rows == 0) return TAPS_OK;
@@ -795,7 +796,7 @@ taps_status chunk_attn_paged(const void* Q, int64_t q_stride, const void* K_page
   const int es = dtype == TAPS_BF16 ? 2 : 4;
   const int64_t row = (int64_t)Hq * head_dim;
   if (q_stride < row || (q_stride * es & 15) != 0) return TAPS_ERR_INVALID_ARG;
-  if (q_stride > (int64_t)1 << 31) return TAPS_ERR_UNSUPPORTED;
+  if (q_stride > (int64_t)1 << 30) return TAPS_ERR_UNSUPPORTED;
   if (batch == 0 || rows == 0) return TAPS_OK;
   if (!Q || !K_pages || !V_pages || !block_table || !q_start || !kv_len || !O)
     return TAPS_ERR_INVALID_ARG;
@@ -803,7 +804,10 @@ taps_status chunk_attn_paged(const void* Q, int64_t q_stride, const void* K_page
   if ((a16 & 15) != 0 ||
       (((uintptr_t)block_table | (uintptr_t)q_start | (uintptr_t)kv_len) & 3) != 0)
     return TAPS_ERR_INVALID_ARG;
-  if (overlap(O, span(rows, row, row, es), Q, span(rows, q_stride, row, es)))
+  const int64_t out = span(rows, row, row, es);
+  const int64_t pool = (int64_t)num_pages * page_rows * Hkv * head_dim * es;
+  if (overlap(O, out, Q, span(rows, q_stride, row, es)) || overlap(O, out, K_pages, pool) ||
+      overlap(O, out, V_pages, pool))
     return TAPS_ERR_INVALID_ARG;
   const ChunkPlan p = plan_chunk(batch, rows, Hq, Hkv, head_dim, max_len, dtype);
   const size_t need = chunk_ws_bytes(p, head_dim);

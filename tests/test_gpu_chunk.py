@@ -281,3 +281,93 @@ def test_arguments_are_checked():
         with pytest.raises(ValueError):
             op(*bad)
     assert op(Q[:0], K, V, table, start * 0, kv).shape == (0, 4, 128)
+
+
+def wider(inp, max_len):
+    """The same requests under a larger bound of their lengths; the table's new entries are junk."""
+    Q, K, V, table, start, kv, _ = inp
+    more = -(-max_len // K.shape[1]) - table.shape[1]
+    junk = torch.full((table.shape[0], max(more, 0)), -9, dtype=torch.int32, device="cuda")
+    return Q, K, V, torch.cat([table, junk], 1).contiguous(), start, kv, max_len
+
+
+@pytest.mark.parametrize("Hq,Hkv,n,bound_of_len", [(40, 8, 1638, 2048), (40, 8, 1639, 2048),
+                                                   (8, 2, 600, 2048), (8, 2, 600, 2049)])
+def test_prompts_at_the_borders_of_the_tile_sizes(Hq, Hkv, n, bound_of_len):
+    check(wider(case(20, [(n, n)], Hq, Hkv, 128, 64, BF), bound_of_len))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n,kv", [(256, 768), (256, 769), (256, 1030), (257, 1024), (257, 1025),
+                                  (257, 1500)])
+def test_few_and_many_tiles_at_the_borders_of_a_cut(hd, n, kv):
+    """8192 and 8224 query rows of all heads; caches that are just not, or just, cut."""
+    check(case(21, [(n, kv)], 32, 8, hd, 64, BF))
+
+
+def test_ragged_batch_in_many_pieces_of_heads_of_64():
+    check(case(22, [(300, 4000), (1, 9000), (900, 900), (0, 50), (17, 3000)], 8, 2, 64, 64, BF))
+    check(case(23, [(300, 4000), (1, 9000), (900, 900), (0, 50), (17, 3000)], 40, 20, 64, 64, BF))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_scratch_that_holds_nan(dtype, hd):
+    """Every part that the second kernel adds was written by the first."""
+    Q, K, V, table, start, kv, max_len = case(24, [(40, 5000), (300, 2000), (2, 90), (0, 4000)], 6,
+                                              2, hd, 64, dtype)
+    op, want = call(Q, K, V, table, start, kv, max_len)
+    n = op._ws_bytes(Q.shape[0])
+    assert n > 0
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    O = torch.full_like(want, 7.0)
+    st = op.lib.chunk_attn_paged(
+        Q.data_ptr(), Q.stride(0), K.data_ptr(), V.data_ptr(), K.shape[0], 64, table.data_ptr(),
+        table.shape[1], start.data_ptr(), kv.data_ptr(), len(kv), Q.shape[0], 6, 2, hd, max_len, 0,
+        taps.BF16 if dtype == BF else taps.FP32, op.scale, O.data_ptr(), ws.data_ptr(), n,
+        torch.cuda.current_stream().cuda_stream)
+    assert st == 0 and torch.equal(O, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_values_that_are_not_finite_stay_in_their_request(dtype):
+    Q, K, V, table, start, kv, max_len = case(25, [(20, 900), (64, 64), (3, 2000), (100, 100)], 4, 2,
+                                              128, 32, dtype)
+    _, want = call(Q, K, V, table, start, kv, max_len)
+    V[table[0, 3].long(), 5, 1, 7] = float("nan")
+    V[table[0, 4].long(), 9, 0] = float("inf")
+    K[table[2, 0].long(), 3, 0] = float("nan")
+    K[table[2, 30].long(), 3, 1] = float("-inf")
+    _, got = call(Q, K, V, table, start, kv, max_len)
+    assert torch.equal(got[20:84], want[20:84]) and torch.equal(got[87:], want[87:])
+    assert torch.isnan(got[:20, 2:, 7]).all() and not torch.isfinite(got[:20, :2]).any()
+    assert torch.isnan(got[84:87, :2]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_queries_that_are_not_finite_stay_in_their_row(dtype):
+    Q, K, V, table, start, kv, max_len = case(26, [(20, 900), (64, 64)], 4, 2, 64, 32, dtype)
+    _, want = call(Q, K, V, table, start, kv, max_len)
+    Q[3, 1, 5], Q[40, 2] = float("nan"), float("inf")
+    _, got = call(Q, K, V, table, start, kv, max_len)
+    other = torch.ones(84, 4, dtype=torch.bool, device="cuda")
+    other[3, 1] = other[40, 2] = False
+    assert torch.equal(got[other], want[other]) and torch.isnan(got[3, 1]).all()
+
+
+def test_requests_with_a_common_beginning():
+    """Pages in several tables: the same as copies of them."""
+    Q, K, V, table, start, kv, max_len = case(27, [(30, 400), (70, 300)], 4, 2, 128, 32, BF)
+    table[1, :6] = table[0, :6]
+    _, shared = check((Q, K, V, table, start, kv, max_len))
+    K2, V2 = torch.cat([K, K[table[0, :6].long()]]), torch.cat([V, V[table[0, :6].long()]])
+    table[1, :6] = torch.arange(K.shape[0], K.shape[0] + 6, device="cuda")
+    _, copied = call(Q, K2, V2, table, start, kv, max_len)
+    assert torch.equal(shared, copied)
+
+
+def test_refuses_output_in_the_pools():
+    Q, K, V, table, start, kv, max_len = case(28, [(8, 8)], 4, 2, 128, 32, BF)
+    for pool in (K, V):
+        with pytest.raises(taps.TapsError):
+            call(Q, K, V, table, start, kv, max_len, out=pool.view(-1)[:8 * 4 * 128].view(8, 4, 128))

@@ -193,3 +193,28 @@ def test_special_values_of_rows_in_parts(dtype):
 def test_numbers_of_rows_around_the_cut(rows):
     x, tok = peaked(rows, rows, 1, 50021)
     check(x, tok, 2)
+
+
+def test_rows_past_32_bits():
+    """Rows whose bytes lie past 4 GB."""
+    x, tok = peaked(41, 9, 1, 1000)
+    far = torch.empty(9, 1 << 28, dtype=BF, device="cuda")
+    far[:, :1000] = x[:, 0]
+    got = check(far[:, None, :1000], tok, top=8)
+    want = check(x, tok, top=8)
+    for a, b in zip(got, want):
+        assert np.array_equal(a, b)
+
+
+def test_scratch_that_holds_nan():
+    x, tok = peaked(42, 3, 1, 70001)
+    op = taps.TokenLogProbs(3, 1, 70001, top=9)
+    want = op(x, tok)
+    ws = torch.full((op.ws_bytes,), 0xFF, dtype=torch.uint8, device="cuda")
+    got = [torch.full_like(t, 7) for t in want]
+    st = op.lib.taps_logprobs(x.data_ptr(), 70001, 3, 1, 70001, taps.BF16, None, tok.data_ptr(), 9,
+                              *(t.data_ptr() for t in got), ws.data_ptr(), op.ws_bytes,
+                              torch.cuda.current_stream().cuda_stream)
+    assert st == 0 and op.ws_bytes > 0
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)

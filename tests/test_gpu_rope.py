@@ -203,3 +203,33 @@ def test_arguments_are_checked():
         taps.rope_frequencies(64, scaling="cubic")
     with pytest.raises(taps.TapsError):
         taps.rope_frequencies(63)
+
+
+def test_pool_rows_past_32_bits():
+    """Slots whose bytes lie past 4 GB; the rows beside them stay."""
+    freq, _ = taps.rope_frequencies(128)
+    Q, K, V, pos, _, _, _, qw, kw = inputs(31, 6, 4, 8, 128, 32, BF, fused=False, pad=False)
+    pages = 70000
+    far = torch.tensor([pages * 32 - 1, 5, 2 ** 21 + 1, 2 ** 21 - 1, pages * 32 - 3, 2 ** 21 + 99],
+                       device="cuda")
+    Kp = torch.empty(pages, 32, 8, 128, dtype=BF, device="cuda")
+    Vp = torch.empty_like(Kp)
+    beside = (far - 1).clamp(min=0)
+    Kp.flatten(0, 1)[beside], Vp.flatten(0, 1)[beside] = 3.0, 4.0
+    op = taps.PagedQKRope(4, 8, 128, 32, freq)
+    out = op(Q, K, V, pos, far, Kp, Vp, qw, kw)
+    K1, V1 = Kp[:2].clone(), Vp[:2].clone()
+    near = torch.arange(6, device="cuda") * 2 + 1
+    want = op(Q, K, V, pos, near, K1, V1, qw, kw)
+    assert torch.equal(out, want)
+    assert torch.equal(Kp.flatten(0, 1)[far], K1.flatten(0, 1)[near])
+    assert torch.equal(Vp.flatten(0, 1)[far], V)
+    assert (Kp.flatten(0, 1)[beside] == 3).all() and (Vp.flatten(0, 1)[beside] == 4).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_negative_positions(dtype):
+    freq, _ = taps.rope_frequencies(64, 1e4)
+    inp = list(inputs(32, 40, 4, 2, 128, 32, dtype))
+    inp[3] = torch.arange(-20, 20, dtype=torch.int32, device="cuda") * 1001
+    check(inp, freq)

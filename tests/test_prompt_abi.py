@@ -120,3 +120,14 @@ def test_logprobs_workspace_is_for_few_rows(lib):
     ws = lib.taps_logprobs_workspace_bytes
     assert ws(4, 512, 151936, 0, 5) == 0 and ws(1, 1, 1000, 0, 5) == 0 and ws(0, 1, 151936, 0, 5) == 0
     assert 0 < ws(1, 1, 151936, 0, 64) <= 16 * (32 + 8 * 64) and ws(1, 1, 151936, 0, 65) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(O=F + GB), dict(O=F + 2 * GB + 16),
+                                dict(O=F + GB - 100 * 4096 * 2 + 16),
+                                dict(K=F + 3 * GB - 600 * 64 * 1024 * 2 + 16)])
+def test_chunk_refuses_an_output_in_the_pools(lib, kw):
+    assert chunk(lib, **kw) == INV
+
+
+def test_strides_whose_spans_would_pass_64_bits_are_refused(lib):
+    assert rope(lib, qs=(1 << 30) + 8) == UNS and chunk(lib, qs=(1 << 30) + 8) == UNS
