@@ -626,8 +626,9 @@ taps_status chunk_attn_paged_validate(int32_t batch, int32_t rows, int32_t Hq, i
                                       int32_t head_dim, int32_t max_len, int32_t page_rows,
                                       int32_t window, int32_t dtype, float scale);
 
-/* Bytes of scratch chunk_attn_paged needs (parts of tiles that are cut; 0 for short caches and
- * for sizes that it rejects).  Calls that may overlap on the GPU need scratch of their own. */
+/* Bytes of scratch chunk_attn_paged needs (parts of tiles that are cut, none for short caches;
+ * where each request begins, for more than 256; 0 for sizes that it rejects).  Calls that may
+ * overlap on the GPU need scratch of their own. */
 size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq, int32_t Hkv,
                                         int32_t head_dim, int32_t max_len, int32_t page_rows,
                                         int32_t dtype);
@@ -650,7 +651,9 @@ size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq,
  *   kv_len       [batch] int32, clamped to [0, max_len].  Rows that no token of the call sees may
  *                hold anything; rows that one sees and that are not finite leave undefined values
  *                in any of the request's outputs
- *   rows         [host] rows of Q and O, sizes the grid
+ *   rows         [host] rows of Q and O, sizes the grid; rows * Hq at most 2^30, batch at most
+ *                2^20, and rows * Hq / 128 (fp32: 64) + batch * Hkv below 8 million or so (a
+ *                launch's threads are counted in 32 bits)
  *   head_dim     64 or 128; Hq a multiple of Hkv
  *   max_len      [host] upper bound of kv_len, at most 2^30
  *   window       0: none; else at least 1

@@ -762,10 +762,10 @@ taps_status chunk_attn_paged_validate(int32_t batch, int32_t rows, int32_t Hq, i
   if (max_len > 1 << 30 || window > 1 << 30) return TAPS_ERR_UNSUPPORTED;
   // a half tile's 32 rows are addressed with 32-bit offsets
   if ((int64_t)Hkv * head_dim * 4 > ((int64_t)1 << 24)) return TAPS_ERR_UNSUPPORTED;
-  // query rows of a request and workgroups are counted in 32 bits
+  // query rows of a request, workgroups and a launch's threads are counted in 32 bits
   if (Hq > 65535 || batch > 1 << 20 || (int64_t)rows * Hq > (int64_t)1 << 30)
     return TAPS_ERR_UNSUPPORTED;
-  if (plan_chunk(batch, rows, Hq, Hkv, head_dim, max_len, dtype).items * Hkv > (int64_t)1 << 30)
+  if (plan_chunk(batch, rows, Hq, Hkv, head_dim, max_len, dtype).items * Hkv >= (int64_t)1 << 23)
     return TAPS_ERR_UNSUPPORTED;
   return TAPS_OK;
 }

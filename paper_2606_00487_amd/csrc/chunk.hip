@@ -8,8 +8,9 @@
 // Pieces.  A workgroup takes the keys of one (KV head, query tile), or a part of them: no piece of
 // a tile that is cut has more than L units of 64 keys, L = all tiles' units / 256 (or 512), so that
 // a few long requests fill the chip as well as many short ones.  The requests' lengths are device
-// data: every workgroup forms L and finds its piece from prefix sums over the batch.  Pieces of a
-// tile that was cut leave (O, max, sum) in fp32, which a second kernel adds.
+// data: every workgroup forms L and finds its piece from prefix sums over the batch, or, of many
+// requests, in an index that a first kernel writes.  Pieces of a tile that was cut leave (O, max,
+// sum) in fp32, which a second kernel adds.
 //
 // bf16 (v_mfma_f32_32x32x16_bf16): eight waves (short prompts and head_dim 64: four) of 32 query
 // rows each share the key tile.  S^T = K Q^T (A: keys from LDS, B: queries in registers) leaves a
@@ -31,6 +32,7 @@
 // us, 90 TFLOP/s (a library product: 145).  128 rows a tile take 352 us there, and 41 for 47 us for
 // 16 tokens over 8K, but 254 for 225 us for 8 ragged requests.
 #include <algorithm>
+#include <climits>
 
 #include "common.h"
 #include "ldsload.h"
@@ -61,33 +63,37 @@ struct ChunkArgs {
   float* wsO;     // [slots][M][HD]; null: no piece is cut
   float2* wsML;   // [slots][M]
   int slots;
+  const int4* index;   // many requests: where each begins
 };
 
-// One request's share: n new tokens (rows q0 ..), kv rows, query tiles and the most key units
-// that one of its tiles sees
+// Most key units that one of a request's tiles sees of kv rows: with a window, the keys of a tile's
+// first to last token's, wherever they begin in a unit
+template <int M>
+__device__ inline int units_of(const ChunkArgs& A, int kv, int G) {
+  const int units = (kv + kUnit - 1) / kUnit;
+  if (A.window <= 0) return units;
+  const int64_t span = (int64_t)A.window + (M + G - 2) / G;
+  return (int)min((int64_t)units, (span + kUnit - 2) / kUnit + 1);
+}
+// One request's share: n new tokens (rows q0 ..), kv rows, query tiles and units_of
 struct Request {
   int q0, n, kv, tiles, units;
 };
 template <int M>
-__device__ inline Request request_of(const ChunkArgs& A, int b, int G) {
-  Request r{0, 0, 0, 0, 0};
-  if (b >= A.batch) return r;
-  r.q0 = min(max(A.q_start[b], 0), A.rows);
-  r.n = max(min(max(A.q_start[b + 1], 0), A.rows) - r.q0, 0);
-  r.kv = min(max(A.kv_len[b], 0), A.max_len);
+__device__ inline Request request_of(const ChunkArgs& A, int b, int G) {   // b >= batch: none
+  const int at = min(b, A.batch - 1);
+  const int q0 = A.q_start[at], q1 = A.q_start[at + 1], kv = A.kv_len[at];
+  Request r;
+  r.q0 = min(max(q0, 0), A.rows);
+  r.n = b < A.batch ? max(min(max(q1, 0), A.rows) - r.q0, 0) : 0;
+  r.kv = b < A.batch ? min(max(kv, 0), A.max_len) : 0;
   r.tiles = (int)(((int64_t)r.n * G + M - 1) / M);
-  r.units = (r.kv + kUnit - 1) / kUnit;
-  // the keys of a tile's first to last token's window, wherever they begin in a unit
-  if (A.window > 0) {
-    const int64_t span = (int64_t)A.window + (M + G - 2) / G;
-    r.units = (int)min((int64_t)r.units, (span + kUnit - 2) / kUnit + 1);
-  }
+  r.units = units_of<M>(A, r.kv, G);
   return r;
 }
 
-__device__ inline int64_t wave_sum_i64(int64_t v) {
-  return (int64_t)lane_u64(wave_scan_u64((uint64_t)v), kWave - 1);
-}
+__device__ inline int64_t wave_scan_i64(int64_t v) { return (int64_t)wave_scan_u64((uint64_t)v); }
+__device__ inline int64_t lane_i64(int64_t v, int l) { return (int64_t)lane_u64((uint64_t)v, l); }
 
 // Key units per piece at most: the sum of tiles * units over the batch, times the KV heads, in
 // `target` parts
@@ -98,16 +104,6 @@ __device__ inline int units_per_piece(const ChunkArgs& A, int64_t total) {
 // ... and the pieces of a tile of the request
 __device__ inline int splits_of(const ChunkArgs& A, int units, int L) {
   return units - A.cut.gain > L ? (units + L - 1) / L : 1;
-}
-template <int M>
-__device__ inline int piece_units(const ChunkArgs& A, int G, const Request& first) {
-  const int lane = threadIdx.x & (kWave - 1);
-  int64_t total = wave_sum_i64((int64_t)first.tiles * first.units);
-  for (int b0 = kWave; b0 < A.batch; b0 += kWave) {
-    const Request r = request_of<M>(A, b0 + lane, G);
-    total += wave_sum_i64((int64_t)r.tiles * r.units);
-  }
-  return units_per_piece(A, total);
 }
 
 // Piece `item` of the batch (without the KV head), item counting the requests' tiles * splits.  The
@@ -120,72 +116,154 @@ struct Piece {
   int group;   // ROWS > 0: the request's group of rows
   bool found;
 };
+constexpr int kWhole = 1 << 30;   // L where nothing is cut
+// what a request has of the pieces and of the second kernel's groups of rows
+struct Share {
+  int splits;
+  int64_t pieces, cut, groups;
+};
+__device__ inline Share share_of(const ChunkArgs& A, const Request& r, int L, int G, int rows) {
+  Share h;
+  h.splits = splits_of(A, r.units, L);
+  h.pieces = (int64_t)r.tiles * h.splits;
+  h.cut = h.splits > 1 ? h.pieces : 0;
+  h.groups = h.splits > 1 ? (r.n * G + rows - 1) / rows : 0;
+  return h;
+}
+// the `at`-th piece or group of a request
+template <int M, int ROWS>
+__device__ inline Piece piece_of(const Request& r, int b, int splits, int L, int at, int slot) {
+  Piece p{};
+  p.b = b, p.q0 = r.q0, p.n = r.n, p.kv = r.kv, p.tiles = r.tiles, p.splits = splits;
+  p.L = splits > 1 ? L : kWhole;
+  if constexpr (ROWS > 0) {
+    p.group = at;
+    p.tile = at / (M / ROWS);
+  } else {
+    p.split = splits == 1 ? 0 : at / p.tiles;
+    p.tile = p.tiles - 1 - (at - p.split * p.tiles);
+  }
+  p.slot = slot + p.tile;
+  p.found = true;
+  return p;
+}
 template <int M, int ROWS>
 __device__ inline Piece find_piece(const ChunkArgs& A, int G, int item) {
   const int lane = threadIdx.x & (kWave - 1);
-  if (A.batch == 1) {   // no sums over the batch, all of it uniform
+  constexpr int rows = ROWS > 0 ? ROWS : 1;
+  if (A.batch == 1) {   // no sums, all of it uniform
     const Request r = request_of<M>(A, 0, G);
-    Piece p{};
-    p.q0 = r.q0, p.n = r.n, p.kv = r.kv, p.tiles = r.tiles;
-    p.L = 1 << 30;
-    p.splits = 1;
-    if (A.wsO != nullptr) {
-      p.L = units_per_piece(A, (int64_t)r.tiles * r.units);
-      p.splits = splits_of(A, r.units, p.L);
-      if (p.splits == 1) p.L = 1 << 30;
-    }
-    if constexpr (ROWS > 0) {
-      p.found = p.splits > 1 && item < (r.n * G + ROWS - 1) / ROWS;
-      p.group = item;
-      p.tile = item / (M / ROWS);
-    } else {
-      p.found = item < r.tiles * p.splits;
-      p.split = r.tiles == 0 || p.splits == 1 ? 0 : item / r.tiles;
-      p.tile = r.tiles - 1 - (item - p.split * r.tiles);
-    }
-    p.slot = p.tile;
-    return p;
+    const int L = A.wsO ? units_per_piece(A, (int64_t)r.tiles * r.units) : kWhole;
+    const Share h = share_of(A, r, L, G, rows);
+    if (item >= (ROWS > 0 ? h.groups : h.pieces)) return Piece{};
+    return piece_of<M, ROWS>(r, 0, h.splits, L, item, 0);
   }
-  const Request first = request_of<M>(A, lane, G);
-  const bool whole = A.wsO == nullptr;
-  const int L = whole ? 1 << 30 : piece_units<M>(A, G, first);
-  Piece p{};
-  p.found = false;
-  int64_t before = 0, cut_before = 0;
-  for (int b0 = 0; b0 < A.batch; b0 += kWave) {
-    const Request r = b0 == 0 ? first : request_of<M>(A, b0 + lane, G);
-    const int splits = whole ? 1 : splits_of(A, r.units, L);
-    const int64_t pieces = (int64_t)r.tiles * splits;
-    const int64_t cut = splits > 1 ? pieces : 0;
-    int64_t count = pieces;
-    if constexpr (ROWS > 0) count = splits > 1 ? ((int64_t)r.n * G + ROWS - 1) / ROWS : 0;
-    const int64_t incl = (int64_t)wave_scan_u64((uint64_t)count);
-    const int64_t cut_incl = (int64_t)wave_scan_u64((uint64_t)cut);
-    const uint64_t hit = __ballot(before + incl > item);
-    if (hit) {
-      const int l = __ffsll((long long)hit) - 1;
-      // (at most item)
-      const int at = (int)(item - (before + (int64_t)lane_u64((uint64_t)(incl - count), l)));
-      auto of = [&](int x) { return (int)__builtin_amdgcn_readlane(x, l); };
-      p.b = b0 + l;
-      p.q0 = of(r.q0), p.n = of(r.n), p.kv = of(r.kv), p.tiles = of(r.tiles);
-      p.splits = of(splits);
-      p.L = p.splits > 1 ? L : 1 << 30;
-      if constexpr (ROWS > 0) {
-        p.group = at;
-        p.tile = at / (M / ROWS);
-      } else {
-        p.split = p.splits == 1 ? 0 : at / p.tiles;
-        p.tile = p.tiles - 1 - (at - p.split * p.tiles);
+  if (A.index == nullptr) {   // a request per lane at a time
+    Request r = request_of<M>(A, lane, G);
+    int L = kWhole;
+    if (A.wsO) {
+      int64_t total = lane_i64(wave_scan_i64((int64_t)r.tiles * r.units), kWave - 1);
+      for (int b0 = kWave; b0 < A.batch; b0 += kWave) {
+        const Request o = request_of<M>(A, b0 + lane, G);
+        total += lane_i64(wave_scan_i64((int64_t)o.tiles * o.units), kWave - 1);
       }
-      p.slot = (int)(cut_before + (int64_t)lane_u64((uint64_t)(cut_incl - cut), l)) + p.tile;
-      p.found = true;
-      return p;
+      L = units_per_piece(A, total);
     }
-    before += (int64_t)lane_u64((uint64_t)incl, kWave - 1);
-    cut_before += (int64_t)lane_u64((uint64_t)cut_incl, kWave - 1);
+    int64_t before = 0, cut_before = 0;
+    for (int b0 = 0; b0 < A.batch; b0 += kWave) {
+      if (b0 > 0) r = request_of<M>(A, b0 + lane, G);
+      const Share h = share_of(A, r, L, G, rows);
+      const int64_t count = ROWS > 0 ? h.groups : h.pieces;
+      const int64_t incl = before + wave_scan_i64(count);
+      const int64_t cut = cut_before + wave_scan_i64(h.cut);
+      const uint64_t hit = __ballot(incl > item);
+      if (hit) {
+        const int l = __ffsll((long long)hit) - 1;
+        auto of = [&](int x) { return (int)__builtin_amdgcn_readlane(x, l); };
+        const Request q{of(r.q0), of(r.n), of(r.kv), of(r.tiles), of(r.units)};
+        return piece_of<M, ROWS>(q, b0 + l, of(h.splits), L,
+                                 item - (int)lane_i64(incl - count, l),
+                                 (int)lane_i64(cut - h.cut, l));
+      }
+      before = lane_i64(incl, kWave - 1), cut_before = lane_i64(cut, kWave - 1);
+    }
+    return Piece{};
   }
-  return p;
+  // the last request that begins at or before the item
+  const int* const begins = (const int*)A.index + (ROWS > 0 ? 2 : 0);
+  const int4 end = A.index[A.batch];
+  if (item >= (ROWS > 0 ? end.z : end.x)) return Piece{};
+  int b = 0;
+  for (int n = A.batch; n > 1;) {
+    const int step = (n + kWave - 1) / kWave;
+    const bool in = lane * step < n;
+    const int v = begins[(size_t)4 * (b + (in ? lane * step : 0))];
+    const int k = __popcll(__ballot(in && v <= item)) - 1;
+    b += k * step;
+    n = min(step, n - k * step);
+  }
+  const int4 e = A.index[b];
+  const Request r = request_of<M>(A, b, G);
+  auto first = [](int x) { return (int)__builtin_amdgcn_readfirstlane(x); };
+  const Request q{first(r.q0), first(r.n), first(r.kv), first(r.tiles), first(r.units)};
+  return piece_of<M, ROWS>(q, b, first(e.w), first(end.w), item - first(ROWS > 0 ? e.z : e.x),
+                           first(e.y));
+}
+
+// More than 256 requests (up to there every workgroup adds up the batch itself, 64 at a time):
+// where each begins, [batch + 1] of (pieces, pieces of cut tiles, groups of `group_rows` rows of
+// the second kernel, its splits; last: the sums and L).  One workgroup, 3 us.  us with / without,
+// requests of 1 to 16 tokens over 100 to 1000 keys, 32/8 heads of 128: 100 requests 54 / 51, 256
+// 123 / 123, 1024 438 / 730, 4096 1723 / 6930.
+constexpr int kIndexThreads = 1024;
+template <int M>
+__global__ __launch_bounds__(kIndexThreads) void chunk_index_kernel(const ChunkArgs A,
+                                                                    int group_rows, int4* index) {
+  __shared__ int64_t s_sum[kIndexThreads / kWave];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int G = A.Hq / A.Hkv;
+  // inclusive sum over the workgroup's threads; total: over all of them
+  auto scan = [&](int64_t v, int64_t& total) {
+    const int64_t incl = wave_scan_i64(v);
+    __syncthreads();
+    if (lane == kWave - 1) s_sum[wave] = incl;
+    __syncthreads();
+    int64_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kIndexThreads / kWave; ++w) {
+      if (w < wave) before += s_sum[w];
+      total += s_sum[w];
+    }
+    return before + incl;
+  };
+  int L = kWhole;
+  if (A.wsO) {
+    int64_t sum = 0, total;
+    for (int b = tid; b < A.batch; b += kIndexThreads) {
+      const Request r = request_of<M>(A, b, G);
+      sum += (int64_t)r.tiles * r.units;
+    }
+    scan(sum, total);
+    L = units_per_piece(A, total);
+  }
+  // (starts that decrease name rows more than once: any number of pieces, of which the grid runs
+  // the first; those that L cuts are few even so)
+  int64_t begin = 0, others = 0;   // others: cut pieces and, in the upper half, groups
+  for (int b0 = 0; b0 < A.batch; b0 += kIndexThreads) {
+    const int b = b0 + tid;
+    const Share h = share_of(A, request_of<M>(A, b, G), L, G, group_rows);
+    const int64_t both = h.cut | h.groups << 32;
+    int64_t total, total_others;
+    const int64_t at = begin + scan(h.pieces, total) - h.pieces;
+    const int64_t o = others + scan(both, total_others) - both;
+    if (b < A.batch)
+      index[b] = make_int4((int)min(at, (int64_t)INT_MAX), (int)o, (int)(o >> 32), h.splits);
+    begin += total, others += total_others;
+  }
+  if (tid == 0)
+    index[A.batch] = make_int4((int)min(begin, (int64_t)INT_MAX), (int)others,
+                               (int)(others >> 32), L);
 }
 
 // Keys [lo, hi) that the tokens t0 .. t1 of a request see between them
@@ -888,6 +966,15 @@ hipError_t launch_combine(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s)
 template <typename T, int HD>
 hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
   const unsigned grid = (unsigned)(p.items * A.Hkv);
+  if (A.index) {
+    int4* const index = const_cast<int4*>(A.index);
+    const int g = p.cut_rows;
+    if (sizeof(T) == 4) chunk_index_kernel<kMF><<<1, kIndexThreads, 0, s>>>(A, g, index);
+    else if (p.rows == 256) chunk_index_kernel<256><<<1, kIndexThreads, 0, s>>>(A, g, index);
+    else chunk_index_kernel<128><<<1, kIndexThreads, 0, s>>>(A, g, index);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if constexpr (sizeof(T) == 4) chunk_f32_kernel<HD><<<grid, kThreads, 0, s>>>(A);
   else if (p.rows == 256) chunk_bf16_kernel<HD, 8><<<grid, 512, 0, s>>>(A);
   else chunk_bf16_kernel<HD, 4><<<grid, 256, 0, s>>>(A);
@@ -943,11 +1030,13 @@ ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int head_dim, int max
   p.cut_groups = may_cut ? std::min<int64_t>(groups, std::max(1, 1024 / Hkv)) : 0;
   p.slots = may_cut ? (int64_t)Hkv * std::max<int64_t>(1, 2 * target / Hkv) : 0;
   p.items = tiles + p.slots / Hkv;
+  p.indexed = batch > 4 * kWave ? batch + 1 : 0;
   return p;
 }
 
 size_t chunk_ws_bytes(const ChunkPlan& p, int head_dim) {
-  return (size_t)p.slots * p.rows * (head_dim * sizeof(float) + sizeof(float2));
+  return (size_t)p.indexed * sizeof(int4) +
+         (size_t)p.slots * p.rows * (head_dim * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const void* V,
@@ -964,8 +1053,9 @@ hipError_t launch_chunk(const void* Q, int64_t q_stride, const void* K, const vo
   A.cut = p.cut;
   A.O = (unsigned char*)O;
   A.slots = (int)p.slots;
-  A.wsO = p.slots ? (float*)ws : nullptr;
-  A.wsML = p.slots ? (float2*)((float*)ws + (size_t)p.slots * p.rows * head_dim) : nullptr;
+  A.index = p.indexed ? (const int4*)ws : nullptr;
+  A.wsO = p.slots ? (float*)((int4*)ws + p.indexed) : nullptr;
+  A.wsML = p.slots ? (float2*)(A.wsO + (size_t)p.slots * p.rows * head_dim) : nullptr;
   if (dtype == TAPS_BF16)
     return head_dim == 128 ? launch_t<__bf16, 128>(A, p, s) : launch_t<__bf16, 64>(A, p, s);
   return head_dim == 128 ? launch_t<float, 128>(A, p, s) : launch_t<float, 64>(A, p, s);

@@ -198,6 +198,7 @@ struct ChunkPlan {
   int64_t cut_groups;  // groups of rows per KV head of requests that are cut (0: none ever is)
   int cut_rows;        // rows of such a group: 16, or 4
   int64_t slots;       // most pieces of cut tiles, all KV heads
+  int indexed;         // more than 256 requests: entries of their index, else 0
 };
 ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int head_dim, int max_len,
                      int dtype);

@@ -371,3 +371,45 @@ def test_refuses_output_in_the_pools():
     for pool in (K, V):
         with pytest.raises(taps.TapsError):
             call(Q, K, V, table, start, kv, max_len, out=pool.view(-1)[:8 * 4 * 128].view(8, 4, 128))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("B", [256, 257, 1025, 4100])
+def test_more_requests_than_are_added_up_by_every_workgroup(dtype, B):
+    """Empty ones among them, and some that are cut."""
+    rng = np.random.default_rng(B)
+    n = rng.integers(0, 5, B)
+    lens = [(int(a), int(a + c)) for a, c in zip(n, rng.integers(0, 60, B))]
+    check(case(29, lens, 4, 2, 64, 32, dtype, pad=3, lead=2))
+    lens[200], lens[B - 2], lens[B - 1] = (9, 9000), (70, 7000), (0, 0)
+    check(case(30, lens, 4, 2, 128, 32, dtype))
+
+
+def test_index_scratch_that_holds_nan_and_graphs():
+    rng = np.random.default_rng(1)
+    lens = [(int(a), int(a + 30)) for a in rng.integers(0, 4, 300)]
+    Q, K, V, table, start, kv, max_len = case(31, lens, 4, 2, 64, 32, BF)
+    op, want = call(Q, K, V, table, start, kv, max_len)
+    ws = torch.full((op._ws_bytes(Q.shape[0]),), 0xFF, dtype=torch.uint8, device="cuda")
+    del ws                                     # torch's allocator hands the same memory out again
+    assert torch.equal(call(Q, K, V, table, start, kv, max_len)[1], want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = op(Q, K, V, table, start, kv)
+    for i in range(3):
+        out.zero_()
+        Q.neg_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, op(Q, K, V, table, start, kv))
+
+
+def test_many_requests_whose_starts_decrease():
+    """Rows that several requests name hold any of theirs; nothing else is written."""
+    Q, K, V, table, start, kv, max_len = case(32, [(2, 40)] * 300, 4, 2, 64, 32, BF, pad=4)
+    odd = start.clone()
+    odd[1::2] = 0
+    buf = torch.full((606, 4, 64), 7.0, dtype=BF, device="cuda")
+    call(Q, K, V, table, odd, kv, max_len, out=buf[1:605])
+    torch.cuda.synchronize()
+    assert (buf[0] == 7).all() and (buf[601:] == 7).all()

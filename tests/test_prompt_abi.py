@@ -131,3 +131,21 @@ def test_chunk_refuses_an_output_in_the_pools(lib, kw):
 
 def test_strides_whose_spans_would_pass_64_bits_are_refused(lib):
     assert rope(lib, qs=(1 << 30) + 8) == UNS and chunk(lib, qs=(1 << 30) + 8) == UNS
+
+
+def test_chunk_scratch_of_many_requests(lib):
+    ws = lib.chunk_attn_paged_workspace_bytes
+    assert ws(256, 300, 32, 8, 128, 640, 64, 0) == 0
+    assert ws(257, 300, 32, 8, 128, 640, 64, 0) == 258 * 16
+    kw = dict(batch=257, rows=300, max_len=640)
+    assert chunk(lib, ws=None, **kw) == WS and chunk(lib, ws_bytes=258 * 16 - 1, **kw) == WS
+    assert chunk(lib, ws=F + 8, **kw) == WS
+
+
+def test_chunk_refuses_more_workgroups_than_a_launch_holds(lib):
+    """Their threads are counted in 32 bits."""
+    v = lib.chunk_attn_paged_validate
+    assert v(1 << 20, 1 << 20, 32, 8, 128, 4096, 64, 0, 0, 1.0) == UNS
+    assert v(1 << 19, 1 << 20, 32, 8, 128, 4096, 64, 0, 0, 1.0) == OK
+    assert v(1, 1 << 24, 64, 8, 128, 4096, 64, 0, 0, 1.0) == OK
+    assert v(1, 1 << 24, 64, 8, 64, 4096, 64, 0, 1, 1.0) == UNS
