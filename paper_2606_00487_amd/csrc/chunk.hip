@@ -286,12 +286,13 @@ __device__ inline float pair_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// permutation of a row's 16-byte chunk index: the rows that an LDS read touches at once land
-// on distinct banks (rows of 16 chunks: all four bits of the row, of 8: three)
+// permutation of a row's 16-byte chunk index: the 16 rows that an LDS read of K touches at once,
+// and the four of V, land on distinct banks (rows of 16 chunks: all four bits of the row; of 8, of
+// which two rows fill the banks: the upper three)
 template <int HD>
 __device__ inline int chunk_perm(int r) {
   if constexpr (HD == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
-  else return ((r & 3) << 1) | ((r >> 2) & 1);
+  else return ((r & 2) << 1) | ((r >> 2) & 3);
 }
 
 // the order of a region's instructions: N times a matrix product, DS LDS reads, V vector and T
