@@ -20,10 +20,9 @@
 // with more than kCand values at the bound (ties), or without k values above kLow (masks), go
 // value by value instead: the largest value not yet taken, then its places in index order.
 //
-// Bound: HBM; in bf16 the vector unit is close behind (9.5 instruction slots an element, of the 16
-// that the memory's rate leaves, four of them the exponential's).  2048 rows of 151,936 in bf16
-// (622 MB) take 129 us, 4.8 TB/s; 64 of them, in four parts each, 17 us with the join's 4 and two
-// launches.
+// Bound: HBM; in bf16 the vector unit is close behind (7.7 instructions an element, one of them the
+// exponential).  2048 rows of 151,936 in bf16 (622 MB) take 121 us, 5.1 TB/s; 64 of them, in four
+// parts each, 16 us with the join's 4 and two launches.
 #include <algorithm>
 #include <cmath>
 
@@ -234,7 +233,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
   // ---- one pass
   float Z, S, c, ref, best, rest;   // best: largest value; rest: the largest of other batches
   int best_at, before;              // before: of the wave's values
-  auto values = [&](const float* x, int n, float mx, int at) __attribute__((always_inline)) {
+  // mx: the largest of the values that come next, of batch `at`
+  auto expect = [&](float mx, int at) __attribute__((always_inline)) {
     if (__ballot(mx > ref + 5.5f)) {   // 5.5 log2 e: 2^8
       const bool upd = mx > ref + 5.5f;
       const float cn = -(mx * kLog2e);
@@ -249,6 +249,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
     }
     rest = fmaxf(rest, fminf(mx, best));
     if (mx > best) best = mx, best_at = at;
+  };
+  auto add = [&](const float* x, int n) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < n; ++e) {
       const float t = fmaf(x[e], kLog2e, c);
@@ -257,37 +259,58 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
       S = fmaf(w, t, S);
     }
   };
-  // the batch in cur; careful: units past the row read as kLow
-  auto batch = [&](auto careful, int k) __attribute__((always_inline)) {
-    float x[UN * E];
+  // batch k in r; careful: values lifted, units past the row as kLow, where a whole round of them
+  // is past it left out
+  auto batch = [&](auto careful, const u32x4 (&r)[UN], int k) __attribute__((always_inline)) {
+    constexpr bool C = decltype(careful)::value;
+    const int rounds = C ? min(UN, (R.units - k * step + NT - 1) / NT) : UN;
+    float x[UN * E], m[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int j = 0; j < UN; ++j) {
+      if (C && j >= rounds) break;
       const int u = k * step + j * NT + tid;
       const float thr = u < tok_unit ? xt_below : xt;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        float v = unit_value<T>(cur[j], e);
-        if constexpr (decltype(careful)::value) v = u < R.units ? v : -INFINITY;
+        float v = unit_value<T>(r[j], e);
+        if constexpr (C) v = u < R.units ? v : -INFINITY;
         before += __popcll(__ballot(v > thr));
-        x[j * E + e] = decltype(careful)::value ? lifted(v) : v;
+        x[j * E + e] = C ? lifted(v) : v;
       }
-    }
-    float m0 = x[0], m1 = x[1];
+      asm volatile("" : "+s"(before));   // counted now: masks kept for later were spilled
 #pragma unroll
-    for (int e = 2; e < UN * E; e += 4) {
-      m0 = max3(m0, x[e], x[e + 1]);
-      if (e + 2 < UN * E) m1 = max3(m1, x[e + 2], x[e + 3]);
+      for (int e = 0; e < E; e += 2)
+        m[(e >> 1) & 1] = max3(m[(e >> 1) & 1], x[j * E + e], x[j * E + e + 1]);
     }
-    values(x, UN * E, max3(m0, m1, m1), k);
+    expect(max3(m[0], m[1], m[1]), k);
+#pragma unroll
+    for (int j = 0; j < UN; ++j) {
+      if (C && j >= rounds) break;
+      add(x + j * E, E);
+    }
   };
   auto pass = [&](auto careful) __attribute__((always_inline)) {
     Z = S = c = 0.f;
     ref = best = rest = -INFINITY;
     best_at = before = 0;
-    for (int k = 0; k < nb; ++k) {
-      if (k + 1 < nb) fetch(k + 1, nxt);
-      if (decltype(careful)::value || k == whole) batch(Flag<true>(), k);
-      else batch(Flag<false>(), k);
+    int k = 0;
+    if constexpr (!decltype(careful)::value) {
+      for (; k + 1 < whole; k += 2) {   // (fetch: past the last the same again)
+        fetch(k + 1, nxt);
+        batch(careful, cur, k);
+        fetch(k + 2, cur);
+        batch(careful, nxt, k + 1);
+      }
+      if (k < whole) {
+        fetch(k + 1, nxt);
+        batch(careful, cur, k++);
+#pragma unroll
+        for (int j = 0; j < UN; ++j) cur[j] = nxt[j];
+      }
+    }
+    for (; k < nb; ++k) {
+      fetch(k + 1, nxt);
+      batch(Flag<true>(), cur, k);
 #pragma unroll
       for (int j = 0; j < UN; ++j) cur[j] = nxt[j];
     }
@@ -298,7 +321,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
     before += __popcll(__ballot(in && (j < tok ? v >= xt : v > xt)));
     if (__ballot(in)) {
       const float x = lifted(v);
-      if (in) values(&x, 1, x, nb);
+      if (in) expect(x, nb), add(&x, 1);
     }
     if (wave == 0 && given && tok_unit >= 0 && tok_unit < R.units) {
       const int u0 = R.index(tok_unit, 0);
@@ -431,7 +454,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
     const float bound = s_bound;
     fallback = !(bound > kLow);
     if (!fallback) {
-      auto add = [&](float v, int j) {
+      auto offer = [&](float v, int j) {
         if (v >= bound) {
           const int at = atomicAdd(&s_count, 1);
           if (at < kCand) s_cand[at] = cand_key(value_key(__float_as_uint(v)), (uint32_t)(j0 + j));
@@ -447,11 +470,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
             const int u = k * step + j * NT + tid;
             if (u < R.units) {
 #pragma unroll
-              for (int e = 0; e < E; ++e) add(unit_value<T>(r[j], e), R.index(u, e));
+              for (int e = 0; e < E; ++e) offer(unit_value<T>(r[j], e), R.index(u, e));
             }
           }
         }
-        if (tid < R.head + R.tail) add(value_at(R.x, R.edge(tid)), R.edge(tid));
+        if (tid < R.head + R.tail) offer(value_at(R.x, R.edge(tid)), R.edge(tid));
       }
       __syncthreads();
       const int n = s_count;
