@@ -39,8 +39,9 @@ constexpr double kLog2eRest = 1.4426950408889634 - (double)kLog2e;
 // where the row's maximum is well above, and t stays finite (0 * inf).  Past 1e6 c's rounding
 // reaches a unit of the exponent.  Rows whose maximum is not between go by the definition.
 constexpr float kLow = -1e6f, kHigh = 1e6f;
-constexpr int kCand = 512;   // candidates for the top alternatives
 constexpr int kThreads = 512, kUnits = 4;   // 16-byte units per thread in a batch of loads
+constexpr int kCand = kThreads;             // candidates for the top alternatives
+constexpr int kFewTop = 48;                 // up to here 64 groups' maxima bound them well
 
 struct LogprobArgs {
   const unsigned char* x;
@@ -163,6 +164,11 @@ __device__ inline double power(double k) {
   const double n = __builtin_rint(k);
   return __builtin_ldexp((double)__builtin_amdgcn_exp2f((float)(k - n)), (int)n);
 }
+// the next float above x (finite)
+__device__ constexpr float next_up(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  return __builtin_bit_cast(float, x == 0.f ? 1u : x > 0.f ? b + 1 : b - 1);
+}
 // ln p of the value v, from the row's maximum and sum
 __device__ inline float log_prob(float v, float M, double Z, double lnz) {
   if (v != v || Z == 0.0) return -INFINITY;
@@ -217,6 +223,14 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
     for (int j = 0; j < UN; ++j) r[j] = R.unit(min(k * step + j * NT + tid, R.units - 1));
   };
   if (nb > 0) fetch(0, cur);
+  auto each = [&](auto f) {   // f(value, index) of the thread's values, a unit at a time
+    for (int u = tid; u < R.units; u += NT) {
+      const u32x4 r = R.unit(u);
+#pragma unroll
+      for (int e = 0; e < E; ++e) f(unit_value<T>(r, e), R.index(u, e));
+    }
+    if (tid < R.head + R.tail) f(value_at(R.x, R.edge(tid)), R.edge(tid));
+  };
 
   const int token = A.tokens[row];
   const bool given = token >= 0 && token < A.vocab;
@@ -344,12 +358,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
   }
   if (!ordinary && given) {   // a token of -inf or NaN: its rank by the definition
     const uint32_t kt = value_key(__float_as_uint(xt));
-    before = 0;
-    for (int q = 0; q < R.n; q += NT) {
-      const int j = q + tid;
-      const uint32_t k = j < R.n ? value_key(__float_as_uint(value_at(R.x, j))) : 0u;
-      before += __popcll(__ballot(j < R.n && (k > kt || (k == kt && j < tok))));
-    }
+    int mine = 0;
+    each([&](float v, int j) {
+      const uint32_t k = value_key(__float_as_uint(v));
+      mine += k > kt || (k == kt && j < tok);
+    });
+    before = (int)wave_sum((double)mine);
   }
 
   // ---- the waves' sums about their own maxima (ref -inf: a thread without values)
@@ -387,10 +401,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
     // about kLow or below, or above kHigh: weights by the definition
     float m = -INFINITY;
     bool any = false;
-    for (int j = tid; j < R.n; j += NT) {
-      const float v = value_at(R.x, j);
+    each([&](float v, int) {
       if (v == v) m = v > m ? v : m, any = true;
-    }
+    });
     m = wave_max(m);
     __syncthreads();
     if (lane == 0) s_m[wave] = m;
@@ -400,16 +413,15 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
     for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w]);
     Md = M;
     double z = 0.0, sn = 0.0;
-    for (int j = tid; have && j < R.n; j += NT) {
-      const float v = value_at(R.x, j);
+    if (have) each([&](float v, int) {
       if (v == M) {
         z += 1.0;
-      } else if (v == v) {
+      } else if (v == v && !isinf(M)) {
         const double d = (double)v - Md, w = exp(d);
         z += w;
         if (w > 0.0) sn += w * d;
       }
-    }
+    });
     z = wave_sum(z), sn = wave_sum(sn);
     if (lane == 0) s_z[wave] = z, s_s[wave] = sn;
     __syncthreads();
@@ -435,25 +447,61 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
   }
   if (top == 0) return;
 
-  // ---- top alternatives: the bound, by the first wave
-  bool fallback = special;
+  // ---- top alternatives: a bound from below, the smallest maximum that fewer than `top` groups of
+  // threads exceed
+  float bound = -INFINITY;
   if (!special) {
-    if (wave == 0) {
-      float v = s_max[lane];
+    if (top <= kFewTop) {   // 64 groups, by the first wave
+      if (wave == 0) {
+        float v = s_max[lane];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) v = fmaxf(v, s_max[w * 64 + lane]);
+        for (int w = 1; w < NW; ++w) v = fmaxf(v, s_max[w * 64 + lane]);
+        int above = 0;
+#pragma unroll
+        for (int q = 0; q < 64; ++q)
+          above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), q)) > v;
+        const float low = -wave_max(above < top ? -v : -INFINITY);
+        if (lane == 0) s_bound = low;
+      }
+    } else {                // NT / 2, by their threads
+      float v = INFINITY;
+      if (tid < NT / 2) s_max[tid] = v = fmaxf(s_max[tid], s_max[tid + NT / 2]);
+      __syncthreads();
       int above = 0;
-#pragma unroll
-      for (int q = 0; q < 64; ++q)
-        above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), q)) > v;
-      // the smallest value that fewer than `top` groups exceed
-      const float bound = -wave_max(above < top ? -v : -INFINITY);
-      if (lane == 0) s_bound = bound;
+#pragma unroll 8
+      for (int q = 0; q < NT / 2; ++q) above += s_max[q] > v;
+      const float low = wave_max(tid < NT / 2 && above < top ? -v : -INFINITY);
+      if (lane == 0) s_m[wave] = low;
+      __syncthreads();
+      if (wave == 0) {
+        const float all = -wave_max(s_m[min(lane, NW - 1)]);
+        if (lane == 0) s_bound = all;
+      }
     }
     __syncthreads();
-    const float bound = s_bound;
-    fallback = !(bound > kLow);
-    if (!fallback) {
+    bound = s_bound;
+  }
+  uint64_t last = 1ull << 32;   // values below this key are still to be found: all of them
+  int have = 0;
+  auto rank_found = [&](int n) {   // the n candidates in LDS
+    for (int q = tid; q < n; q += NT) {
+      const uint64_t mine = s_cand[q];
+      int r = 0;
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) r += s_cand[j] > mine;
+      if (r < top) found(r, mine);
+    }
+    have = min(n, top);
+  };
+  if (!(bound > kLow) && R.n <= kCand) {   // few values: all of them
+    for (int j = tid; j < R.n; j += NT)
+      s_cand[j] = cand_key(value_key(__float_as_uint(value_at(R.x, j))), (uint32_t)(j0 + j));
+    __syncthreads();
+    rank_found(R.n);
+    last = 0;
+  } else if (!special) {
+    bound = fmaxf(bound, next_up(kLow));   // masked rows: the values above kLow
+    for (;;) {
       auto offer = [&](float v, int j) {
         if (v >= bound) {
           const int at = atomicAdd(&s_count, 1);
@@ -478,29 +526,33 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
       }
       __syncthreads();
       const int n = s_count;
-      fallback = n > kCand;
-      if (!fallback) {
-        for (int q = tid; q < n; q += NT) {
-          const uint64_t mine = s_cand[q];
-          int r = 0;
-          for (int j = 0; j < n; ++j) r += s_cand[j] > mine;
-          if (r < top) found(r, mine);
-        }
+      if (n <= kCand) {
+        rank_found(n);
+        last = value_key(__float_as_uint(bound));
+        break;
       }
+      // too many: from the `top`-th of those that were kept, or, where the bound itself occurs too
+      // often, above it (its places follow in index order)
+      static_assert(kCand == NT, "a candidate per thread");
+      const uint64_t mine = s_cand[tid];
+      int r = 0;
+      for (int j = 0; j < kCand; ++j) r += s_cand[j] > mine;
+      __syncthreads();
+      if (r == top - 1) s_bound = key_value((uint32_t)(mine >> 32));
+      if (tid == 0) s_count = 0;
+      __syncthreads();
+      bound = s_bound > bound ? s_bound : next_up(bound);
     }
   }
-  if (!fallback) return;
 
-  // ---- value by value: the largest key below the last one, then its indices in order
-  uint64_t last = 1ull << 32;   // above every value's key
-  int have = 0;
+  // ---- the rest value by value: the largest key below the last one, then its indices in order
   while (have < top) {
     uint32_t m = 0;
     bool any = false;
-    for (int j = tid; j < R.n; j += NT) {
-      const uint32_t k = value_key(__float_as_uint(value_at(R.x, j)));
+    each([&](float v, int) {
+      const uint32_t k = value_key(__float_as_uint(v));
       if (k < last) m = max(m, k), any = true;
-    }
+    });
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
     __syncthreads();
@@ -509,22 +561,31 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
     m = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) m = max(m, (uint32_t)s_int[w]);
-    for (int q = 0; q < R.n && have < top; q += NT) {
-      const int j = q + tid;
-      const float v = j < R.n ? value_at(R.x, j) : 0.f;
-      const bool hit = j < R.n && value_key(__float_as_uint(v)) == m;
-      const uint64_t mask = __ballot(hit);
+    for (int q = 0; q < R.n && have < top; q += NT * 8) {   // 8 neighbours a thread
+      uint32_t hits = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int j = q + tid * 8 + e;
+        if (j < R.n && value_key(__float_as_uint(value_at(R.x, j))) == m) hits |= 1u << e;
+      }
+      int incl = __popc(hits);
+      const int mine = incl;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int below = __shfl_up(incl, o);
+        if (lane >= o) incl += below;
+      }
       __syncthreads();
-      if (lane == 0) s_int[wave] = __popcll(mask);
+      if (lane == kWave - 1) s_int[wave] = incl;
       __syncthreads();
-      int at = have, total = 0;
+      int at = have + incl - mine, total = 0;
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
         if (w < wave) at += s_int[w];
         total += s_int[w];
       }
-      at += __popcll(mask & ((1ull << lane) - 1));
-      if (hit && at < top) found(at, cand_key(m, (uint32_t)(j0 + j)));
+      for (; hits != 0 && at < top; ++at, hits &= hits - 1)
+        found(at, cand_key(m, (uint32_t)(j0 + q + tid * 8 + __ffs((int)hits) - 1)));
       have += total;
     }
     last = m;
@@ -559,8 +620,20 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(const Logpr
   for (int q = tid; q < n; q += kJoinThreads) {
     const uint64_t mine = s_key[q];
     int r = 0;
+    if (n <= 64) {
 #pragma unroll 8
-    for (int j = 0; j < n; ++j) r += s_key[j] > mine;
+      for (int j = 0; j < n; ++j) r += s_key[j] > mine;
+    } else {   // each part's are in order: by bisection
+      for (int p = 0; p < n; p += top) {
+        int lo = 0, hi = top;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (s_key[p + mid] > mine) lo = mid + 1;
+          else hi = mid;
+        }
+        r += lo;
+      }
+    }
     if (r >= top || mine == 0) continue;
     A.top_idx[(size_t)row * top + r] = (int)cand_index(mine);
     A.top_lp[(size_t)row * top + r] = log_prob(key_value((uint32_t)(mine >> 32)), M, Z, lnz);

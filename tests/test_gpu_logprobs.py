@@ -218,3 +218,59 @@ def test_scratch_that_holds_nan():
     assert st == 0 and op.ws_bytes > 0
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("mask", [-INF, torch.finfo(BF).min, -1e9, -20000.0])
+@pytest.mark.parametrize("V,rows", [(151936, 2), (30011, 3)])
+def test_masks_that_leave_few_values(dtype, mask, V, rows):
+    """0 to 100 values left, alternatives among them and in the mask; V in parts and whole."""
+    left = [0, 1, 5, 40, 63, 64, 65, 100][:rows * 4]
+    for top in (1, 5, 20, 33, 64):
+        x, tok = peaked(43, len(left), 1, V, dtype=dtype)
+        rng = np.random.default_rng(top)
+        for b, n in enumerate(left):
+            keep = torch.from_numpy(rng.choice(V, n, replace=False)).cuda()
+            row = torch.full((V,), mask, dtype=dtype, device="cuda")
+            row[keep] = x[b, 0, keep]
+            x[b, 0] = row
+            if n:
+                tok[b, 0] = int(keep[0])
+        check(x, tok, top=top)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("top", [20, 32, 33, 64])
+@pytest.mark.parametrize("distinct,equal", [(0, 600), (10, 600), (10, 5000), (31, 513), (500, 600),
+                                            (2000, 3000), (64, 20000), (5, 511)])
+def test_more_values_at_the_bound_than_candidates(dtype, top, distinct, equal):
+    """A few values above many equal ones, anywhere in the row; the rest far below."""
+    V = 40000
+    rng = np.random.default_rng(distinct + equal + top)
+    x = torch.from_numpy(rng.normal(size=(3, 1, V)) - 40).cuda().to(dtype)
+    for b in range(3):
+        at = torch.from_numpy(rng.permutation(V)[:distinct + equal]).cuda()
+        if b == 2:
+            at = at.sort().values          # the distinct ones first
+        x[b, 0, at[:distinct]] = (3 + torch.arange(distinct, device="cuda") / 64).to(dtype)
+        x[b, 0, at[distinct:]] = 2.0
+    tok = torch.tensor([[5], [at[0].item()], [at[-1].item()]], dtype=torch.int32, device="cuda")
+    check(x, tok, top=top)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("V", [1, 63, 64, 65, 200, 511, 512, 513, 700, 2000])
+def test_all_alternatives_of_small_vocabularies(dtype, V):
+    x, tok = peaked(44, 4, 1, V, dtype=dtype) if V >= 20 else (
+        torch.ones(4, 1, V, dtype=dtype, device="cuda"),
+        torch.zeros(4, 1, dtype=torch.int32, device="cuda"))
+    x[1] = -INF
+    x[2, 0, : V // 2] = NAN
+    x[3, 0, V // 2:] = INF
+    check(x, tok, top=min(V, 64))
+
+
+def test_sixty_four_alternatives_of_many_rows():
+    x, tok = peaked(45, 300, 1, 20000)
+    check(x, tok, top=64)
+    check(x.float(), tok, top=64)
