@@ -14,11 +14,13 @@
 // that meets one in its first loads does so at once), and rows whose maximum is not an ordinary
 // number are summed by the definition.
 //
-// Top alternatives: the k-th largest of 64 groups' maxima bounds the row's k-th value from below.
-// The few threads that reach it look again at the batch of loads that held their maximum (at all
-// of them if a second batch reaches the bound), and what they find is ranked by counting.  Rows
-// with more than kCand values at the bound (ties), or without k values above kLow (masks), go
-// value by value instead: the largest value not yet taken, then its places in index order.
+// Top alternatives: the k-th largest of 64 groups' maxima (of 256 from 49 alternatives on: the
+// smallest of 64 groups' maxima leaves hundreds; 48 take 20.5 us for 23.5) bounds the row's k-th
+// value from below.  The few threads that reach it look again at the batch of loads that held their
+// maximum (at all of them if a second batch reaches the bound), and what they find is ranked by
+// counting.  More than kCand values at the bound raise it: to the k-th of those kept, or past it
+// where it occurs too often.  Places that are left (ties, masked values) go value by value: the
+// largest value not yet taken, then its places in index order.
 //
 // Bound: HBM; in bf16 the vector unit is close behind (7.7 instructions an element, one of them the
 // exponential).  2048 rows of 151,936 in bf16 (622 MB) take 121 us, 5.1 TB/s; 64 of them, in four
@@ -642,18 +644,21 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(const Logpr
 
 }  // namespace
 
-// Parts of a row: a workgroup for each CU where the rows are few, none with less than a whole batch
-// of values.  The vector unit of one CU bounds a row on its own (152K values in bf16: 10 us); the
-// join costs 4 us and more workgroups contend.  us a call (5 alternatives, from graphs) with 1 / 2
-// / 4 / 8 parts, bf16 rows of 151,936: one row 18.1 / 15.5 / 13.1 / 12.3, 64 rows 27.1 / 20.1 /
-// 15.3 / 16.9, 128 rows 27.0 / 21.4 / 21.5 / 26.2, 256 rows 29.7 / 28.5 / 31.3 / 43.0; fp32 rows of
-// 50,257: one 10.0 / 10.7 / 9.8 / 9.4, 64 rows 13.7 / 13.1 / 11.1 / 12.7, 256 rows 17.3 / 20.2 /
-// 21.8 / 28.7; bf16 rows of 32,000: one 9.0 / 10.6 / 10.5 / 10.3.
+// Parts of a row: a workgroup for each CU where the rows are few (two, for more than 64 long rows),
+// none with less than a whole batch of values.  The vector unit of one CU bounds a row on its own
+// (152K values in bf16: 8 us); the join costs 4 us and more workgroups contend.  us a call (5
+// alternatives, from graphs) with 1 / 2 / 4 / 8 parts, bf16 rows of 151,936: one row 16.8 / 14.6 /
+// 12.3 / 11.5, 64 rows 25.9 / 19.3 / 14.6 / 15.0, 96 rows 25.7 / 19.5 / 18.1 / 17.9, 160 rows (1 /
+// 2 / 3 / 4) 27.0 / 26.3 / 22.8 / 22.4, 256 rows 29.0 / 28.5 / 28.7 / 36.4; fp32 rows of 50,257:
+// one 10.1 / 10.6 / 10.1 / 9.7, 96 rows 13.2 / 12.7 / 13.4 / 14.6, 256 rows 17.3 / 19.5 / 21.5 /
+// 29.0; 64 bf16 rows of 100,000 19.4 / 15.4 / 13.5 / 15.0; bf16 rows of 32,000: one 9.1 / 10.7 /
+// 9.9 / 9.5.
 int logprobs_parts(int64_t rows, int vocab, int dtype) {
   if (rows <= 0) return 1;
   const int64_t batch = kThreads * kUnits * (dtype == TAPS_BF16 ? 8 : 4);
   const int64_t most = std::min<int64_t>(kMaxParts, vocab / batch);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, 256 / rows));
+  const int wgs = rows > 64 && most >= 8 ? 512 : 256;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, wgs / rows));
 }
 size_t logprobs_ws_bytes(int64_t rows, int vocab, int dtype, int top) {
   const int parts = logprobs_parts(rows, vocab, dtype);
