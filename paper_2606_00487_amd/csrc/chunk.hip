@@ -16,9 +16,9 @@
 // rows each share the key tile.  S^T = K Q^T (A: keys from LDS, B: queries in registers) leaves a
 // query's scores in two lanes; they go, as P^T, straight into the B operand of O^T += V^T P^T,
 // whose key order follows the accumulators; the transposing LDS read takes V in that order.  K and
-// V cycle through rings of three tiles, filled by loads straight into LDS two tiles ahead; S of the
-// next tile is issued between this one's softmax and products, each matrix instruction among the
-// vector and LDS instructions of the other part.
+// V cycle through rings of three tiles (V of two where two workgroups are to share a CU), filled by
+// loads straight into LDS two tiles ahead; S of the next tile is issued between this one's softmax
+// and products, each matrix instruction among the vector and LDS instructions of the other part.
 // Bound: the matrix instructions (4 head_dim flops a visible pair and head) and, for few rows over
 // a long cache, HBM.  head_dim 128, 32/8 heads: a prompt of 16,384 tokens takes 1.88 ms, 1167
 // TFLOP/s (a library product of 8192^3: 1219).  A step of 64 keys takes 3500 cycles of which the
@@ -311,13 +311,13 @@ template <int P>
 struct Slot {
   static constexpr int value = P;
 };
-// W waves, 32 query rows each
-template <int HD, int W>
+// W waves, 32 query rows each; VR tiles of V in LDS
+template <int HD, int W, int VR>
 __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int M = 32 * W;
   constexpr int KT = 64;              // keys per tile
-  constexpr int RING = 3;             // tiles of K and of V in LDS
+  constexpr int RING = 3;             // tiles of K in LDS
   constexpr int ROWB = HD * 2, CPR = ROWB / 16;   // bytes and 16-byte chunks of a row
   constexpr int TILEB = KT * ROWB;
   constexpr int NKK = HD / 16, NDB = HD / 32;
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
   constexpr int BPW = TILEB / 1024 / HW;          // 1 KB loads per wave and tile
   constexpr int BROWS = 1024 / ROWB;              // rows per load: 4 or 8
   typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
-  __shared__ __attribute__((aligned(1024))) unsigned char s_k[RING * TILEB], s_v[RING * TILEB];
+  __shared__ __attribute__((aligned(1024))) unsigned char s_k[RING * TILEB], s_v[VR * TILEB];
 
   const int G = A.Hq / A.Hkv;
   const int kvh = blockIdx.x % A.Hkv;
@@ -538,51 +538,55 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
 
   // Begin of step t (slot P = t mod 3): V(t) and K(t + 1) have landed (the wave's loads of one more
   // tile may be out).  The barrier also says that every wave has read K(t) and V(t - 1), whose
-  // slots are filled next.
+  // slots are filled next.  (VR 2: V(t) was its waves' last load, and V(t + 1) takes the slot of
+  // V(t - 1))
   auto advance = [&]() __attribute__((always_inline)) {
-    TAPS_WAIT_VMCNT(BPW);
+    if (VR == 3 || loads_k) TAPS_WAIT_VMCNT(BPW);
+    else TAPS_WAIT_VMCNT(0);
     TAPS_LDS_BARRIER();
   };
-  const int ahead = loads_k ? 3 : 2;             // tiles from a step's to the one it loads
-  auto fill = [&](int P) __attribute__((always_inline)) { issue(loads_k ? P : (P + 2) % 3); };
+  const int ahead = loads_k ? 3 : VR - 1;        // tiles from a step's to the one it loads
+  auto fill = [&](int P, int PV) __attribute__((always_inline)) {
+    issue(loads_k ? P : (PV + VR - 1) % VR);
+  };
   // Step t: the weights and products of tile t, from its scores (s0, s1; m0: the largest of s0),
   // and the scores of tile t + 1 (past the last one: of zeros) into n0 and, when they are used
   // up, s0.
   float m0 = -INFINITY;
-  auto step = [&](auto pt, int t, f32x16& s0, f32x16& s1, f32x16& n0)
+  auto step = [&](auto pt, auto pv, int t, f32x16& s0, f32x16& s1, f32x16& n0)
                   __attribute__((always_inline)) {
-    constexpr int P = decltype(pt)::value, PN = (P + 1) % 3;
+    constexpr int P = decltype(pt)::value, PN = (P + 1) % 3, PV = decltype(pv)::value;
     advance();
 #pragma unroll
     for (int i = 0; i < 4; ++i) read_k(PN, i);
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) read_v(P, 0, db);
+    for (int db = 0; db < NDB; ++db) read_v(PV, 0, db);
     rescale(tile_max(s0, s1, k0 + t * KT, m0));
     __builtin_amdgcn_sched_barrier(0);
     const bf16x8 w0 = weights(s0, 0);
     scores(PN, 0, 0, NKK, n0);
     interleave<NKK, 1, 24 / NKK - 1, 1>();
     __builtin_amdgcn_sched_barrier(0);
-    fill(P);
+    fill(P, PV);
     __builtin_amdgcn_sched_barrier(0);
-    product(P, 0, w0);
+    product(PV, 0, w0);
     const bf16x8 w1 = weights(s0, 1);
     interleave<NDB, 2, 16 / NDB, 8 / NDB>();
     __builtin_amdgcn_sched_barrier(0);
-    product(P, 1, w1);
+    product(PV, 1, w1);
     scores(PN, 1, 0, NKK / 2, s0);
     const bf16x8 w2 = weights(s1, 0);
     interleave<NDB + NKK / 2, 2, 2, 1>();
     __builtin_amdgcn_sched_barrier(0);
     prepare(t + 1 + ahead);
     __builtin_amdgcn_sched_barrier(0);
-    product(P, 2, w2);
+    product(PV, 2, w2);
     scores(PN, 1, NKK / 2, NKK, s0);
     const bf16x8 w3 = weights(s1, 1);
     asm volatile("" : "+v"(l_run));               // (the sum is not put off to the next step)
     interleave<NDB + NKK / 2, 2, 2, 1>();
     __builtin_amdgcn_sched_barrier(0);
-    product(P, 3, w3);
+    product(PV, 3, w3);
     m0 = largest(n0);
     asm volatile("" : "+v"(m0));
   };
@@ -598,8 +602,10 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
       for (int kk = 0; kk < NKK; ++kk) q[kk] = *(const bf16x8*)(qp + kk * 16 + hl * 8);
     }
     prepare(1);
-    issue(1);
-    prepare(2);
+    if (VR == 3 || loads_k) {
+      issue(1);
+      prepare(2);
+    }
     if (loads_k) {
       issue(2);
       prepare(3);
@@ -609,7 +615,7 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
     if (wrow0 > last) {                           // no rows: the wave only loads
       for (int t = 0, P = 0; t < nt; ++t, P = P == 2 ? 0 : P + 1) {
         advance();
-        fill(P);
+        fill(P, VR == 3 ? P : t & 1);
         prepare(t + 1 + ahead);
       }
     } else {
@@ -619,10 +625,21 @@ __global__ __launch_bounds__(64 * W) void chunk_bf16_kernel(const ChunkArgs A) {
       scores(0, 0, 0, NKK, a);
       scores(0, 1, 0, NKK, b);
       m0 = largest(a);
-      for (int t = 0; t < nt; t += 3) {   // (one exit: with three the accumulators moved about)
-        step(Slot<0>(), t, a, b, c);
-        if (t + 1 < nt) step(Slot<1>(), t + 1, c, a, b);
-        if (t + 2 < nt) step(Slot<2>(), t + 2, b, c, a);
+      if constexpr (VR == 3) {
+        for (int t = 0; t < nt; t += 3) {   // (one exit: with three the accumulators moved about)
+          step(Slot<0>(), Slot<0>(), t, a, b, c);
+          if (t + 1 < nt) step(Slot<1>(), Slot<1>(), t + 1, c, a, b);
+          if (t + 2 < nt) step(Slot<2>(), Slot<2>(), t + 2, b, c, a);
+        }
+      } else {
+        for (int t = 0; t < nt; t += 6) {
+          step(Slot<0>(), Slot<0>(), t, a, b, c);
+          if (t + 1 < nt) step(Slot<1>(), Slot<1>(), t + 1, c, a, b);
+          if (t + 2 < nt) step(Slot<2>(), Slot<0>(), t + 2, b, c, a);
+          if (t + 3 < nt) step(Slot<0>(), Slot<1>(), t + 3, a, b, c);
+          if (t + 4 < nt) step(Slot<1>(), Slot<0>(), t + 4, c, a, b);
+          if (t + 5 < nt) step(Slot<2>(), Slot<1>(), t + 5, b, c, a);
+        }
       }
     }
     TAPS_WAIT_VMCNT(0);   // (empty) loads past the piece land before the LDS is released
@@ -977,8 +994,9 @@ hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if constexpr (sizeof(T) == 4) chunk_f32_kernel<HD><<<grid, kThreads, 0, s>>>(A);
-  else if (p.rows == 256) chunk_bf16_kernel<HD, 8><<<grid, 512, 0, s>>>(A);
-  else chunk_bf16_kernel<HD, 4><<<grid, 256, 0, s>>>(A);
+  else if (p.rows == 256) chunk_bf16_kernel<HD, HD == 128 ? 8 : 4, 3><<<grid, 512, 0, s>>>(A);
+  else if (p.pair) chunk_bf16_kernel<HD, 4, HD == 128 ? 2 : 3><<<grid, 256, 0, s>>>(A);
+  else chunk_bf16_kernel<HD, 4, 3><<<grid, 256, 0, s>>>(A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 0) return e;
   if constexpr (sizeof(T) == 2)
@@ -990,19 +1008,22 @@ hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
 
 }  // namespace
 
-// Tiles of 256 query rows use each key tile in LDS twice as often as those of 128; 128 spread a
-// short prompt over more CUs, and at head_dim 64, where the exponentials bound the kernel, three
-// workgroups of them share a CU.  us a call with 256 / 128 rows (32/8 heads): head_dim 128, prompts
-// of 600, 1024, 1536, 2048, 2560 and 4096 tokens 24 / 19, 40 / 27, 52 / 41, 67 / 61, 80 / 90 and
-// 145 / 182; 512 tokens over 8K 92 / 105, 8 prompts of 100 to 1000 47 / 50; head_dim 64, prompts of
-// 1024 and 2048 29 / 20 and 47 / 39, 16 requests of 1 to 1024 tokens over 16K to 1 47 / 39, 512
-// over 8K 60 / 63.
-// Cuts.  Pieces: one per CU (three share one at head_dim 64: 16 requests of 1 to 1024 tokens take
-// 39 us with 512 for 44 with 256; fp32: 512).  min_units: mostly a piece's start and end.  gain:
-// what the second kernel costs; an fp32 unit takes as long as four in bf16.  Where 64 tiles or more
-// take part the pieces may be longer, and where max_len then lets none be cut the second kernel is
-// not launched: a prompt of 1024 takes 27 us with 8 and 30 with 4, 16 tokens over 900 keys 21 and
-// 15.
+// Tiles of 256 query rows use each key tile in LDS twice as often as those of 128.  128 spread a
+// short prompt over more CUs; with a ring of two tiles of V two workgroups share a CU (pair), so
+// that one computes while the other begins or ends; at head_dim 64, where the exponentials bound
+// the kernel, three do with rings of three.  us a call (32/8 heads of 128) with 256 rows / 128
+// alone / 128 in pairs: prompts of 1024, 1536, 2048 and 2560 tokens 40 / 27.5 / 29, 52 / 42 / 45,
+// 67 / 61 / 58 and 80 / 90 / 72, of 4096 145 / 182 / 160; 1200 after 1200 67 / 73 / 63; 8 prompts
+// of 1000 122 / - / 111, 8 of 100 to 1000 46 / 50 / 39; 512 after 8K 92 / 105 / 98; 64 requests of
+// one token after 50 to 300 keys - / 20 / 15, 256 of them - / 70 / 48, 16 after 512 to 16K 95 / 84
+// / 79.  head_dim 64, 256 / 128 rows: prompts of 1024 and 2048 29 / 20 and 47 / 39, 16 requests of
+// 1 to 1024 tokens over 16K to 1 47 / 39, 512 over 8K 60 / 63.
+// Cuts.  Pieces: one per CU, or two where there are many tiles (16 requests of one token 79 us with
+// 512 for 86 with 256, one of 16 tokens after 32K 39 for 33) and at head_dim 64 (16 requests of 1
+// to 1024 tokens 39 for 44); fp32: 512.  min_units: mostly a piece's start and end.  gain: what the
+// second kernel costs; an fp32 unit takes as long as four in bf16.  Where 64 tiles or more take
+// part the pieces may be longer, and where max_len then lets none be cut the second kernel is not
+// launched: a prompt of 1024 takes 27 us with 8 and 30 with 4, 16 tokens over 900 keys 21 and 15.
 // Bounds of what the device finds.  Tiles: the requests' rows / M, and one more per request.
 // With L >= (sum of tiles * units) * Hkv / target, the cut requests (units > L) have at most
 // target / Hkv tiles between them, and at most twice as many pieces as their tiles * units / L.
@@ -1010,12 +1031,15 @@ ChunkPlan plan_chunk(int batch, int rows, int Hq, int Hkv, int head_dim, int max
                      int dtype) {
   ChunkPlan p;
   const int64_t heads = (int64_t)rows * Hq;       // query rows of all heads
-  p.rows = dtype == TAPS_FP32 ? kMF
-           : head_dim == 64 || (heads <= 65536 && max_len <= 2048) ? 128 : 256;
+  const bool small = max_len <= 2560 || (int64_t)rows * (Hq / Hkv) <= (int64_t)64 * batch;
+  p.rows = dtype == TAPS_FP32 ? kMF : head_dim == 64 || small ? 128 : 256;
+  p.pair = p.rows == 128 && head_dim == 128 &&
+           (max_len > 2560 || heads / 128 + (int64_t)batch * Hkv > 300);
   p.cut = p.rows == kMF ? ChunkCut{9, 2, 1}
           : p.rows == 256
               ? ChunkCut{8, 4, 6}
-              : ChunkCut{head_dim == 64 ? 9 : 8, heads > 8192 ? 8 : 4, 8};
+              : ChunkCut{head_dim == 64 || (int64_t)batch * Hkv >= 128 ? 9 : 8,
+                         heads > 8192 ? 8 : 4, 8};
   const int64_t M = p.rows, target = (int64_t)1 << p.cut.target_log2;
   const int64_t tiles = std::min<int64_t>((int64_t)rows * (Hq / Hkv) / M + batch,
                                           (int64_t)rows * (Hq / Hkv));

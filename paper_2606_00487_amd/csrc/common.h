@@ -193,6 +193,7 @@ struct ChunkCut {
 };
 struct ChunkPlan {
   int rows;            // query rows of a tile
+  bool pair;           // two workgroups of 128 rows share a CU (head_dim 128)
   ChunkCut cut;
   int64_t items;       // most pieces per KV head
   int64_t cut_groups;  // groups of rows per KV head of requests that are cut (0: none ever is)

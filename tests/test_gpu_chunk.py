@@ -413,3 +413,27 @@ def test_many_requests_whose_starts_decrease():
     call(Q, K, V, table, odd, kv, max_len, out=buf[1:605])
     torch.cuda.synchronize()
     assert (buf[0] == 7).all() and (buf[601:] == 7).all()
+
+
+@pytest.mark.parametrize("n,kv,bound_of_len", [(1168, 1168, 1168), (1172, 1172, 1172), (600, 600, 2560),
+                                               (600, 600, 2561), (16, 3000, 3000), (17, 3000, 3000),
+                                               (1300, 2500, 2560)])
+def test_one_request_at_the_borders_of_pairs(n, kv, bound_of_len):
+    """Tiles alone and two workgroups a CU, whole and cut."""
+    check(wider(case(33, [(n, kv)], 32, 8, 128, 64, BF), bound_of_len))
+
+
+@pytest.mark.parametrize("B", [15, 16, 37, 38])
+def test_single_tokens_at_the_borders_of_pairs(B):
+    rng = np.random.default_rng(B)
+    lens = [(1, int(k)) for k in rng.integers(1, 3000, B)]
+    lens[3] = (1, 2700)
+    check(case(34, lens, 32, 8, 128, 64, BF))
+    check(case(35, [(1, min(k, 900)) for _, k in lens], 32, 8, 128, 64, BF))
+
+
+def test_ragged_prompts_in_pairs():
+    rng = np.random.default_rng(5)
+    lens = [(int(n), int(n)) for n in rng.integers(1, 700, 12)]
+    check(case(36, lens, 16, 4, 128, 32, BF, lead=1, pad=2))
+    check(case(37, lens, 16, 4, 128, 32, BF, window=100), window=100)
