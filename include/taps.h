@@ -627,8 +627,8 @@ taps_status chunk_attn_paged_validate(int32_t batch, int32_t rows, int32_t Hq, i
                                       int32_t window, int32_t dtype, float scale);
 
 /* Bytes of scratch chunk_attn_paged needs (parts of tiles that are cut, none for short caches;
- * where each request begins, for more than 256; 0 for sizes that it rejects).  Calls that may
- * overlap on the GPU need scratch of their own. */
+ * where each request begins, for more than 256; 0 for sizes that it rejects).  Enough for calls
+ * with fewer rows too.  Calls that may overlap on the GPU need scratch of their own. */
 size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq, int32_t Hkv,
                                         int32_t head_dim, int32_t max_len, int32_t page_rows,
                                         int32_t dtype);
@@ -678,7 +678,7 @@ taps_status taps_logprobs_validate(int32_t batch, int32_t budget, int32_t vocab,
                                    int64_t row_stride, int32_t dtype, int32_t top);
 
 /* Bytes of scratch taps_logprobs needs (the parts that few rows are cut into; 0 for many rows or a
- * small vocabulary).  Calls that may overlap on the GPU need scratch of their own. */
+ * small vocabulary, so that fewer rows may need more).  Calls that may overlap on the GPU need scratch of their own. */
 size_t taps_logprobs_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab, int32_t dtype,
                                      int32_t top);
 

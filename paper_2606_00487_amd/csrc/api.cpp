@@ -777,7 +777,11 @@ size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq,
                                 1.0f) != TAPS_OK ||
       batch == 0 || rows == 0)
     return 0;
-  return chunk_ws_bytes(plan_chunk(batch, rows, Hq, Hkv, head_dim, max_len, dtype), head_dim);
+  // (few rows are cut into shorter pieces, and from a shorter cache on)
+  const int few = std::min(rows, std::max(1, 8192 / Hq));
+  const ChunkPlan all = plan_chunk(batch, rows, Hq, Hkv, head_dim, max_len, dtype);
+  const ChunkPlan least = plan_chunk(batch, few, Hq, Hkv, head_dim, max_len, dtype);
+  return std::max(chunk_ws_bytes(all, head_dim), chunk_ws_bytes(least, head_dim));
 }
 
 taps_status chunk_attn_paged(const void* Q, int64_t q_stride, const void* K_pages,

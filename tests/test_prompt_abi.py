@@ -149,3 +149,14 @@ def test_chunk_refuses_more_workgroups_than_a_launch_holds(lib):
     assert v(1 << 19, 1 << 20, 32, 8, 128, 4096, 64, 0, 0, 1.0) == OK
     assert v(1, 1 << 24, 64, 8, 128, 4096, 64, 0, 0, 1.0) == OK
     assert v(1, 1 << 24, 64, 8, 64, 4096, 64, 0, 1, 1.0) == UNS
+
+
+def test_chunk_scratch_is_enough_for_fewer_rows(lib):
+    ws = lib.chunk_attn_paged_workspace_bytes
+    sizes = [1, 2, 16, 33, 63, 64, 65, 255, 256, 257, 300, 640, 1024, 1025, 2048, 5000, 70000]
+    for Hq, Hkv, hd, dt in ((32, 8, 128, 0), (16, 2, 64, 0), (5, 1, 128, 0), (64, 64, 128, 0),
+                            (32, 8, 128, 1), (4, 2, 64, 1)):
+        for batch in (1, 3, 16, 40, 300):
+            for max_len in (64, 192, 193, 700, 768, 769, 1000, 1024, 1025, 2560, 2561, 9000, 100000):
+                got = [ws(batch, n, Hq, Hkv, hd, max_len, 64, dt) for n in sizes]
+                assert got == sorted(got), (Hq, Hkv, hd, dt, batch, max_len, got)
