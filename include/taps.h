@@ -678,7 +678,8 @@ taps_status taps_logprobs_validate(int32_t batch, int32_t budget, int32_t vocab,
                                    int64_t row_stride, int32_t dtype, int32_t top);
 
 /* Bytes of scratch taps_logprobs needs (the parts that few rows are cut into; 0 for many rows or a
- * small vocabulary, so that fewer rows may need more).  Calls that may overlap on the GPU need scratch of their own. */
+ * small vocabulary, so that fewer rows may need more).  Calls that may overlap on the GPU need
+ * scratch of their own. */
 size_t taps_logprobs_workspace_bytes(int32_t batch, int32_t budget, int32_t vocab, int32_t dtype,
                                      int32_t top);
 
