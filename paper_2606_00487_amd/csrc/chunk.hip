@@ -28,8 +28,8 @@
 // 1.0, its pages 1.4, the first tile 1.3, the first scores 0.4, its end 1.1), which bounds ragged
 // batches; at head_dim 64 the exponentials take longer than the products.
 // fp32 (v_mfma_f32_16x16x4_f32): four waves of 16 query rows, key tiles of 32 staged through
-// registers, bound by the fp32 matrix instructions: a prompt of 2048 tokens, 32/8 heads of 128, 380
-// us, 90 TFLOP/s (a library product: 145).  128 rows a tile take 352 us there, and 41 for 47 us for
+// registers, bound by the fp32 matrix instructions: a prompt of 2048 tokens, 32/8 heads of 128, 370
+// us, 93 TFLOP/s (a library product: 145).  128 rows a tile take 352 us there, and 41 for 47 us for
 // 16 tokens over 8K, but 254 for 225 us for 8 ragged requests.
 #include <algorithm>
 #include <climits>
@@ -743,10 +743,12 @@ __global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) 
   const float* const Vp = (const float*)A.V + (size_t)kvh * HD;
   const int32_t* const bt = A.pk.btab + (size_t)p.b * A.pk.max_pages;
   f32x4 xk[LD], xv[LD];
-  auto load = [&](int t) {   // keys outside [lo, k_end) read as zeros
+  auto page_of = [&](int t) {   // (past the piece: any)
+    const int entry = bt[min((k0 + t * KT) >> A.pk.page_shift, A.pk.max_pages - 1)];
+    return min(max(entry, 0), A.pk.num_pages - 1);
+  };
+  auto load = [&](int t, int page) {   // keys outside [lo, k_end) read as zeros
     const int r0 = k0 + t * KT;
-    const int entry = bt[min(r0 >> A.pk.page_shift, A.pk.max_pages - 1)];
-    const int page = min(max(entry, 0), A.pk.num_pages - 1);
     const size_t prow = ((size_t)page << A.pk.page_shift) + (r0 & ((1 << A.pk.page_shift) - 1));
 #pragma unroll
     for (int j = 0; j < LD; ++j) {
@@ -772,14 +774,20 @@ __global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) 
   // the reference stays in score units: the exponent is (s - m) * scale, whose rounding error
   // falls with the weight of the term
   float m_ref = -INFINITY, l_run = 0.f;
+  int page = 0;   // of the next tile to load
   if (nt > 0) {
-    load(0);
+    const int first = page_of(0);
+    page = page_of(1);
+    load(0, first);
     keep(0);
   }
   __syncthreads();
   for (int t = 0; t < nt; ++t) {
     const int key = k0 + t * KT, buf = t & 1;
-    if (t + 1 < nt) load(t + 1);
+    if (t + 1 < nt) {
+      load(t + 1, page);
+      page = page_of(t + 2);
+    }
     if (key <= pos_hi && key + KT > w_lo) {
       f32x4 s[2];
 #pragma unroll
