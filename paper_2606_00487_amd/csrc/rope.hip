@@ -231,8 +231,8 @@ hipError_t launch_t(const RopeArgs& A, int interleaved, hipStream_t s) {
   constexpr int HPW = kWave / (HD / (2 * RUN));
   const int passes = (A.Hq + HPW - 1) / HPW + 2 * ((A.Hkv + HPW - 1) / HPW);
   // few rows: a row's passes over several waves, each of which forms the row's angles (us of 600,
-  // 1024 and 2047 rows of 32/8 heads of 128 with up to 2048 / 4096 / 8192 waves: 6.5 / 8.2 / 8.2, 8.3 /
-  // 9.7 / 11.9, 11.8 / 12.3 / 15.6; of 64 rows 4.2)
+  // 1024 and 2047 rows of 32/8 heads of 128 with up to 2048 / 4096 / 8192 waves: 6.5 / 8.2 / 8.2,
+  // 8.3 / 9.7 / 11.9, 11.8 / 12.3 / 15.6; of 64 rows 4.2)
   const int per_row = std::min(passes, std::max(1, 2048 / A.rows));
   const int64_t units = (int64_t)A.rows * per_row;
   const unsigned grid = (unsigned)std::min<int64_t>((units + kWaves - 1) / kWaves, 2048);
