@@ -655,7 +655,9 @@ size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq,
  *                2^20, and rows * Hq / 128 (fp32: 64) + batch * Hkv below 8 million or so (a
  *                launch's threads are counted in 32 bits)
  *   head_dim     64 or 128; Hq a multiple of Hkv
- *   max_len      [host] upper bound of kv_len, at most 2^30
+ *   max_len      [host] upper bound of kv_len, at most 2^30; it picks the tiles, so that one near
+ *                the lengths is the faster one (a prompt of 1024, 32/8 heads of 128, takes 27 us,
+ *                39 under a bound of 32K)
  *   window       0: none; else at least 1
  *   dtype        TAPS_BF16 (fp32 accumulation, weights rounded to bf16 for the second product,
  *                output rounded to nearest even) or TAPS_FP32

@@ -732,7 +732,8 @@ class PagedChunkAttention:
 
     def __init__(self, batch, max_rows, Hq, Hkv, head_dim, max_len, page_rows, dtype=BF16,
                  scale=None, window=0):
-        """max_rows: most rows (new tokens of all requests) of a call."""
+        """max_rows: most rows (new tokens of all requests) of a call.  max_len: most cache rows of
+        a request; near the real lengths the tiles fit best."""
         self.lib = load()
         self.scale = float(scale if scale is not None else head_dim ** -0.5)
         self.batch, self.max_rows, self.max_len, self.window = batch, max_rows, max_len, window
