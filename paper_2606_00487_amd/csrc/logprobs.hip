@@ -7,7 +7,9 @@
 // about a reference of its own, which moves only when a value exceeds it by 2^8; they are joined in
 // 64 bits.  A weight is 2^t, t = fma(x, log2 e, c) with c = -(reference * log2 e) rounded: what the
 // rounding and the constant's error add to every t of a thread is known and taken out in the join,
-// so that a weight near the top is good to 2^-23.
+// so that a weight near the top is good to 2^-23.  The largest value's own weight is 1 without a
+// rounding: a thread that holds it takes what it added for it out again.  So Z >= 1, no log
+// probability is above 0, and a row of which a mask leaves one value gives exactly 0.
 //
 // The pass takes values as they are.  An infinity or NaN makes S one too: a wave that ends with
 // such a sum goes over its values again with those below kLow, and NaN, lifted to kLow (a wave
@@ -174,7 +176,7 @@ __device__ constexpr float next_up(float x) {
 // ln p of the value v, from the row's maximum and sum
 __device__ inline float log_prob(float v, float M, double Z, double lnz) {
   if (v != v || Z == 0.0) return -INFINITY;
-  return v == M ? (float)-lnz : (float)(((double)v - (double)M) - lnz);
+  return v == M ? (float)(0.0 - lnz) : (float)(((double)v - (double)M) - lnz);   // (no -0)
 }
 // the value of a value_key
 __device__ inline float key_value(uint32_t k) {
@@ -371,12 +373,18 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
   // ---- the waves' sums about their own maxima (ref -inf: a thread without values)
   {
     const float m = wave_max(best);
-    double a = 0.0, k = 0.0;
+    double a = 0.0, k = 0.0, rz = Z, rs = S;
     if (ref != -INFINITY) {
       k = -(double)c + (double)ref * kLog2eRest - (double)m * 1.4426950408889634;
       a = power(k);
     }
-    const double z = wave_sum(a * Z), sn = wave_sum(a * ((double)S + k * Z));
+    // (`best` was added about the reference that is in force: a larger one moves it)
+    const bool holds = best == m && ref != -INFINITY;
+    if (holds) {
+      const float t = fmaf(best, kLog2e, c), w = __builtin_amdgcn_exp2f(t);
+      rz -= w, rs -= fmaf(w, t, 0.f);
+    }
+    const double z = wave_sum(a * rz + (holds ? 1.0 : 0.0)), sn = wave_sum(a * (rs + k * rz));
     s_max[tid] = best;
     if (lane == 0) s_m[wave] = m, s_z[wave] = z, s_s[wave] = sn, s_int[wave] = before;
     if (tid == 0) s_count = 0;
@@ -445,7 +453,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
   if (tid == 0 && A.parts == 1) {
     A.rank[row] = given ? rank : -1;
     A.logprob[row] = given ? lp(xt) : -INFINITY;
-    A.entropy[row] = Zd == 0.0 ? 0.f : (float)(lnz - Sd / Zd);
+    A.entropy[row] = Zd == 0.0 ? 0.f : (float)fmax(lnz - Sd / Zd, 0.0);
   }
   if (top == 0) return;
 
@@ -616,7 +624,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(const Logpr
   if (tid == 0) {
     A.rank[row] = p.given ? rank : -1;
     A.logprob[row] = p.given ? log_prob(p.token, M, Z, lnz) : -INFINITY;
-    A.entropy[row] = Z == 0.0 ? 0.f : (float)(lnz - S / Z);
+    A.entropy[row] = Z == 0.0 ? 0.f : (float)fmax(lnz - S / Z, 0.0);
   }
   __syncthreads();
   for (int q = tid; q < n; q += kJoinThreads) {
