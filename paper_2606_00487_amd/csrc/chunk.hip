@@ -863,8 +863,7 @@ __global__ __launch_bounds__(kThreads) void chunk_f32_kernel(const ChunkArgs A) 
     if (slot >= A.slots) return;
     const size_t at = (size_t)slot * kMF + wave * 16 + c;
     out = A.wsO + at * HD;
-    // (base 2, after the scale)
-    if (g == 0) A.wsML[at] = make_float2(m_ref * A.scale_log2, l);
+    if (g == 0) A.wsML[at] = make_float2(m_ref, l);   // (in score units)
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r)
@@ -886,9 +885,12 @@ __device__ inline void store4(__bf16* p, const f32x4& x) {
   for (int t = 0; t < 4; ++t) r[t] = (__bf16)x[t];
   *(bf16x4*)p = r;
 }
-// weight of a part about the reference m (base 2) where the sum's is M
-__device__ inline float part_weight(float m, float M) {
-  return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+// weight of a part about the reference m where the sum's is M: both of base 2 in bf16, whose parts
+// were summed about that very number, and in fp32 in score units, as in the parts' own exponents
+template <typename T>
+__device__ inline float part_weight(const ChunkArgs& A, float m, float M) {
+  if (m == -INFINITY) return 0.f;
+  return __builtin_amdgcn_exp2f(sizeof(T) == 4 ? (m - M) * A.scale_log2 : m - M);
 }
 template <typename T, int HD, int M, int ROWS, int GROUPS>
 __global__ __launch_bounds__(kCombineThreads) void chunk_combine_kernel(const ChunkArgs A) {
@@ -929,7 +931,7 @@ __global__ __launch_bounds__(kCombineThreads) void chunk_combine_kernel(const Ch
       float Mc = Mx;
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) Mc = fmaxf(Mc, ml[k].x);
-      const float a = part_weight(Mx, Mc);
+      const float a = part_weight<T>(A, Mx, Mc);
       L *= a;
 #pragma unroll
       for (int w = 0; w < W; ++w) acc[w] *= a;
@@ -937,7 +939,7 @@ __global__ __launch_bounds__(kCombineThreads) void chunk_combine_kernel(const Ch
       for (int k = 0; k < kAhead; ++k) {
         if (s0 + k * GROUPS >= pieces) continue;
         if (ml[k].x != -INFINITY) {
-          const float e = part_weight(ml[k].x, Mc);
+          const float e = part_weight<T>(A, ml[k].x, Mc);
           L += e * ml[k].y;
 #pragma unroll
           for (int w = 0; w < W; ++w) acc[w] += e * x[k][w];
@@ -956,7 +958,7 @@ __global__ __launch_bounds__(kCombineThreads) void chunk_combine_kernel(const Ch
       float Mc = Mx;
 #pragma unroll
       for (int g = 0; g < GROUPS - 1; ++g) Mc = fmaxf(Mc, s_ml[g][rr].x);
-      const float a = part_weight(Mx, Mc);
+      const float a = part_weight<T>(A, Mx, Mc);
       L *= a;
 #pragma unroll
       for (int w = 0; w < W; ++w) acc[w] *= a;
@@ -964,7 +966,7 @@ __global__ __launch_bounds__(kCombineThreads) void chunk_combine_kernel(const Ch
       for (int g = 0; g < GROUPS - 1; ++g) {
         const float2 ml = s_ml[g][rr];
         if (ml.x != -INFINITY) {
-          const float e = part_weight(ml.x, Mc);
+          const float e = part_weight<T>(A, ml.x, Mc);
           L += e * ml.y;
 #pragma unroll
           for (int w = 0; w < W; ++w) acc[w] += e * s_acc[g][rr][tr][w];
