@@ -587,7 +587,7 @@ taps_status taps_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling
  *   inv_freq        DEVICE [rot_dim / 2] fp64, 8-byte aligned: the pairs' turns per position
  *   q_norm, k_norm  DEVICE [head_dim] RMSNorm weights in the call's dtype, 16-byte aligned, or
  *                   NULL: no norm
- *   norm_eps        finite and >= 0
+ *   norm_eps        finite and >= 0 (0: a head of zeros becomes NaN)
  *   mscale          factor of cosines and sines, finite (1 without stretching)
  *   rot_dim         dims of a head that turn, from its first on: a multiple of 8, 8 .. head_dim
  *   interleaved     0: pair j is (j, j + rot_dim / 2); 1: (2j, 2j + 1) */

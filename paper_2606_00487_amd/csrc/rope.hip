@@ -15,6 +15,9 @@
 // product no better than 2^-4 of a radian.  The reduced angle (|x| <= pi / 4, off by 2^-25) goes
 // through the Taylor series of sine and cosine to x^11 and x^10 (remainders below 2^-33).
 //
+// The norm takes heads of any size: where the mean square leaves 2^-100 .. 2^100 (values near the
+// ends of the type's range, an eps of almost nothing) the head is scaled by a power of two first.
+//
 // Bound: HBM, everything is read and written once.  16,384 rows of 32/8 heads of 128 in bf16 (403
 // MB) take 83 us, 4.8 TB/s (a copy of 2 GB: 5.0); 2047 rows of 16/2 heads of 64 in fp32 (21 MB) 7.7
 // us.
@@ -79,18 +82,26 @@ struct Run<float, 4> {
 };
 
 template <int CTRL>
-__device__ inline float dpp_add(float x) {
-  return x + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, 0xf, 0xf,
-                                                         true));
+__device__ inline float dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, 0xf, 0xf, true));
 }
-// sum over the LPH (4, 8 or 16) lanes of a head, in each of them
-template <int LPH>
-__device__ inline float head_sum(float x) {
-  x = dpp_add<0xB1>(x);    // lane ^ 1
-  x = dpp_add<0x4E>(x);    // lane ^ 2
-  if constexpr (LPH >= 8) x = dpp_add<0x141>(x);    // the other four of eight
-  if constexpr (LPH == 16) x = dpp_add<0x140>(x);   // the other eight of sixteen
+// f over the LPH (4, 8 or 16) lanes of a head, the same in each of them
+template <int LPH, typename F>
+__device__ inline float over_head(float x, F f) {
+  x = f(x, dpp<0xB1>(x));    // lane ^ 1
+  x = f(x, dpp<0x4E>(x));    // lane ^ 2
+  if constexpr (LPH >= 8) x = f(x, dpp<0x141>(x));    // the other four of eight
+  if constexpr (LPH == 16) x = f(x, dpp<0x140>(x));   // the other eight of sixteen
   return x;
+}
+// eps + the mean of a head's squares, EPL values a lane
+template <int HD, int EPL>
+__device__ inline float mean_square(const float* x, float eps) {
+  float sq = 0.f;
+#pragma unroll
+  for (int t = 0; t < EPL; ++t) sq = fmaf(x[t], x[t], sq);
+  sq = over_head<HD / EPL>(sq, [](float a, float b) { return a + b; });
+  return fmaf(sq, 1.f / HD, eps);
 }
 
 // m cos and m sin of pos * f, f in turns per position
@@ -187,10 +198,25 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeArgs A, int pe
           Rn::widen(x0[i], x);
           Rn::widen(x1[i], x + RUN);
           if (kind == 0 ? A.qw != nullptr : A.kw != nullptr) {
-            float sq = 0.f;
+            float ms = mean_square<HD, EPL>(x, A.eps);
+            // squares beyond 32 bits, or so small that they lose theirs: the head and the root of
+            // eps by a power of two near 1 (the norm does not depend on it)
+            const bool far = !(ms > 0x1p-100f && ms < 0x1p100f);
+            if (__ballot(far)) {
+              float mx = 0.f;
 #pragma unroll
-            for (int t = 0; t < EPL; ++t) sq = fmaf(x[t], x[t], sq);
-            const float ms = fmaf(head_sum<LPH>(sq), 1.f / HD, A.eps);
+              for (int t = 0; t < EPL; ++t) mx = fmaxf(mx, fabsf(x[t]));
+              mx = over_head<LPH>(mx, [](float a, float b) { return fmaxf(a, b); });
+              int e = __builtin_amdgcn_frexp_expf(mx);   // (0 of 0, infinity and NaN)
+              if (A.eps > 0.f) {
+                const int half = (__builtin_amdgcn_frexp_expf(A.eps) + 1) >> 1;
+                e = mx > 0.f ? max(e, half) : half;
+              }
+              e = far ? e : 0;
+#pragma unroll
+              for (int t = 0; t < EPL; ++t) x[t] = __builtin_ldexpf(x[t], -e);
+              ms = mean_square<HD, EPL>(x, __builtin_ldexpf(A.eps, -2 * e));
+            }
             float rs = __builtin_amdgcn_rsqf(ms);
             // one Newton step: the instruction alone is off by a unit in the last place
             const float e = fmaf(-ms * rs, rs, 1.f);
