@@ -660,7 +660,8 @@ size_t chunk_attn_paged_workspace_bytes(int32_t batch, int32_t rows, int32_t Hq,
  *                39 under a bound of 32K)
  *   window       0: none; else at least 1
  *   dtype        TAPS_BF16 (fp32 accumulation, weights rounded to bf16 for the second product,
- *                output rounded to nearest even) or TAPS_FP32
+ *                output rounded to nearest even) or TAPS_FP32.  For batches of one token per
+ *                request decode_attn_paged is mostly faster and, in bf16, more exact
  *   scale        softmax scale, finite and > 0
  *   O            [rows][Hq][head_dim] in dtype, 16-byte aligned; not in the memory of Q or of the
  *                pools (checked)
