@@ -22,7 +22,9 @@
 // maximum (at all of them if a second batch reaches the bound), and what they find is ranked by
 // counting.  More than kCand values at the bound raise it: to the k-th of those kept, or past it
 // where it occurs too often.  Places that are left (ties, masked values) go value by value: the
-// largest value not yet taken, then its places in index order.
+// largest value not yet taken, then its places in index order.  Rows whose maximum is not an ordinary
+// number have no such bound and find all their alternatives so, a scan of the row for each distinct
+// value: 64 fp32 rows of 151,936 205 us with 5 alternatives, 2070 with 64 (ordinary ones 19.5, 27).
 //
 // Bound: HBM; in bf16 the vector unit is close behind (7.7 instructions an element, one of them the
 // exponential).  2048 rows of 151,936 in bf16 (622 MB) take 121 us, 5.1 TB/s; 64 of them, in four
@@ -204,7 +206,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(const LogprobArgs A)
   const size_t at_part = (size_t)row * A.parts + part;
   uint64_t* const keys = A.keys + at_part * top;
   if (A.n_nodes && row % A.budget >= A.n_nodes[row / A.budget]) {
-    if (part > 0) return;   // (with parts the second kernel writes the same)
+    if (part > 0) return;   // (part 0 writes such a row, the second kernel leaves it as it is)
     if (tid < top) tidx[tid] = -1, tlp[tid] = 0.f;
     if (tid == 0) A.logprob[row] = 0.f, A.entropy[row] = 0.f, A.rank[row] = -1;
     return;
