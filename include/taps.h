@@ -569,7 +569,13 @@ taps_status taps_sample(const void *logits, int64_t row_stride, int32_t batch, i
  *                     slower, the fastest as before (rot_dim at least 4)
  *   TAPS_ROPE_YARN    by parts (YaRN, arXiv 2309.00071, alpha 1 and beta 32): with r = L f_j / (2
  *                     pi) turns over the trained length and g = (r - 1) / 31 clamped to [0, 1],
- *                     g f_j + (1 - g) f_j / s; cosines and sines are multiplied by 0.1 ln s + 1 */
+ *                     g f_j + (1 - g) f_j / s; cosines and sines are multiplied by 0.1 ln s + 1.
+ *                     The ramp is the paper's, linear in the turns r.  Many checkpoints that name
+ *                     this kind were run with another, linear in the pair's index between the two
+ *                     pairs (rounded) where r is 32 and 1: at theta 1e6, 128 dims, L 32768 and s 4
+ *                     pair 32 turns 0.60 f_j there and 0.35 f_j here.  For those, and for any other
+ *                     kind, fill taps_rope.inv_freq and mscale oneself; nothing here is compared
+ *                     with a released model */
 typedef enum {
   TAPS_ROPE_PLAIN = 0,
   TAPS_ROPE_LINEAR = 1,
