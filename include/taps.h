@@ -712,7 +712,7 @@ size_t taps_logprobs_workspace_bytes(int32_t batch, int32_t budget, int32_t voca
  * (infinite values too), 0 for NaN, as in taps_sample at T = 1.  The rank order is value
  * descending, then index ascending; -0 equals +0; NaN is last.  A row of NaN alone has log
  * probabilities -inf and entropy 0.  Sums are fp32 per thread, joined in fp64; log probabilities
- * are at most 0 and entropies at least 0, and both are 0 where the largest value alone has a weight.
+ * are at most 0 and entropies at least 0, both 0 where the largest value alone has a weight.
  * Rows whose largest value is 1e6 or more, or -999,000 or less, take a scan of the row for each
  * alternative (64 fp32 rows of 151,936: 205 us with 5, 2070 with 64, for 19.5 and 27). */
 taps_status taps_logprobs(const void *logits, int64_t row_stride, int32_t batch, int32_t budget,

@@ -659,9 +659,9 @@ def rope_frequencies(rot_dim, theta=1e6, scaling="none", factor=1.0, trained_len
                      device="cuda"):
     """taps_rope_frequencies: the turns per position of a head's rot_dim / 2 pairs in radians
     (float64 tensor) and the factor of cosines and sines.  scaling: "none", "linear", "ntk" or
-    "yarn" (positions up to `factor` times the trained length).  "yarn" is the paper's ramp, linear in
-    a pair's turns; a checkpoint that was run with a ramp linear in the pair's index needs its own
-    frequencies, which PagedQKRope takes as they are (see include/taps.h)."""
+    "yarn" (positions up to `factor` times the trained length).  "yarn" is the paper's ramp, linear
+    in a pair's turns; a checkpoint that was run with a ramp linear in the pair's index needs its
+    own frequencies, which PagedQKRope takes as they are (see include/taps.h)."""
     if scaling not in _lib.ROPE_SCALINGS:
         raise ValueError(
             f"scaling: expected one of {', '.join(_lib.ROPE_SCALINGS)}, got {scaling!r}")

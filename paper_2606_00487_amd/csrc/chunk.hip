@@ -26,11 +26,12 @@
 // library's product keeps them busier at 1.5 GHz, to the same product of the two.  16 tokens over
 // 32,768 keys: 33 us, 4.1 TB/s with the join.  A piece costs 5.4 us besides its steps (finding it
 // 1.0, its pages 1.4, the first tile 1.3, the first scores 0.4, its end 1.1), which bounds ragged
-// batches; at head_dim 64 the exponentials take longer than the products.
+// batches; at head_dim 64 the vector unit (32 exponentials a step) is the fuller one.
 // fp32 (v_mfma_f32_16x16x4_f32): four waves of 16 query rows, key tiles of 32 staged through
 // registers, bound by the fp32 matrix instructions: a prompt of 2048 tokens, 32/8 heads of 128, 370
-// us, 93 TFLOP/s (a library product: 145).  128 rows a tile take 352 us there, and 41 for 47 us for
-// 16 tokens over 8K, but 254 for 225 us for 8 ragged requests.
+// us, 93 TFLOP/s (a library product: 145); 40 % of the LDS's active cycles are bank conflicts, 9 %
+// of all (source not traced).  128 rows a tile take 352 us there, and 41 for 47 us for 16 tokens
+// over 8K, but 254 for 225 us for 8 ragged requests.
 #include <algorithm>
 #include <climits>
 
@@ -1032,7 +1033,11 @@ hipError_t launch_t(const ChunkArgs& A, const ChunkPlan& p, hipStream_t s) {
 // 67 / 61 / 58 and 80 / 90 / 72, of 4096 145 / 182 / 160; 1200 after 1200 67 / 73 / 63; 8 prompts
 // of 1000 122 / - / 111, 8 of 100 to 1000 46 / 50 / 39; 512 after 8K 92 / 105 / 98; 64 requests of
 // one token after 50 to 300 keys - / 20 / 15, 256 of them - / 70 / 48, 16 after 512 to 16K 95 / 84
-// / 79.  head_dim 64, 256 / 128 rows: prompts of 1024 and 2048 29 / 20 and 47 / 39, 16 requests of
+// / 79.  Ragged batches, 256 / 128 rows, differ little: 16 requests of 1 to 200 tokens after 100 to
+// 2000 keys 33 / 34.5, 32 of 1 to 500 after up to 2000 46.5 / 46, 8 of 100 to 1000 after up to 1500
+// 54 / 48.5, 16 of 1 to 1024 after 1 to 16K 63.5 / 63.5, but under a bound of 4000 keys the rule
+// gives up 10 %: 16 of 1 to 500 after 100 to 4000 46.5 / 41.7, 64 of 1 to 200 104 / 97.  head_dim
+// 64, 256 / 128 rows: prompts of 1024 and 2048 29 / 20 and 47 / 39, 16 requests of
 // 1 to 1024 tokens over 16K to 1 47 / 39, 512 over 8K 60 / 63.
 // Cuts.  Pieces: one per CU, or two where there are many tiles (16 requests of one token 79 us with
 // 512 for 86 with 256, one of 16 tokens after 32K 39 for 33) and at head_dim 64 (16 requests of 1

@@ -22,9 +22,10 @@
 // maximum (at all of them if a second batch reaches the bound), and what they find is ranked by
 // counting.  More than kCand values at the bound raise it: to the k-th of those kept, or past it
 // where it occurs too often.  Places that are left (ties, masked values) go value by value: the
-// largest value not yet taken, then its places in index order.  Rows whose maximum is not an ordinary
-// number have no such bound and find all their alternatives so, a scan of the row for each distinct
-// value: 64 fp32 rows of 151,936 205 us with 5 alternatives, 2070 with 64 (ordinary ones 19.5, 27).
+// largest value not yet taken, then its places in index order.  Rows whose maximum is not an
+// ordinary number have no such bound and find all their alternatives so, a scan of the row for each
+// distinct value: 64 fp32 rows of 151,936 205 us with 5 alternatives, 2070 with 64 (ordinary ones
+// 19.5 and 27).
 //
 // Bound: HBM; in bf16 the vector unit is close behind (7.7 instructions an element, one of them the
 // exponential).  2048 rows of 151,936 in bf16 (622 MB) take 121 us, 5.1 TB/s; 64 of them, in four
